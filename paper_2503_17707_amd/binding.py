@@ -44,6 +44,14 @@ class Config(ctypes.Structure):
                 ("max_new_tokens", ctypes.c_int32), ("merge_shadow", ctypes.c_int32)]
 
 
+class KvPool(ctypes.Structure):
+    """pb_kv_pool"""
+    _fields_ = [("base", ctypes.c_void_p), ("page_stride", ctypes.c_int64), ("v_offset", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
 _SIGS = {
     "pb_layer_bytes": (ctypes.c_size_t, [ctypes.POINTER(Config)]),
     "pb_globals_bytes": (ctypes.c_size_t, [ctypes.POINTER(Config)]),
@@ -138,6 +146,28 @@ _SIGS = {
                                        ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32,
                                        ctypes.c_int32, ctypes.c_int32, ctypes.c_float,
                                        ctypes.c_void_p]),
+    "pb_op_kv_append": (ctypes.c_int, [ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                       ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p,
+                                       ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p,
+                                       ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p]),
+    "pb_op_paged_attention": (ctypes.c_int, [ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                             ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p,
+                                             ctypes.c_int32, ctypes.c_int32, ctypes.c_float, ctypes.c_int32,
+                                             ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t,
+                                             ctypes.c_void_p]),
+    "pb_op_paged_attention_workspace": (ctypes.c_size_t, [ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p,
+                                                          ctypes.c_int32]),
+    "pb_op_beam_select": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p,
+                                         ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                                         ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                         ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "pb_op_beam_select_workspace": (ctypes.c_size_t, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32]),
+    "pb_op_page_fork": (ctypes.c_int, [ctypes.c_int32, ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64,
+                                       ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int32,
+                                       ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p,
+                                       ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                       ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "pb_op_page_fork_workspace": (ctypes.c_size_t, [ctypes.c_int32, ctypes.c_int32]),
 }
 
 _lib = None
@@ -677,3 +707,184 @@ def op_layernorm(dtype: int, x, g, b, out, eps: float = 1e-5, stream=None):
     check(lib().pb_op_layernorm(dtype, _ptr(x), _ptr(g), _ptr(b), _ptr(out),
                                 1 if out.dtype == torch.float32 else 0, rows, d, eps,
                                 _stream(stream)))
+
+
+# ---- a cache of pages, and beam search over it -----------------------------------
+# A layer's pool is a tensor [n_pages, 2 (k, v), kv heads, page_size, head_dim] of any
+# strides with unit last one: a page may hold cache rows [k | v] (a permuted view) or
+# each head's tokens in a row.  What the C entry points cannot see (types, shapes,
+# strides that no argument carries, the device) is checked here.
+
+def _on_device(op, stream, *tensors):
+    """Every tensor (None: an operand left out) is on the current device, where the
+    call is enqueued, and so is a stream that is given."""
+    import torch
+
+    dev = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise PbError(PB_EINVAL, "%s: tensors on %s and on %s" % (op, tensors[0].device, t.device))
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise PbError(PB_EINVAL, "%s: tensors on %s, which is not the current device" % (op, tensors[0].device))
+    if stream is not None and stream.device_index != dev:
+        raise PbError(PB_EINVAL, "%s: the stream is another device's" % op)
+
+
+def _int32(op, name, t, *shape):
+    import torch
+
+    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
+        raise PbError(PB_EINVAL, "%s: %s must be contiguous int32 %s" % (op, name, list(shape)))
+
+
+def _storage(op, dtype, *tensors):
+    import torch
+
+    want = torch.float16 if dtype == PB_F16 else torch.bfloat16
+    for t in tensors:
+        if t.dtype != want:
+            raise PbError(PB_EINVAL, "%s: %s operand with dtype %d" % (op, t.dtype, dtype))
+
+
+def _heads(op, name, t):
+    """Row stride of [rows, heads, head_dim] whose rows are contiguous."""
+    if t.dim() != 3:
+        raise PbError(PB_EINVAL, "%s: %s must be [rows, heads, head_dim]" % (op, name))
+    rs, hs, es = t.stride()
+    if es != 1 or (hs != t.shape[2] and t.shape[1] > 1):
+        raise PbError(PB_EINVAL, "%s: the heads of a row of %s must be contiguous" % (op, name))
+    return rs
+
+
+def kv_pool(pool) -> KvPool:
+    """pb_kv_pool of a layer's pool tensor [n_pages, 2, kv heads, page_size, head_dim]."""
+    if pool.dim() != 5 or pool.shape[1] != 2 or pool.stride(4) != 1:
+        raise PbError(PB_EINVAL, "a pool is [n_pages, 2, kv heads, page_size, head_dim] with unit last stride")
+    n, _, h, ps, hd = pool.shape
+    a, b, c, d, _ = pool.stride()
+    return KvPool(pool.data_ptr(), a, b, c, d, n, ps, h, hd)
+
+
+def _tables(op, tables):
+    import torch
+
+    if tables.dtype != torch.int32 or tables.dim() != 2 or (tables.stride(1) != 1 and tables.shape[1] > 1
+                                                                      and tables.shape[0] > 0):
+        raise PbError(PB_EINVAL, "%s: tables must be int32 [rows, width] with contiguous rows" % op)
+    return tables.shape[0], tables.shape[1], (tables.stride(0) if tables.shape[0] > 1 else tables.shape[1])
+
+
+def op_kv_append(dtype: int, k, v, pool, tables, start, lens, row0=None, max_rows: Optional[int] = None, stream=None):
+    """pb_op_kv_append: tokens start[s] .. lens[s]-1 of every sequence from rows row0[s], row0[s] + 1, ... of
+    k and v [rows, kv heads, head_dim] (views of a fused projection's rows fit).  Without row0 the rows are a
+    padded batch of max_rows per sequence; max_rows defaults to rows / sequences then, to rows with row0."""
+    op = "op_kv_append"
+    c = kv_pool(pool)
+    S, width, ld = _tables(op, tables)
+    _storage(op, dtype, k, v, pool)
+    _int32(op, "start", start, S)
+    _int32(op, "lens", lens, S)
+    if row0 is not None:
+        _int32(op, "row0", row0, S)
+    n = k.shape[0]
+    if k.shape != v.shape or tuple(k.shape[1:]) != (c.n_kv_heads, c.head_dim):
+        raise PbError(PB_EINVAL, "%s: k and v must be [rows, %d, %d]" % (op, c.n_kv_heads, c.head_dim))
+    if max_rows is None:
+        max_rows = n if row0 is not None else n // max(S, 1)
+    _on_device(op, stream, k, v, pool, tables, start, lens, row0)
+    check(lib().pb_op_kv_append(dtype, k.data_ptr(), _heads(op, "k", k), v.data_ptr(), _heads(op, "v", v), n,
+                                ctypes.byref(c), tables.data_ptr(), width, ld, start.data_ptr(), lens.data_ptr(),
+                                _ptr(row0), S, max_rows, _stream(stream)))
+
+
+def paged_attention_workspace(n_seqs: int, n_heads: int, pool, width: int) -> int:
+    """Bytes of workspace with which op_paged_attention splits as it likes."""
+    return lib().pb_op_paged_attention_workspace(n_seqs, n_heads, ctypes.byref(kv_pool(pool)), width)
+
+
+def op_paged_attention(dtype: int, q, pool, tables, lens, out, scale: float = 1.0, window: int = 0, workspace=None,
+                       stream=None):
+    """pb_op_paged_attention: q and out [sequences, heads, head_dim] (rows may be strided); scale 1 for a q that is
+    divided by sqrt(head_dim) already."""
+    op = "op_paged_attention"
+    c = kv_pool(pool)
+    S, width, ld = _tables(op, tables)
+    _storage(op, dtype, q, pool, out)
+    _int32(op, "lens", lens, S)
+    if q.shape != out.shape or q.shape[0] != S or q.dim() != 3 or q.shape[2] != c.head_dim:
+        raise PbError(PB_EINVAL, "%s: q and out must be [%d, heads, %d]" % (op, S, c.head_dim))
+    _on_device(op, stream, q, pool, tables, lens, out, workspace)
+    check(lib().pb_op_paged_attention(dtype, q.data_ptr(), _heads(op, "q", q), ctypes.byref(c), tables.data_ptr(), width,
+                                      ld, lens.data_ptr(), S, q.shape[1], scale, window, out.data_ptr(),
+                                      _heads(op, "out", out), _ptr(workspace), _nbytes(workspace), _stream(stream)))
+
+
+def _nbytes(workspace):
+    if workspace is None:
+        return 0
+    if not workspace.is_contiguous():
+        raise PbError(PB_EINVAL, "a workspace must be contiguous")
+    return workspace.numel() * workspace.element_size()
+
+
+def beam_select_workspace(B: int, W: int, V: int) -> int:
+    """Bytes of workspace of op_beam_select."""
+    return lib().pb_op_beam_select_workspace(B, W, V)
+
+
+def op_beam_select(logits, scores, alive, out_scores, out_tokens, out_parents, out_alive, eos: int, pad: int,
+                   workspace, stream=None):
+    """pb_op_beam_select: logits fp32 [B W, V] (rows may be strided), scores fp32 and alive int32 [B, W], outputs
+    [B, W] (out_scores and out_alive may be scores and alive)."""
+    import torch
+
+    op = "op_beam_select"
+    if scores.dim() != 2:
+        raise PbError(PB_EINVAL, "%s: scores must be [B, W]" % op)
+    B, W = scores.shape
+    for name, t in (("scores", scores), ("out_scores", out_scores)):
+        if t.dtype != torch.float32 or t.shape != scores.shape or not t.is_contiguous():
+            raise PbError(PB_EINVAL, "%s: %s must be contiguous float32 [%d, %d]" % (op, name, B, W))
+    for name, t in (("alive", alive), ("out_tokens", out_tokens), ("out_parents", out_parents), ("out_alive", out_alive)):
+        _int32(op, name, t, B, W)
+    if (logits.dtype != torch.float32 or logits.dim() != 2 or logits.shape[0] != B * W
+            or (logits.stride(1) != 1 and logits.shape[1] > 1)):
+        raise PbError(PB_EINVAL, "%s: logits must be float32 [%d, V] with contiguous rows" % (op, B * W))
+    _on_device(op, stream, logits, scores, alive, out_scores, out_tokens, out_parents, out_alive, workspace)
+    check(lib().pb_op_beam_select(logits.data_ptr(), logits.stride(0), scores.data_ptr(), alive.data_ptr(), B, W,
+                                  logits.shape[1], eos, pad, out_scores.data_ptr(), out_tokens.data_ptr(),
+                                  out_parents.data_ptr(), out_alive.data_ptr(), _ptr(workspace), _nbytes(workspace),
+                                  _stream(stream)))
+
+
+def page_fork_workspace(out_rows: int, n_pages: int) -> int:
+    """Bytes of workspace of op_page_fork."""
+    return lib().pb_op_page_fork_workspace(out_rows, n_pages)
+
+
+def op_page_fork(dtype: int, pools, parents, tables, lens, refs, grow, out_tables, out_start, out_lens, out_refs, short_of,
+                 workspace, stream=None):
+    """pb_op_page_fork: pools [layers, n_pages, 2, kv heads, page_size, head_dim]; parents, grow, out_start, out_lens
+    int32 [out rows]; tables int32 [in rows, width], out_tables [out rows, width]; lens int32 [in rows]; refs,
+    out_refs int32 [n_pages]; short_of int32 [2]."""
+    op = "op_page_fork"
+    if pools.dim() != 6 or pools.shape[0] < 1:
+        raise PbError(PB_EINVAL, "%s: pools must be [layers, n_pages, 2, kv heads, page_size, head_dim]" % op)
+    c = kv_pool(pools[0])
+    _storage(op, dtype, pools)
+    S, width, _ = _tables(op, tables)
+    R = parents.shape[0]
+    _int32(op, "tables", tables, S, width)
+    _int32(op, "out_tables", out_tables, R, width)
+    _int32(op, "lens", lens, S)
+    for name, t in (("parents", parents), ("grow", grow), ("out_start", out_start), ("out_lens", out_lens)):
+        _int32(op, name, t, R)
+    _int32(op, "refs", refs, c.n_pages)
+    _int32(op, "out_refs", out_refs, c.n_pages)
+    _int32(op, "short_of", short_of, 2)
+    _on_device(op, stream, pools, parents, tables, lens, refs, grow, out_tables, out_start, out_lens, out_refs, short_of,
+               workspace)
+    check(lib().pb_op_page_fork(dtype, ctypes.byref(c), pools.shape[0], pools.stride(0), parents.data_ptr(), R,
+                                tables.data_ptr(), width, lens.data_ptr(), S, refs.data_ptr(), grow.data_ptr(),
+                                out_tables.data_ptr(), out_start.data_ptr(), out_lens.data_ptr(), out_refs.data_ptr(),
+                                short_of.data_ptr(), _ptr(workspace), _nbytes(workspace), _stream(stream)))

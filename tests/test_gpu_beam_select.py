@@ -1,0 +1,147 @@
+"""Beam selection against float64 candidates: widths, vocabularies, ties, banned
+and undefined logits, ended and empty hypotheses."""
+import numpy as np
+import pytest
+
+from gpu_common import log
+
+pytestmark = pytest.mark.gpu
+
+INF = float("inf")
+
+
+def _run(logits, scores, alive, eos=2, pad=1, pitch=0, in_place=False):
+    import torch
+
+    from paged_common import select64
+    from paper_2503_17707_amd import binding as pb
+
+    logits = np.asarray(logits, np.float32)
+    scores, alive = np.asarray(scores, np.float32), np.asarray(alive, np.int32)
+    (B, W), V = scores.shape, logits.shape[1]
+    log("beam select B=%d W=%d V=%d" % (B, W, V))
+    want = select64(logits, scores, alive, eos, pad)
+    lg = torch.full((B * W, V + pitch), float("nan"), device="cuda")
+    lg[:, :V] = torch.from_numpy(logits)
+    sc, al = torch.from_numpy(scores).cuda(), torch.from_numpy(alive).cuda()
+    out = [sc if in_place else torch.full((B, W), 9.0, device="cuda"),
+           *(torch.full((B, W), 9, dtype=torch.int32, device="cuda") for _ in range(2)),
+           al if in_place else torch.full((B, W), 9, dtype=torch.int32, device="cuda")]
+    ws = torch.full((pb.beam_select_workspace(B, W, V),), 255, dtype=torch.uint8, device="cuda")
+    pb.op_beam_select(lg[:, :V], sc, al, *out, eos=eos, pad=pad, workspace=ws)
+    for name, got, ref in zip(("tokens", "parents", "alive"), out[1:], want[1:]):
+        assert np.array_equal(got.cpu().numpy(), ref), (name, got.cpu().numpy(), ref)
+    got = out[0].double().cpu().numpy()
+    # fp32 sums of positive terms, each within (|l - m| log2 e + 2) 2^-24 of its
+    # exponential where l - m and its product are rounded; terms of l - m < -40 weigh
+    # under 2^-57 each: the log sum is off by less than 64 2^-24 + V 2^-57, and the
+    # sums of up to V / 64 terms per thread by at most another V / 64 2^-24 (V 2^-24 for
+    # the shortest blocks); then one rounding of the score
+    tol = (64 + min(V, 4096)) * 2.0 ** -24 + np.abs(want[0]) * 2.0 ** -24
+    with np.errstate(invalid="ignore"):
+        assert np.all((got == want[0]) | (np.abs(got - want[0]) <= tol))
+    return want
+
+
+def _random(rs, B, W, V, sd=3.0):
+    logits = rs.randn(B * W, V).astype(np.float32) * sd
+    logits[:, rs.randint(0, V, max(1, V // 50))] = -INF
+    scores = np.sort(-rs.uniform(2, 9, (B, W)), axis=1)[:, ::-1].astype(np.float32)
+    return logits, scores, (rs.rand(B, W) < 0.85).astype(np.int32)
+
+
+@pytest.mark.parametrize("W", [1, 2, 3, 4, 5, 8, 13, 16, 31, 32])
+@pytest.mark.parametrize("B,V", [(1, 50272), (2, 1000), (3, 257)])
+def test_widths(B, W, V):
+    _run(*_random(np.random.RandomState(W), B, W, V))
+
+
+@pytest.mark.parametrize("V", [3, 4, 5, 63, 64, 65, 255, 1023, 1024, 1025, 4095, 4097, 8191, 8193, 32000, 65537, 128256,
+                               262147])
+def test_vocabularies(V):
+    rs = np.random.RandomState(V)
+    _run(*_random(rs, 2, 4, V))
+    _run(*_random(rs, 1, 7, V), pitch=V % 3 + 1)  # rows that are not 16-byte aligned
+
+
+@pytest.mark.parametrize("B", [17, 200, 700])
+def test_many_prompts(B):
+    _run(*_random(np.random.RandomState(B), B, 3, 501))
+
+
+def test_more_places_than_candidates():
+    rs = np.random.RandomState(4)
+    for V, W in ((3, 8), (5, 32), (4, 3)):
+        logits, scores, alive = _random(rs, 2, W, V)
+        logits[0] = -INF
+        logits[W:, 1:] = -INF
+        _run(logits, scores, alive)
+        _run(logits, scores, np.zeros_like(alive))
+
+
+@pytest.mark.parametrize("W,V", [(4, 100), (8, 5000), (32, 50272)])
+def test_ties_go_to_the_lowest_index(W, V):
+    rs = np.random.RandomState(W)
+    scores, alive = np.full((2, W), -1.5, np.float32), np.ones((2, W), np.int32)
+    # all equal; few values; the same row for all beams
+    _run(np.zeros((2 * W, V)), scores, alive)
+    row = rs.randint(0, 3, V).astype(np.float32)
+    _run(np.tile(row, (2 * W, 1)), scores, alive)
+    _run(np.tile(row[::-1], (2 * W, 1)), scores, alive, eos=-1)
+    # descending and ascending rows: the best in one place of the row
+    _run(np.tile(np.linspace(5, -5, V), (2 * W, 1)), scores, alive)
+    _run(np.tile(np.linspace(-5, 5, V), (2 * W, 1)), scores, alive)
+    # all the best side by side, and one in each of W far places
+    x = np.zeros((2 * W, V)); x[:, V // 2:V // 2 + 2 * W] = 4 + rs.rand(2 * W, 2 * W)
+    _run(x, scores, alive)
+
+
+def test_first_step_and_ended_hypotheses():
+    rs = np.random.RandomState(6)
+    W, V = 4, 900
+    logits, scores, alive = _random(rs, 3, W, V)
+    alive[:] = 1
+    scores[:, 1:] = -INF
+    scores[:, 0] = 0
+    _run(logits, scores, alive)
+    scores[1] = [np.nan, INF, -INF, -3]
+    want = _run(logits, scores, alive)
+    assert set(want[2][1]) == {W + 3}
+    # ended ones compete with their own score; all ended
+    scores[:] = np.sort(-rs.uniform(1, 4, (3, W)), axis=1)[:, ::-1]
+    alive[0], alive[1, 1:] = 0, 0
+    want = _run(logits, scores, alive, in_place=True)
+    assert want[3][0].tolist() == [0] * W and want[2][0].tolist() == [0, 1, 2, 3]
+
+
+def test_end_token_and_pad():
+    rs = np.random.RandomState(7)
+    logits, scores, alive = _random(rs, 2, 4, 300)
+    logits[:, 299] = 30.0  # the end token is the best everywhere
+    alive[:] = 1
+    want = _run(logits, scores, alive, eos=299, pad=0)
+    assert not want[3][:, 0].any()
+    want = _run(logits, scores, alive, eos=-1, pad=299)
+    assert want[3].all()
+
+
+def test_logits_that_are_not_finite():
+    rs = np.random.RandomState(8)
+    logits, scores, alive = _random(rs, 2, 5, 2000)
+    alive[:] = 1
+    logits[:, ::3] = np.nan
+    logits[1] = np.nan
+    logits[2] = -INF
+    logits[3, 700] = INF
+    logits[4, [5, 6, 1999]] = INF
+    logits[5] = INF
+    logits[6, 10] = 3.4e38
+    _run(logits, scores, alive)
+
+
+def test_large_logits_and_scores():
+    rs = np.random.RandomState(9)
+    logits, scores, alive = _random(rs, 2, 4, 5000, sd=200.0)
+    _run(logits, scores, alive)
+    _run(logits * 1e30, scores, alive)
+    _run(logits + 1e4, scores * 1000, alive)

@@ -1,0 +1,201 @@
+"""Attention of one new token over a paged cache against float64: lengths from none
+to thousands, pages of every kind of size, head groups, layouts, windows, and
+what a table may hold outside the tokens attended to."""
+import numpy as np
+import pytest
+
+from gpu_common import log
+
+pytestmark = pytest.mark.gpu
+
+
+def _run(kind, H, Hkv, hd, ps, layout, lens, window=0, seed=0, scale=None, ws="own", width=None, ld_extra=0):
+    import torch
+
+    from paged_common import CODE, DT, attention64, dev, make_pool, make_tables
+    from paper_2503_17707_amd import binding as pb
+
+    log("paged attention", kind, H, Hkv, hd, ps, layout, lens, window, ws)
+    rs = np.random.RandomState(seed)
+    S = len(lens)
+    lens = np.array(lens, np.int32)
+    n_pages = int(sum(-(-max(int(n), 0) // ps) for n in lens)) + 2
+    width = width or max(1, -(-int(max(lens)) // ps))
+    tables = make_tables(rs, np.maximum(lens, 0), ps, n_pages, width)
+    pool = make_pool(seed, kind, (n_pages,), Hkv, ps, hd, layout)
+    for s in range(S):  # what follows a sequence's last token, and unused pages, is NaN
+        if lens[s] > 0 and lens[s] % ps:
+            pool[int(tables[s, (lens[s] - 1) // ps]), :, :, lens[s] % ps:] = float("nan")
+    for p in set(range(n_pages)) - set(tables.ravel().tolist()):
+        pool[p] = float("nan")
+    g = torch.Generator().manual_seed(seed + 1)
+    rows = (torch.randn((S, H * hd + ld_extra), generator=g) * 2).to(DT[kind]).cuda()
+    q = rows[:, :H * hd].unflatten(1, (H, hd))
+    scale = hd ** -0.5 if scale is None else scale
+    full = torch.full((S + 2, H * hd + ld_extra), 7.0, dtype=DT[kind], device="cuda")
+    out = full[1:S + 1, :H * hd].unflatten(1, (H, hd))
+    work = None
+    if ws == "own":
+        need = pb.paged_attention_workspace(S, H, pool, width)
+        work = torch.full((max(need, 16),), 255, dtype=torch.uint8, device="cuda")
+    elif ws == "small":
+        work = torch.full((5000,), 255, dtype=torch.uint8, device="cuda")
+    pb.op_paged_attention(CODE[kind], q, pool, dev(tables), dev(lens), out, scale=scale, window=window, workspace=work)
+    ref, tol = attention64(q, pool, tables, lens, ps, scale, window)
+    err = (out.double().cpu() - ref).abs()
+    worst = float((err / tol.clamp(min=1e-300)).max())
+    log("  worst error / tolerance %.3f" % worst)
+    assert torch.all(err <= tol), "worst error / tolerance %.3f" % worst
+    # rows before the first and behind the last sequence, and between rows, are untouched
+    assert torch.all(full[0] == 7) and torch.all(full[S + 1] == 7) and torch.all(full[:, H * hd:] == 7)
+    return out
+
+
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("layout", ["rows", "heads", "gaps"])
+def test_lengths(kind, hd, layout):
+    _run(kind, 4, 4, hd, 16, layout, [1, 0, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 129, 255, 257, 511, 513])
+
+
+@pytest.mark.parametrize("ps", [1, 2, 3, 7, 8, 20, 48, 64, 100, 128, 333, 4096])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_page_sizes(ps, hd):
+    _run("f16", 2, 2, hd, ps, "heads", [1, 99, 333, 700, 64], width=max(1, -(-700 // ps)) + 3)
+
+
+@pytest.mark.parametrize("H,Hkv", [(1, 1), (2, 1), (3, 1), (8, 2), (16, 1), (17, 1), (24, 4), (33, 1), (40, 8), (71, 1),
+                                   (130, 2)])
+@pytest.mark.parametrize("kind,hd", [("bf16", 128), ("f16", 64)])
+def test_head_groups(kind, hd, H, Hkv):
+    _run(kind, H, Hkv, hd, 16, "rows", [1, 37, 300, 1025], ld_extra=40)
+
+
+@pytest.mark.parametrize("window", [1, 2, 16, 31, 100, 1000])
+@pytest.mark.parametrize("ps", [1, 16, 20])
+def test_windows(window, ps):
+    _run("bf16", 4, 2, 64, ps, "heads", [0, 1, 2, 16, 33, 100, 101, 700], window=window)
+
+
+@pytest.mark.parametrize("ws", ["own", "small", None])
+@pytest.mark.parametrize("lens", [[5000], [4097, 1, 0, 900], [2048] * 3])
+@pytest.mark.parametrize("kind,H,Hkv,hd", [("f16", 4, 4, 64), ("bf16", 8, 1, 128)])
+def test_long_sequences_in_pieces(kind, H, Hkv, hd, lens, ws):
+    _run(kind, H, Hkv, hd, 16, "rows", lens, ws=ws)
+
+
+@pytest.mark.parametrize("S", [70, 300, 1100])
+def test_many_sequences(S):
+    rs = np.random.RandomState(S)
+    lens = rs.randint(0, 90, S)
+    lens[S // 2] = 1500
+    _run("f16", 2, 1, 64, 16, "heads", lens.tolist())
+
+
+def test_peaked_and_flat_scores():
+    # large scores: one key takes all; scale 0: the mean of the values
+    _run("f16", 4, 4, 64, 16, "heads", [700, 65], scale=3.0)
+    _run("f16", 4, 4, 64, 16, "heads", [700, 65], scale=0.0)
+    _run("bf16", 4, 4, 128, 16, "heads", [700, 65], scale=-0.3)
+
+
+def test_many_small_probabilities_beside_a_large_one():
+    """One key far above 20000 others that weigh 2^-18 each: together 7 percent."""
+    import torch
+
+    from paged_common import attention64, dev
+    from paper_2503_17707_amd import binding as pb
+
+    n, hd, ps = 20000, 64, 16
+    log("paged attention small probabilities")
+    pool = torch.zeros((n // ps, 2, 1, ps, hd), dtype=torch.float16, device="cuda")
+    pool[:, 1] = 1.0
+    pool[0, 0, 0, 0, 0] = 18 * 0.6931471805599453
+    pool[0, 1, 0, 0] = -1.0
+    q = torch.zeros((1, 1, hd), dtype=torch.float16, device="cuda")
+    q[..., 0] = 1.0
+    tables = np.arange(n // ps, dtype=np.int32)[None]
+    out = torch.empty_like(q)
+    ws = torch.empty(pb.paged_attention_workspace(1, 1, pool, n // ps) + 16, dtype=torch.uint8, device="cuda")
+    pb.op_paged_attention(1, q, pool, dev(tables), dev(np.array([n], np.int32)), out, workspace=ws)
+    ref, tol = attention64(q, pool, tables, [n], ps, 1.0, 0)
+    assert torch.all((out.double().cpu() - ref).abs() <= tol)
+
+
+@pytest.mark.parametrize("window", [0, 40])
+def test_bad_pages_give_nan_only_where_they_are_attended_to(window):
+    import torch
+
+    from paged_common import dev, make_pool, make_tables
+    from paper_2503_17707_amd import binding as pb
+
+    log("paged attention bad pages", window)
+    ps, hd, H = 16, 64, 2
+    lens = np.array([100, 100, 100, 100, 100, 90, -5], np.int32)
+    tables = make_tables(np.random.RandomState(1), np.clip(lens, 0, 96), ps, 50, 6)
+    tables[:5, 5] = [59, 58, 57, 56, 55]
+    tables = np.concatenate([tables, np.full((7, 1), -1, np.int32)], 1)
+    tables[:5, 6] = [50, 51, 52, 53, 54]
+    tables[1, 6], tables[2, 5], tables[3, 0], tables[4, 2] = -1, 60, -7, 1 << 30
+    pool = make_pool(1, "f16", (60,), H, ps, hd, "heads")
+    q = torch.randn((7, H, hd), device="cuda").half()
+    out = torch.empty_like(q)
+    pb.op_paged_attention(1, q, pool, dev(tables), dev(lens), out, window=window)
+    nan = torch.isnan(out.flatten(1)).all(1).tolist()
+    fine = torch.isfinite(out.flatten(1)).all(1).tolist()
+    in_reach = not window  # pages 0 and 2 (tokens 0-15, 32-47) lie before the last 40 tokens
+    assert nan == [False, True, True, in_reach, in_reach, False, False]
+    assert fine == [not x for x in nan]
+    assert torch.all(out[6] == 0)
+    # lens past the table's width
+    lens[5] = 7 * ps + 1
+    pb.op_paged_attention(1, q, pool, dev(tables), dev(lens), out, window=window)
+    assert torch.isnan(out[5]).all()
+
+
+def test_values_that_are_not_finite_come_through():
+    """An infinite value at a token attended to reaches the output as the formula has it."""
+    import torch
+
+    from paged_common import dev, make_pool
+    from paper_2503_17707_amd import binding as pb
+
+    log("paged attention infinities")
+    pool = make_pool(3, "bf16", (4,), 1, 16, 64, "heads")
+    pool[1, 1, 0, 3, 5] = float("inf")
+    pool[2, 1, 0, 2, 9] = float("nan")
+    pool[3, 1, 0, 11, 20] = -float("inf")  # the last token, in the middle of a tile
+    q = torch.randn((1, 1, 64), device="cuda").bfloat16()
+    out = torch.empty_like(q)
+    pb.op_paged_attention(0, q, pool, dev(np.array([[0, 1, 2, 3]], np.int32)), dev(np.array([60], np.int32)), out, scale=0.1)
+    assert out[0, 0, 5] == float("inf") and torch.isnan(out[0, 0, 9])
+    assert out[0, 0, 20] == -float("inf")
+    keep = [i for i in range(64) if i not in (5, 9, 20)]
+    assert torch.isfinite(out[0, 0, keep]).all()
+
+
+def test_pool_past_32_bit_offsets():
+    """Pages more than 2^32 bytes (and 2^31 elements) into a pool."""
+    import torch
+
+    from paged_common import attention64, dev
+    from paper_2503_17707_amd import binding as pb
+
+    log("paged attention large pool")
+    ps, hd, H = 16, 128, 2
+    n_pages = (5 << 30) // (2 * H * ps * hd * 2)
+    pool = torch.empty((n_pages, 2, H, ps, hd), dtype=torch.float16, device="cuda")
+    far = [n_pages - 1, 3, n_pages - 2, n_pages // 2 + 7]
+    g = torch.Generator(device="cuda").manual_seed(5)
+    for p in far:
+        pool[p] = torch.randn(pool[p].shape, generator=g, device="cuda").half()
+    tables = np.array([far], np.int32)
+    k = torch.randn((1, H, hd), generator=g, device="cuda").half()
+    pb.op_kv_append(1, k, k, pool, dev(tables), dev(np.array([60], np.int32)), dev(np.array([61], np.int32)))
+    assert torch.equal(pool[far[3], 0, :, 12], k[0]) and torch.equal(pool[far[3], 1, :, 12], k[0])
+    q = torch.randn((1, H, hd), generator=g, device="cuda").half()
+    out = torch.empty_like(q)
+    pb.op_paged_attention(1, q, pool, dev(tables), dev(np.array([61], np.int32)), out, scale=0.1)
+    near = torch.stack([pool[p] for p in far])
+    ref, tol = attention64(q, near, np.arange(4, dtype=np.int32)[None], [61], ps, 0.1, 0)
+    assert torch.all((out.double().cpu() - ref).abs() <= tol)
