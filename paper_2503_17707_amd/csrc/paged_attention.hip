@@ -1,4 +1,24 @@
-// Attention of one new token per sequence over a paged cache.
+// Attention of one new token per sequence over a paged cache, flash-style: one
+// pass over a sequence's keys and values with a running maximum and sum (fp32).
+//
+// What bounds it is reading the keys and values once: per token and key/value
+// head 2 HD elements against 4 HD flops per query head, and with up to 16 query
+// heads to a key/value head the matrix units take them all at the price of one.
+// So everything here serves loads in flight and an even share of them:
+//
+//  - A wave takes tiles of 32 tokens.  Keys go from memory straight into the
+//    A operand of v_mfma_f32_16x16x32 (a lane holds 8 consecutive dimensions of one
+//    token), S^T[token, query] = K Q^T with the group's queries as the 16 columns.
+//    Values are contracted over tokens, which memory does not hold consecutively:
+//    they pass through LDS (written by rows, read with the transposing
+//    ds_read_b64_tr_b16), O^T[dimension, query] += V^T P^T.  As soon as a tile's
+//    registers are free the next tile's loads are issued, so a wave has 8 KB
+//    (HD 64) or 16 KB (HD 128) in flight while it works.
+//  - Sequences are cut into pieces of equal length, the same for all sequences of
+//    a call and chosen on the device from their lengths (the lengths may change
+//    between replays of a recorded launch), so that about PIECES blocks of equal
+//    work cover a ragged batch as well as one long sequence.  A second launch
+//    joins the pieces of sequences that have several.
 #include "common.h"
 #include "paged.h"
 
@@ -7,120 +27,452 @@ namespace pb {
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
+constexpr int KT = 32;        // tokens per tile
+constexpr int NW = 4;         // waves per block
+constexpr int IDS = 1024;     // page ids held in LDS at a time
+#ifndef PB_PA_TARGET
+#define PB_PA_TARGET 1024
+#endif
+#ifndef PB_PA_CMIN
+#define PB_PA_CMIN 512
+#endif
+constexpr int PIECES = PB_PA_TARGET;  // blocks aimed at
+constexpr int SHORTEST = PB_PA_CMIN;  // tokens a piece has at least
 
-// One block per (head, sequence), its waves taking 64-key chunks in turn with a
-// running max and sum (fp32), joined at the end.
-template <typename T, int HD, int NW>
-__global__ __launch_bounds__(64 * NW) void paged_attention_kernel(PagedAttentionParams p) {
-    constexpr int G = HD / 8;     // lanes per key row
-    constexpr int KPI = 64 / G;   // keys per load instruction
-    constexpr int NI = 64 / KPI;  // load instructions per 64-key chunk
-    __shared__ float wm[NW], wl[NW], wo[NW][HD];
-    __shared__ int bad;
-    const int h = blockIdx.x, s = blockIdx.y;
-    const int kvh = h / (p.n_heads / p.pool.n_kv_heads);
+// How a call is cut: written to the workspace by the first block, read by the join.
+struct Cut {
+    int on;        // 0: one piece per sequence, no join
+    int qb;        // blocks of 16 NQ query heads per key/value head
+    int32_t* at;   // [rows + 1] first piece of each sequence
+    float* ml;     // [pieces][n_heads][2] maximum (log2 units) and sum
+    float* acc;    // [pieces][n_heads][HD] unnormalised output
+};
+
+template <typename T> __device__ constexpr uint32_t ones2();
+template <> __device__ constexpr uint32_t ones2<_Float16>() { return 0x3C003C00u; }
+template <> __device__ constexpr uint32_t ones2<__bf16>() { return 0x3F803F80u; }
+
+// Probabilities are kept times 2^SHIFT: in fp16 those below 2^-14 of the largest
+// would lose bits and those below 2^-24 vanish, and a hundred thousand of them can
+// matter; with the shift the same happens below 2^-26 and 2^-36.
+template <typename T> __device__ constexpr float shift_of();
+template <> __device__ constexpr float shift_of<_Float16>() { return 12.f; }
+template <> __device__ constexpr float shift_of<__bf16>() { return 0.f; }
+
+// 16-byte chunk of row `row` in a tile of values: the 16 lanes of a transposing
+// read address four rows at two neighbouring chunks; (row & 3) and bit 2 of the row
+// keep them, and the rows of the next lane group, in different banks.
+template <int HD> __device__ __forceinline__ int vswz(int row, int ch) {
+    if (HD == 128) return ch ^ ((row & 3) << 1) ^ (((row >> 2) & 1) << 3);
+    return ch ^ (((row & 3) ^ ((row >> 2) & 1)) << 1);
+}
+
+// Transposing LDS read: within 16 lanes, lane i receives element i % 4 of the
+// 8-byte segments addressed by lanes 4 j + i / 4, j = 0..3.
+__device__ __forceinline__ u32x2 read_tr16(const uint8_t* p) {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p)));
+}
+
+// Maximum over the four lanes that hold a query's scores (l, l ^ 16, l ^ 32, l ^ 48).
+__device__ __forceinline__ float group4_max(float v) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// LDS written and read by the same wave: its LDS instructions run in order, the
+// compiler has to keep them so.
+__device__ __forceinline__ void wave_lds_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Tokens of sequence s that its query attends to: [lo, lo + n).  A length past the
+// table's width counts as none here and is found out where ids are read.
+struct Span {
+    int lo, n;
+    bool wide;
+};
+__device__ __forceinline__ Span span_of(const PagedAttentionParams& p, int s) {
+    Span r;
     const int len = max(p.lens[s], 0);
-    const int lo = p.window > 0 ? max(0, len - p.window) : 0;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int sub = lane % G, grp = lane / G;
-    const int32_t* ids = p.tab.ids + s * p.tab.ld;
-    uint16_t* orow = p.out + s * p.ld_out + h * HD;
-    if (threadIdx.x == 0) bad = 0;
+    r.wide = len > (int64_t)p.tab.width * p.pool.page_size;
+    r.n = r.wide ? 0 : p.window > 0 ? min(len, p.window) : len;
+    r.lo = len - r.n;
+    return r;
+}
+
+// Sum over the block's 64 NW threads.
+__device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* lds) {
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) lds[wave] = v;
     __syncthreads();
-    const int c0 = (int)p.pool.div.quot(lo), c1 = len ? (int)p.pool.div.quot(len - 1) + 1 : 0;
-    for (int c = c0 + threadIdx.x; c < c1; c += 64 * NW)
-        if (c >= p.tab.width || ids[c] < 0 || ids[c] >= p.pool.n_pages) bad = 1;
+    v = 0;
+    for (int w = 0; w < NW; ++w) v += lds[w];
     __syncthreads();
-    if (bad || len == 0) {
-        for (int j = threadIdx.x; j < HD; j += 64 * NW) ((T*)orow)[j] = (T)(bad ? NAN : 0.f);
-        return;
-    }
-    float q[8];
-    {
-        const u32x4 raw = *(const u32x4*)(p.q + s * p.ld_q + h * HD + sub * 8);
-        T e[8];
-        __builtin_memcpy(e, &raw, 16);
-        for (int j = 0; j < 8; ++j) q[j] = (float)e[j] * p.scale;
-    }
-    const uint16_t* base = p.pool.base + kvh * p.pool.head_stride + sub * 8;
-    float m_run = -INFINITY, l = 0.f, o[8];
-    for (int j = 0; j < 8; ++j) o[j] = 0.f;
-    for (int k0 = lo + wave * 64; k0 < len; k0 += NW * 64) {
-        u32x4 kr[NI], vr[NI];
-#pragma unroll
-        for (int i = 0; i < NI; ++i) {
-            const int key = min(k0 + i * KPI + grp, len - 1);
-            const int col = p.pool.div.quot(key);
-            const uint16_t* a = base + ids[col] * p.pool.page_stride + (key - col * p.pool.page_size) * p.pool.token_stride;
-            kr[i] = *(const u32x4*)a;
-            vr[i] = *(const u32x4*)(a + p.pool.v_offset);
+    return v;
+}
+
+// Piece length of this call: PIECES blocks of it hold all tokens of all heads, but
+// no piece is shorter than SHORTEST.
+__device__ __forceinline__ int piece_length(int64_t tokens, int blocks_per_piece) {
+    const int64_t c = (tokens * blocks_per_piece + PIECES - 1) / PIECES;
+    const int64_t m = min(c > SHORTEST ? c : (int64_t)SHORTEST, (int64_t)1 << 30);  // no sequence is longer
+    return (int)((m + KT * NW - 1) / (KT * NW)) * (KT * NW);
+}
+
+template <typename T, int HD, int NQ>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NQ == 4 ? 1 : 2)))
+void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
+    typedef typename Mfma<T>::vec8 vec8;
+    constexpr int CS = HD / 32;          // 32-wide steps over the head
+    constexpr int CT = HD / 16;          // 16-row tiles of O^T
+    constexpr int CPR = HD / 8;          // 16-byte chunks per token
+    constexpr int RPI = 64 / CPR;        // tokens per load instruction of values
+    constexpr int NV = KT / RPI;         // ... instructions
+    constexpr int VB = KT * HD * 2;      // bytes of a wave's values in LDS
+    static_assert(16 * HD * 4 == VB, "a wave's 16 fp32 outputs fit where its values were");
+    __shared__ __attribute__((aligned(16))) uint8_t sv[NW * VB];  // values; later one 16-query output per wave
+    __shared__ int32_t ids[IDS];
+    __shared__ float wm[NW][16 * NQ], wl[NW][16 * NQ];
+    __shared__ int64_t red[NW];
+    __shared__ int found[3];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int lr = lane & 15, lg = lane >> 4;
+    const int group = p.n_heads / p.pool.n_kv_heads;
+    const int hb = p.pool.n_kv_heads * cut.qb;
+    const int kvh = blockIdx.x % hb / cut.qb, q0 = blockIdx.x % cut.qb * 16 * NQ;
+    int s = blockIdx.x / hb, piece = 0, pieces = 1, slot = 0, len_c = 0x7fffffff;
+
+    if (cut.on) {
+        // which piece of which sequence: every block works the cut out for itself
+        // from the lengths (a scan over them)
+        const int S = p.tab.rows, per = (S + 64 * NW - 1) / (64 * NW);
+        const int s0 = min(tid * per, S), s1 = min(s0 + per, S);
+        int64_t sum = 0;
+        for (int i = s0; i < s1; ++i) sum += span_of(p, i).n;
+        len_c = piece_length(block_sum(sum, red), hb);
+        int mine = 0;
+        for (int i = s0; i < s1; ++i) mine += max(1, (span_of(p, i).n + len_c - 1) / len_c);
+        int x = mine;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(x, o, 64);
+            if (lane >= o) x += y;
         }
-        float sc[NI], mx = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < NI; ++i) {
-            T e[8];
-            __builtin_memcpy(e, &kr[i], 16);
-            float a = 0.f;
-            for (int j = 0; j < 8; ++j) a += q[j] * (float)e[j];
-            for (int sh = 1; sh < G; sh <<= 1) a += __shfl_xor(a, sh, 64);
-            sc[i] = k0 + i * KPI + grp < len ? a : -INFINITY;
-            mx = fmaxf(mx, sc[i]);
+        if (lane == 63) red[wave] = x;
+        if (tid == 0) found[0] = -1;
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) x += (int)red[w];
+        int at = x - mine;
+        const int item = blockIdx.x / hb;
+        for (int i = s0; i < s1; ++i) {
+            const int k = max(1, (span_of(p, i).n + len_c - 1) / len_c);
+            if (item >= at && item < at + k) {
+                found[0] = i;
+                found[1] = item - at;
+                found[2] = k;
+            }
+            if (blockIdx.x == 0) cut.at[i] = at;
+            at += k;
         }
-        const float m_new = fmaxf(m_run, wave_max(mx));
-        const float alpha = __builtin_amdgcn_exp2f((m_run - m_new) * LOG2E);
-        l *= alpha;
-        for (int j = 0; j < 8; ++j) o[j] *= alpha;
+        if (blockIdx.x == 0 && tid == 64 * NW - 1) cut.at[S] = at;
+        __syncthreads();
+        s = found[0];
+        piece = found[1];
+        pieces = found[2];
+        slot = item;
+        if (s < 0) return;  // the grid is sized for the most pieces there can be
+    }
+
+    const Span sp = span_of(p, s);
+    const int ka = sp.lo + piece * (cut.on ? len_c : 0);
+    const int kb = cut.on ? min(sp.lo + sp.n, ka + len_c) : sp.lo + sp.n;
+    const int nq = min(group - q0, 16 * NQ);  // query heads of this block
+    const int h0 = kvh * group + q0;
+
+    vec8 qf[NQ][CS];
 #pragma unroll
-        for (int i = 0; i < NI; ++i) {
-            const float e = k0 + i * KPI + grp < len ? __builtin_amdgcn_exp2f((sc[i] - m_new) * LOG2E) : 0.f;
-            l += e;
-            T x[8];
-            // past the end the last token was read: its value may be infinite
-            if (k0 + i * KPI + grp >= len) vr[i] = u32x4{0, 0, 0, 0};
-            __builtin_memcpy(x, &vr[i], 16);
-            for (int j = 0; j < 8; ++j) o[j] += e * (float)x[j];
+    for (int t = 0; t < NQ; ++t) {
+        const uint16_t* qr = p.q + s * p.ld_q + (int64_t)(h0 + min(16 * t + lr, nq - 1)) * HD;
+#pragma unroll
+        for (int c = 0; c < CS; ++c) qf[t][c] = as_vec8<T>(*(const u32x4*)(qr + c * 32 + lg * 8));
+    }
+    f32x4 o[NQ][CT], ol[NQ];
+    float m[NQ];
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) {
+        m[t] = -INFINITY;
+        ol[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < CT; ++c) o[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const float fold = p.scale * LOG2E;
+    const uint16_t* base = p.pool.base + kvh * p.pool.head_stride;
+    uint8_t* myv = sv + wave * VB;
+    bool bad = sp.wide;
+
+    // ids of IDS pages at a time
+    for (int seg = ka; seg < kb && !bad;) {
+        const int col0 = (int)p.pool.div.quot(seg);
+        const int64_t end = (int64_t)(col0 + IDS) * p.pool.page_size;
+        const int seg_end = end < kb ? (int)end : kb;
+        const int cols = (int)p.pool.div.quot(seg_end - 1) + 1 - col0;
+        const int32_t* row = p.tab.ids + s * p.tab.ld + col0;
+        bool wrong = false;
+        __syncthreads();
+        for (int i = tid; i < cols; i += 64 * NW) {
+            const int id = row[i];
+            wrong |= id < 0 || id >= p.pool.n_pages;
+            ids[i] = id;
         }
-        m_run = m_new;
+        bad = __syncthreads_or(wrong);
+        if (bad) break;
+
+        auto token = [&](int key) {  // address of a token's keys (this head)
+            const int col = (int)p.pool.div.quot(key);
+            return base + ids[col - col0] * p.pool.page_stride + (key - col * p.pool.page_size) * p.pool.token_stride;
+        };
+        u32x4 kr[2][CS], vr[NV];
+        auto load = [&](int k0) {  // tokens past the end: the last one again
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint16_t* a = token(min(k0 + 16 * i + lr, seg_end - 1)) + lg * 8;
+#pragma unroll
+                for (int c = 0; c < CS; ++c) kr[i][c] = *(const u32x4*)(a + c * 32);
+            }
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                vr[i] = *(const u32x4*)(token(min(k0 + i * RPI + lane / CPR, seg_end - 1)) + p.pool.v_offset + lane % CPR * 8);
+        };
+        int k0 = seg + wave * KT;
+        if (k0 < seg_end) load(k0);
+        for (; k0 < seg_end; k0 += KT * NW) {
+            f32x4 sc[NQ][2];
+#pragma unroll
+            for (int t = 0; t < NQ; ++t)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    sc[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int c = 0; c < CS; ++c) sc[t][i] = Mfma<T>::mma(as_vec8<T>(kr[i][c]), qf[t][c], sc[t][i]);
+                }
+            const bool edge = k0 + KT > seg_end;
+            wave_lds_order();
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int r = i * RPI + lane / CPR;
+                // no weight reaches tokens past the end, but zero times what is read
+                // in their place need not be zero
+                if (edge && k0 + r >= seg_end) vr[i] = u32x4{0, 0, 0, 0};
+                *(u32x4*)(myv + r * HD * 2 + (vswz<HD>(r, lane % CPR) << 4)) = vr[i];
+            }
+            wave_lds_order();
+            if (k0 + KT * NW < seg_end) load(k0 + KT * NW);
+
+            vec8 pf[NQ];
+#pragma unroll
+            for (int t = 0; t < NQ; ++t) {
+                float mx = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        float x = sc[t][i][r] * fold;
+                        if (edge && k0 + 16 * i + 4 * lg + r >= seg_end) x = -INFINITY;
+                        sc[t][i][r] = x;
+                        mx = fmaxf(mx, x);
+                    }
+                const float m_new = fmaxf(m[t], group4_max(mx));
+                const float mb = m_new == -INFINITY ? 0.f : m_new;  // nothing but -inf so far: all weights 0
+                const float alpha = __builtin_amdgcn_exp2f(m[t] - mb);
+                m[t] = m_new;
+                T w[8];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        w[4 * i + r] = (T)__builtin_amdgcn_exp2f(sc[t][i][r] - (mb - shift_of<T>()));
+                u32x4 raw;
+                __builtin_memcpy(&raw, w, 16);
+                pf[t] = as_vec8<T>(raw);
+                if (__any(alpha != 1.f)) {
+#pragma unroll
+                    for (int c = 0; c < CT; ++c)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) o[t][c][r] *= alpha;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) ol[t][r] *= alpha;
+                }
+            }
+            // V^T operand, row c, k index 8 lg + 4 i + j <-> token 16 i + 4 lg + j (the
+            // order in which a lane holds its probabilities)
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+                u32x2 v[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int r = 16 * i + 4 * lg + (lr >> 2);
+                    const int col = 16 * c + 4 * (lr & 3);
+                    v[i] = read_tr16(myv + r * HD * 2 + (vswz<HD>(r, col >> 3) << 4) + (col & 7) * 2);
+                }
+                const vec8 vf = as_vec8<T>(u32x4{v[0][0], v[0][1], v[1][0], v[1][1]});
+#pragma unroll
+                for (int t = 0; t < NQ; ++t) o[t][c] = Mfma<T>::mma(vf, pf[t], o[t][c]);
+            }
+            // the sum of the probabilities as they enter the products: ones^T P^T
+            const vec8 ones = as_vec8<T>(u32x4{ones2<T>(), ones2<T>(), ones2<T>(), ones2<T>()});
+#pragma unroll
+            for (int t = 0; t < NQ; ++t) ol[t] = Mfma<T>::mma(ones, pf[t], ol[t]);
+        }
+        seg = seg_end;
     }
-    for (int sh = G; sh < 64; sh <<= 1) {
-        l += __shfl_xor(l, sh, 64);
-        for (int j = 0; j < 8; ++j) o[j] += __shfl_xor(o[j], sh, 64);
+
+    // join the waves, 16 query heads at a time
+    if (lg == 0)
+#pragma unroll
+        for (int t = 0; t < NQ; ++t) {
+            wm[wave][16 * t + lr] = m[t];
+            wl[wave][16 * t + lr] = ol[t][0];
+        }
+    const int q = tid / 16;
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) {
+        if (16 * t >= nq) break;
+        __syncthreads();
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+            *(f32x4*)(sv + wave * VB + lr * HD * 4 + (((4 * c + lg) ^ lr) << 4)) = o[t][c];
+        __syncthreads();
+        if (16 * t + q >= nq) continue;
+        float M = -INFINITY, L = 0.f, f[NW];
+#pragma unroll
+        for (int w = 0; w < NW; ++w) M = fmaxf(M, wm[w][16 * t + q]);
+        const float Mb = M == -INFINITY ? 0.f : M;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            f[w] = __builtin_amdgcn_exp2f(wm[w][16 * t + q] - Mb);
+            L += f[w] * wl[w][16 * t + q];
+        }
+        if (bad) L = NAN;
+        const int h = h0 + 16 * t + q;
+        const bool empty = sp.n == 0 && !bad;
+#pragma unroll
+        for (int j = 0; j < HD / 64; ++j) {
+            const int ch = j * 16 + tid % 16;  // 4 dimensions
+            f32x4 a = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const f32x4 x = *(const f32x4*)(sv + w * VB + q * HD * 4 + ((ch ^ q) << 4));
+#pragma unroll
+                for (int r = 0; r < 4; ++r) a[r] += f[w] * x[r];
+            }
+            if (pieces > 1) {
+                *(f32x4*)(cut.acc + ((int64_t)slot * p.n_heads + h) * HD + 4 * ch) = a;
+            } else {
+                const float inv = empty ? 0.f : 1.f / L;
+                *(u32x2*)(p.out + s * p.ld_out + (int64_t)h * HD + 4 * ch) =
+                    pack4<T>(a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv);
+            }
+        }
+        if (pieces > 1 && tid % 16 == 0) {
+            cut.ml[((int64_t)slot * p.n_heads + h) * 2] = Mb;
+            cut.ml[((int64_t)slot * p.n_heads + h) * 2 + 1] = L;
+        }
     }
-    if (lane == 0) {
-        wm[wave] = m_run;
-        wl[wave] = l;
+}
+
+// One block per (head, sequence) with several pieces: HD / 4 threads across the
+// head, the others taking pieces in turn.
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttentionParams p, Cut cut) {
+    constexpr int TX = HD / 4, TY = 256 / TX;
+    __shared__ float sa[TY][HD], sl[TY], smax[TY];
+    const int h = blockIdx.x, s = blockIdx.y;
+    const int i0 = cut.at[s], n = cut.at[s + 1] - i0;
+    if (n <= 1) return;
+    const int x = threadIdx.x % TX, y = threadIdx.x / TX;
+    const float* ml = cut.ml + ((int64_t)i0 * p.n_heads + h) * 2;
+    float M = -INFINITY;
+    for (int i = y; i < n; i += TY) M = fmaxf(M, ml[(int64_t)i * p.n_heads * 2]);
+    if (x == 0) smax[y] = M;
+    __syncthreads();
+    M = smax[0];
+    for (int i = 1; i < TY; ++i) M = fmaxf(M, smax[i]);
+    f32x4 a = f32x4{0.f, 0.f, 0.f, 0.f};
+    float L = 0.f;
+    for (int i = y; i < n; i += TY) {
+        const float f = __builtin_amdgcn_exp2f(ml[(int64_t)i * p.n_heads * 2] - M);
+        L += f * ml[(int64_t)i * p.n_heads * 2 + 1];
+        const f32x4 v = *(const f32x4*)(cut.acc + ((int64_t)(i0 + i) * p.n_heads + h) * HD + 4 * x);
+        for (int r = 0; r < 4; ++r) a[r] += f * v[r];
     }
-    if (grp == 0)
-        for (int j = 0; j < 8; ++j) wo[wave][sub * 8 + j] = o[j];
+    *(f32x4*)&sa[y][4 * x] = a;
+    if (x == 0) sl[y] = L;
     __syncthreads();
     if (threadIdx.x < HD) {
-        float M = -INFINITY, acc = 0.f, L = 0.f;
-        for (int w = 0; w < NW; ++w) M = fmaxf(M, wm[w]);
-        for (int w = 0; w < NW; ++w) {
-            if (lo + w * 64 >= len) continue;  // a wave with no key
-            const float f = __builtin_amdgcn_exp2f((wm[w] - M) * LOG2E);
-            acc += f * wo[w][threadIdx.x];
-            L += f * wl[w];
+        float o = 0.f;
+        L = 0.f;
+        for (int i = 0; i < TY; ++i) {
+            o += sa[i][threadIdx.x];
+            L += sl[i];
         }
-        ((T*)orow)[threadIdx.x] = (T)(acc / L);
+        ((T*)p.out)[s * p.ld_out + (int64_t)h * HD + threadIdx.x] = (T)(o / L);
     }
+}
+
+// Most pieces a call can have: PIECES blocks' worth and the remainder of each
+// sequence, or every sequence at the table's width cut into shortest pieces.
+int64_t most_pieces(int rows, int hb, int width, int page_size) {
+    const int64_t each = ((int64_t)width * page_size + SHORTEST - 1) / SHORTEST;
+    const int64_t a = PIECES / hb + rows, b = rows * each;
+    return a < b ? a : b;
+}
+
+size_t cut_bytes(int rows, int64_t pieces, int n_heads, int hd) {
+    return (((size_t)rows + 1) * 4 + 15) / 16 * 16 + (size_t)pieces * n_heads * (hd + 2) * 4;
+}
+
+template <typename T, int HD>
+hipError_t launch(const PagedAttentionParams& p, hipStream_t s) {
+    const int group = p.n_heads / p.pool.n_kv_heads;
+    const int nq = group <= 16 ? 1 : group <= 32 ? 2 : 4;
+    Cut cut{};
+    cut.qb = (group + 16 * nq - 1) / (16 * nq);
+    const int hb = p.pool.n_kv_heads * cut.qb;
+    int64_t items = p.tab.rows;
+    const int64_t most = most_pieces(p.tab.rows, hb, p.tab.width, p.pool.page_size);
+    if (most > p.tab.rows && p.ws && p.ws_bytes >= cut_bytes(p.tab.rows, most, p.n_heads, HD)) {
+        cut.on = 1;
+        cut.at = (int32_t*)p.ws;
+        cut.acc = (float*)((char*)p.ws + (((size_t)p.tab.rows + 1) * 4 + 15) / 16 * 16);
+        cut.ml = cut.acc + (size_t)most * p.n_heads * HD;
+        items = most;
+    }
+    if (items * hb > 0x7fffffff) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)(items * hb));
+    if (nq == 1) PB_LAUNCH((paged_attention_kernel<T, HD, 1>), grid, dim3(64 * NW), 0, s, p, cut);
+    else if (nq == 2) PB_LAUNCH((paged_attention_kernel<T, HD, 2>), grid, dim3(64 * NW), 0, s, p, cut);
+    else PB_LAUNCH((paged_attention_kernel<T, HD, 4>), grid, dim3(64 * NW), 0, s, p, cut);
+    if (cut.on) PB_LAUNCH((paged_join_kernel<T, HD>), dim3(p.n_heads, p.tab.rows), dim3(256), 0, s, p, cut);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-size_t paged_attention_workspace(int, int, int, int, int, int) { return 0; }
+size_t paged_attention_workspace(int n_seqs, int n_heads, int n_kv_heads, int hd, int width, int page_size) {
+    const int group = n_heads / n_kv_heads, nq = group <= 16 ? 1 : group <= 32 ? 2 : 4;
+    const int64_t most = most_pieces(n_seqs, n_kv_heads * ((group + 16 * nq - 1) / (16 * nq)), width, page_size);
+    return most > n_seqs ? cut_bytes(n_seqs, most, n_heads, hd) : 0;
+}
 
 hipError_t launch_paged_attention(int dtype, const PagedAttentionParams& p, hipStream_t s) {
-    const dim3 grid(p.n_heads, p.tab.rows);
     if (p.tab.rows <= 0) return hipSuccess;
-    if (p.pool.head_dim == 64) {
-        if (dtype == 1) PB_LAUNCH((paged_attention_kernel<_Float16, 64, 8>), grid, dim3(512), 0, s, p);
-        else PB_LAUNCH((paged_attention_kernel<__bf16, 64, 8>), grid, dim3(512), 0, s, p);
-    } else {
-        if (dtype == 1) PB_LAUNCH((paged_attention_kernel<_Float16, 128, 8>), grid, dim3(512), 0, s, p);
-        else PB_LAUNCH((paged_attention_kernel<__bf16, 128, 8>), grid, dim3(512), 0, s, p);
-    }
-    return hipGetLastError();
+    if (p.pool.head_dim == 64) return dtype == 1 ? launch<_Float16, 64>(p, s) : launch<__bf16, 64>(p, s);
+    return dtype == 1 ? launch<_Float16, 128>(p, s) : launch<__bf16, 128>(p, s);
 }
 
 }  // namespace pb

@@ -105,7 +105,9 @@ extern "C" int pb_op_kv_append(int32_t dtype, const void* k, int64_t ld_k, const
 }
 
 extern "C" size_t pb_op_paged_attention_workspace(int32_t n_seqs, int32_t n_heads, const pb_kv_pool* pool, int32_t width) {
-    if (!sizes_ok(pool) || n_seqs < 0 || n_seqs > 65535 || width < 1 || n_heads < 1 || n_heads % pool->n_kv_heads) return 0;
+    if (!sizes_ok(pool) || n_seqs < 0 || n_seqs > 65535 || width < 1 || n_heads < 1 || n_heads > 65535 ||
+        n_heads % pool->n_kv_heads || (int64_t)width * pool->page_size > (1 << 30))
+        return 0;
     return pb::paged_attention_workspace(n_seqs, n_heads, pool->n_kv_heads, pool->head_dim, width, pool->page_size);
 }
 
@@ -120,6 +122,7 @@ extern "C" int pb_op_paged_attention(int32_t dtype, const void* q, int64_t ld_q,
     if (n_heads < 1 || n_heads > 65535 || n_heads % pool->n_kv_heads)
         return refuse("%s: %d heads are no multiple of %d key and value heads", op, n_heads, pool->n_kv_heads);
     if (window < 0 || !(scale - scale == 0.f)) return refuse("%s: window=%d scale=%g", op, window, (double)scale);
+    if ((int64_t)width * pool->page_size > (1 << 30)) return refuse("%s: tables of more than 2^30 tokens a row", op);
     if (n_seqs == 0) return PB_OK;
     const int64_t cols = (int64_t)n_heads * pool->head_dim;
     if (!rows_ok(q, ld_q, n_seqs, cols) || !rows_ok(out, ld_out, n_seqs, cols))
