@@ -95,7 +95,7 @@ int pb_op_layernorm(int32_t dtype, const float* x, const void* g, const void* b,
  * (c = 1), of page i is at
  *   base + i page_stride + c v_offset + h head_stride + t token_stride + j,
  * strides in elements of dt, multiples of 8 and at least head_dim (that of a
- * dimension of size 1 is not used); base 16-byte aligned.  head_dim is 64 or 128,
+ * dimension of size 1 is not used), token_stride below 2^31; base 16-byte aligned.  head_dim is 64 or 128,
  * page_size 1..4096 tokens.  Both a page that holds its tokens as the model's
  * cache rows [k | v] (token_stride 2 Hkv hd, v_offset Hkv hd, head_stride hd)
  * and one that holds each head's tokens in a row fit.  A page table row holds the

@@ -27,14 +27,33 @@ namespace pb {
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr int KT = 32;        // tokens per tile
-constexpr int NW = 4;         // waves per block
-constexpr int IDS = 1024;     // page ids held in LDS at a time
+// Tokens per tile: with one operand of queries 16, half the registers and so
+// three waves per SIMD instead of two at the same bytes in flight; with more, 32.
+template <int NQ> constexpr int tile_of() { return NQ == 1 ? 16 : 32; }
+constexpr int IDS = 512;      // pages whose places are held in LDS at a time
 #ifndef PB_PA_TARGET
 #define PB_PA_TARGET 1024
 #endif
+#ifndef PB_PA_EU
+#define PB_PA_EU 2
+#endif
+#ifndef PB_PA_NWF
+#define PB_PA_NWF 8
+#endif
+#ifndef PB_PA_FEW
+#define PB_PA_FEW 512
+#endif
 #ifndef PB_PA_CMIN
-#define PB_PA_CMIN 512
+#define PB_PA_CMIN 256
+#endif
+#ifndef PB_PA_CU
+#define PB_PA_CU 256
+#endif
+#ifndef PB_PA_CMAX
+#define PB_PA_CMAX 512
+#endif
+#ifndef PB_PA_UNCUT
+#define PB_PA_UNCUT 1024
 #endif
 constexpr int PIECES = PB_PA_TARGET;  // blocks aimed at
 constexpr int SHORTEST = PB_PA_CMIN;  // tokens a piece has at least
@@ -43,10 +62,22 @@ constexpr int SHORTEST = PB_PA_CMIN;  // tokens a piece has at least
 struct Cut {
     int on;        // 0: one piece per sequence, no join
     int qb;        // blocks of 16 NQ query heads per key/value head
-    int32_t* at;   // [rows + 1] first piece of each sequence
+    int32_t* at;   // [rows][2] first piece of each sequence, how many
     float* ml;     // [pieces][n_heads][2] maximum (log2 units) and sum
     float* acc;    // [pieces][n_heads][HD] unnormalised output
 };
+
+// D[16x16] += A[16x16] B[16x16]: lane l holds A row l % 16, k = 4 (l / 16) .. + 3, and
+// B column l % 16 likewise; D as the 16x16x32 product's.
+template <typename T> __device__ __forceinline__ f32x4 mma16(u32x2 a, u32x2 b, f32x4 c);
+template <> __device__ __forceinline__ f32x4 mma16<_Float16>(u32x2 a, u32x2 b, f32x4 c) {
+    typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+    return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4, a), __builtin_bit_cast(f16x4, b), c, 0, 0, 0);
+}
+template <> __device__ __forceinline__ f32x4 mma16<__bf16>(u32x2 a, u32x2 b, f32x4 c) {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, a), __builtin_bit_cast(s16x4, b), c, 0, 0, 0);
+}
 
 template <typename T> __device__ constexpr uint32_t ones2();
 template <> __device__ constexpr uint32_t ones2<_Float16>() { return 0x3C003C00u; }
@@ -105,6 +136,7 @@ __device__ __forceinline__ Span span_of(const PagedAttentionParams& p, int s) {
 }
 
 // Sum over the block's 64 NW threads.
+template <int NW>
 __device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* lds) {
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
     const int wave = threadIdx.x >> 6;
@@ -116,27 +148,33 @@ __device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* lds) {
     return v;
 }
 
-// Piece length of this call: PIECES blocks of it hold all tokens of all heads, but
-// no piece is shorter than SHORTEST.
+// Pieces of this call are at most so long: PIECES blocks of it hold all tokens of
+// all heads, but none is shorter than SHORTEST (twice that once there are more
+// blocks than CUs).
 __device__ __forceinline__ int piece_length(int64_t tokens, int blocks_per_piece) {
     const int64_t c = (tokens * blocks_per_piece + PIECES - 1) / PIECES;
-    const int64_t m = min(c > SHORTEST ? c : (int64_t)SHORTEST, (int64_t)1 << 30);  // no sequence is longer
-    return (int)((m + KT * NW - 1) / (KT * NW)) * (KT * NW);
+    const int64_t least = min(max(tokens * blocks_per_piece / PB_PA_CU, (int64_t)SHORTEST), (int64_t)PB_PA_CMAX);
+    return (int)min(max(c, least), (int64_t)1 << 30);  // no sequence is longer
 }
 
-template <typename T, int HD, int NQ>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NQ == 4 ? 1 : 2)))
+__device__ __forceinline__ int pieces_of(int n, int len_c) { return max(1, (n + len_c - 1) / len_c); }
+
+template <typename T, int HD, int NQ, int NW>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NQ == 2 ? 2 : PB_PA_EU)))
 void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
     typedef typename Mfma<T>::vec8 vec8;
+    constexpr int KT = tile_of<NQ>();
+    constexpr int RT = KT / 16;          // 16-token tiles of S^T
     constexpr int CS = HD / 32;          // 32-wide steps over the head
     constexpr int CT = HD / 16;          // 16-row tiles of O^T
     constexpr int CPR = HD / 8;          // 16-byte chunks per token
     constexpr int RPI = 64 / CPR;        // tokens per load instruction of values
     constexpr int NV = KT / RPI;         // ... instructions
     constexpr int VB = KT * HD * 2;      // bytes of a wave's values in LDS
-    static_assert(16 * HD * 4 == VB, "a wave's 16 fp32 outputs fit where its values were");
-    __shared__ __attribute__((aligned(16))) uint8_t sv[NW * VB];  // values; later one 16-query output per wave
-    __shared__ int32_t ids[IDS];
+    constexpr int WB = 16 * HD * 4;      // bytes of 16 query heads' fp32 output
+    static_assert(WB >= VB, "LDS of a wave");
+    __shared__ __attribute__((aligned(16))) uint8_t sv[NW * WB];  // each wave's values, later its output
+    __shared__ int64_t places[IDS];      // elements from the pool's base to each page
     __shared__ float wm[NW][16 * NQ], wl[NW][16 * NQ];
     __shared__ int64_t red[NW];
     __shared__ int found[3];
@@ -146,40 +184,53 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
     const int group = p.n_heads / p.pool.n_kv_heads;
     const int hb = p.pool.n_kv_heads * cut.qb;
     const int kvh = blockIdx.x % hb / cut.qb, q0 = blockIdx.x % cut.qb * 16 * NQ;
-    int s = blockIdx.x / hb, piece = 0, pieces = 1, slot = 0, len_c = 0x7fffffff;
+    int s = blockIdx.x / hb, piece = 0, pieces = 1, slot = 0;
 
     if (cut.on) {
-        // which piece of which sequence: every block works the cut out for itself
-        // from the lengths (a scan over them)
+        // Which piece of which sequence: every block works the cut out for itself
+        // from the lengths (a scan over them).  A sequence's pieces are equally long;
+        // the long pieces come first, so that the short ones fill the end.
         const int S = p.tab.rows, per = (S + 64 * NW - 1) / (64 * NW);
         const int s0 = min(tid * per, S), s1 = min(s0 + per, S);
         int64_t sum = 0;
         for (int i = s0; i < s1; ++i) sum += span_of(p, i).n;
-        len_c = piece_length(block_sum(sum, red), hb);
-        int mine = 0;
-        for (int i = s0; i < s1; ++i) mine += max(1, (span_of(p, i).n + len_c - 1) / len_c);
-        int x = mine;
+        const int len_c = piece_length(block_sum<NW>(sum, red), hb);
+        auto is_long = [&](int n, int k) { return n >= (int64_t)k * (len_c / 2); };
+        int64_t mine = 0;  // pieces of long sequences, of short ones in the upper half
+        for (int i = s0; i < s1; ++i) {
+            const int n = span_of(p, i).n, k = pieces_of(n, len_c);
+            mine += (int64_t)k << (is_long(n, k) ? 0 : 32);
+        }
+        int64_t x = mine;
         for (int o = 1; o < 64; o <<= 1) {
-            const int y = __shfl_up(x, o, 64);
+            const int64_t y = __shfl_up(x, o, 64);
             if (lane >= o) x += y;
         }
         if (lane == 63) red[wave] = x;
         if (tid == 0) found[0] = -1;
         __syncthreads();
-        for (int w = 0; w < wave; ++w) x += (int)red[w];
-        int at = x - mine;
+        int64_t all = 0;
+        for (int w = 0; w < NW; ++w) {
+            if (w < wave) x += red[w];
+            all += red[w];
+        }
+        x -= mine;
+        int at_long = (int)(uint32_t)x, at_short = (int)(x >> 32) + (int)(uint32_t)all;
         const int item = blockIdx.x / hb;
         for (int i = s0; i < s1; ++i) {
-            const int k = max(1, (span_of(p, i).n + len_c - 1) / len_c);
+            const int n = span_of(p, i).n, k = pieces_of(n, len_c);
+            int& at = is_long(n, k) ? at_long : at_short;
             if (item >= at && item < at + k) {
                 found[0] = i;
                 found[1] = item - at;
                 found[2] = k;
             }
-            if (blockIdx.x == 0) cut.at[i] = at;
+            if (blockIdx.x == 0) {
+                cut.at[2 * i] = at;
+                cut.at[2 * i + 1] = k;
+            }
             at += k;
         }
-        if (blockIdx.x == 0 && tid == 64 * NW - 1) cut.at[S] = at;
         __syncthreads();
         s = found[0];
         piece = found[1];
@@ -189,8 +240,9 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
     }
 
     const Span sp = span_of(p, s);
-    const int ka = sp.lo + piece * (cut.on ? len_c : 0);
-    const int kb = cut.on ? min(sp.lo + sp.n, ka + len_c) : sp.lo + sp.n;
+    const int len_p = pieces == 1 ? sp.n : (sp.n + pieces * 32 - 1) / (pieces * 32) * 32;
+    const int ka = sp.lo + min(piece * len_p, sp.n);
+    const int kb = min(ka + len_p, sp.lo + sp.n);
     const int nq = min(group - q0, 16 * NQ);  // query heads of this block
     const int h0 = kvh * group + q0;
 
@@ -212,10 +264,10 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
     }
     const float fold = p.scale * LOG2E;
     const uint16_t* base = p.pool.base + kvh * p.pool.head_stride;
-    uint8_t* myv = sv + wave * VB;
+    uint8_t* myv = sv + wave * WB;
     bool bad = sp.wide;
 
-    // ids of IDS pages at a time
+    // IDS pages at a time
     for (int seg = ka; seg < kb && !bad;) {
         const int col0 = (int)p.pool.div.quot(seg);
         const int64_t end = (int64_t)(col0 + IDS) * p.pool.page_size;
@@ -227,35 +279,38 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
         for (int i = tid; i < cols; i += 64 * NW) {
             const int id = row[i];
             wrong |= id < 0 || id >= p.pool.n_pages;
-            ids[i] = id;
+            places[i] = id * p.pool.page_stride;
         }
         bad = __syncthreads_or(wrong);
         if (bad) break;
 
-        auto token = [&](int key) {  // address of a token's keys (this head)
-            const int col = (int)p.pool.div.quot(key);
-            return base + ids[col - col0] * p.pool.page_stride + (key - col * p.pool.page_size) * p.pool.token_stride;
+        // Address of a token's keys (this head).  The products are what a load costs
+        // most in instructions: three of 32 bits here.
+        auto token = [&](int key) {
+            const uint32_t col = p.pool.div.quot(key), t = key - col * p.pool.page_size;
+            return base + (places[col - col0] + (int64_t)((uint64_t)t * (uint32_t)p.pool.token_stride));
         };
-        u32x4 kr[2][CS], vr[NV];
+        u32x4 kr[RT][CS], vr[NV];
         auto load = [&](int k0) {  // tokens past the end: the last one again
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int i = 0; i < RT; ++i) {
                 const uint16_t* a = token(min(k0 + 16 * i + lr, seg_end - 1)) + lg * 8;
 #pragma unroll
                 for (int c = 0; c < CS; ++c) kr[i][c] = *(const u32x4*)(a + c * 32);
             }
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                vr[i] = *(const u32x4*)(token(min(k0 + i * RPI + lane / CPR, seg_end - 1)) + p.pool.v_offset + lane % CPR * 8);
+                vr[i] = __builtin_nontemporal_load(
+                    (const u32x4*)(token(min(k0 + i * RPI + lane / CPR, seg_end - 1)) + p.pool.v_offset + lane % CPR * 8));
         };
         int k0 = seg + wave * KT;
         if (k0 < seg_end) load(k0);
         for (; k0 < seg_end; k0 += KT * NW) {
-            f32x4 sc[NQ][2];
+            f32x4 sc[NQ][RT];
 #pragma unroll
             for (int t = 0; t < NQ; ++t)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                for (int i = 0; i < RT; ++i) {
                     sc[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int c = 0; c < CS; ++c) sc[t][i] = Mfma<T>::mma(as_vec8<T>(kr[i][c]), qf[t][c], sc[t][i]);
@@ -273,12 +328,12 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
             wave_lds_order();
             if (k0 + KT * NW < seg_end) load(k0 + KT * NW);
 
-            vec8 pf[NQ];
+            u32x2 pf[NQ][RT];  // P^T, 4 tokens of a query in each
 #pragma unroll
             for (int t = 0; t < NQ; ++t) {
                 float mx = -INFINITY;
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+                for (int i = 0; i < RT; ++i)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         float x = sc[t][i][r] * fold;
@@ -290,15 +345,13 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
                 const float mb = m_new == -INFINITY ? 0.f : m_new;  // nothing but -inf so far: all weights 0
                 const float alpha = __builtin_amdgcn_exp2f(m[t] - mb);
                 m[t] = m_new;
-                T w[8];
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+                for (int i = 0; i < RT; ++i) {
+                    float w[4];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        w[4 * i + r] = (T)__builtin_amdgcn_exp2f(sc[t][i][r] - (mb - shift_of<T>()));
-                u32x4 raw;
-                __builtin_memcpy(&raw, w, 16);
-                pf[t] = as_vec8<T>(raw);
+                    for (int r = 0; r < 4; ++r) w[r] = __builtin_amdgcn_exp2f(sc[t][i][r] - (mb - shift_of<T>()));
+                    pf[t][i] = pack4<T>(w[0], w[1], w[2], w[3]);
+                }
                 if (__any(alpha != 1.f)) {
 #pragma unroll
                     for (int c = 0; c < CT; ++c)
@@ -308,25 +361,33 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
                     for (int r = 0; r < 4; ++r) ol[t][r] *= alpha;
                 }
             }
-            // V^T operand, row c, k index 8 lg + 4 i + j <-> token 16 i + 4 lg + j (the
-            // order in which a lane holds its probabilities)
+            // V^T operand, row c: tokens 16 i + 4 lg + j, in the order in which a lane
+            // holds its probabilities
+            const uint32_t one = ones2<T>();
 #pragma unroll
-            for (int c = 0; c < CT; ++c) {
-                u32x2 v[2];
+            for (int c = 0; c <= CT; ++c) {
+                u32x2 v[RT];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int r = 16 * i + 4 * lg + (lr >> 2);
-                    const int col = 16 * c + 4 * (lr & 3);
-                    v[i] = read_tr16(myv + r * HD * 2 + (vswz<HD>(r, col >> 3) << 4) + (col & 7) * 2);
+                for (int i = 0; i < RT; ++i) {
+                    if (c < CT) {
+                        const int r = 16 * i + 4 * lg + (lr >> 2);
+                        const int col = 16 * c + 4 * (lr & 3);
+                        v[i] = read_tr16(myv + r * HD * 2 + (vswz<HD>(r, col >> 3) << 4) + (col & 7) * 2);
+                    } else {
+                        // the sum of the probabilities as they enter the products
+                        v[i] = u32x2{one, one};
+                    }
                 }
-                const vec8 vf = as_vec8<T>(u32x4{v[0][0], v[0][1], v[1][0], v[1][1]});
 #pragma unroll
-                for (int t = 0; t < NQ; ++t) o[t][c] = Mfma<T>::mma(vf, pf[t], o[t][c]);
+                for (int t = 0; t < NQ; ++t) {
+                    f32x4& d = c < CT ? o[t][c < CT ? c : 0] : ol[t];
+                    if constexpr (RT == 2)
+                        d = Mfma<T>::mma(as_vec8<T>(u32x4{v[0][0], v[0][1], v[1][0], v[1][1]}),
+                                         as_vec8<T>(u32x4{pf[t][0][0], pf[t][0][1], pf[t][1][0], pf[t][1][1]}), d);
+                    else
+                        d = mma16<T>(v[0], pf[t][0], d);
+                }
             }
-            // the sum of the probabilities as they enter the products: ones^T P^T
-            const vec8 ones = as_vec8<T>(u32x4{ones2<T>(), ones2<T>(), ones2<T>(), ones2<T>()});
-#pragma unroll
-            for (int t = 0; t < NQ; ++t) ol[t] = Mfma<T>::mma(ones, pf[t], ol[t]);
         }
         seg = seg_end;
     }
@@ -338,14 +399,14 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
             wm[wave][16 * t + lr] = m[t];
             wl[wave][16 * t + lr] = ol[t][0];
         }
-    const int q = tid / 16;
+    const int q = tid / (4 * NW);       // 4 NW threads to a query head
 #pragma unroll
     for (int t = 0; t < NQ; ++t) {
         if (16 * t >= nq) break;
         __syncthreads();
 #pragma unroll
         for (int c = 0; c < CT; ++c)
-            *(f32x4*)(sv + wave * VB + lr * HD * 4 + (((4 * c + lg) ^ lr) << 4)) = o[t][c];
+            *(f32x4*)(sv + wave * WB + lr * HD * 4 + (((4 * c + lg) ^ lr) << 4)) = o[t][c];
         __syncthreads();
         if (16 * t + q >= nq) continue;
         float M = -INFINITY, L = 0.f, f[NW];
@@ -361,12 +422,13 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
         const int h = h0 + 16 * t + q;
         const bool empty = sp.n == 0 && !bad;
 #pragma unroll
-        for (int j = 0; j < HD / 64; ++j) {
-            const int ch = j * 16 + tid % 16;  // 4 dimensions
+        for (int j = 0; j < (HD + 16 * NW - 1) / (16 * NW); ++j) {
+            const int ch = j * 4 * NW + tid % (4 * NW);  // 4 dimensions
+            if (4 * ch >= HD) break;
             f32x4 a = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
-                const f32x4 x = *(const f32x4*)(sv + w * VB + q * HD * 4 + ((ch ^ q) << 4));
+                const f32x4 x = *(const f32x4*)(sv + w * WB + q * HD * 4 + ((ch ^ q) << 4));
 #pragma unroll
                 for (int r = 0; r < 4; ++r) a[r] += f[w] * x[r];
             }
@@ -378,50 +440,73 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
                     pack4<T>(a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv);
             }
         }
-        if (pieces > 1 && tid % 16 == 0) {
+        if (pieces > 1 && tid % (4 * NW) == 0) {
             cut.ml[((int64_t)slot * p.n_heads + h) * 2] = Mb;
             cut.ml[((int64_t)slot * p.n_heads + h) * 2 + 1] = L;
         }
     }
 }
 
-// One block per (head, sequence) with several pieces: HD / 4 threads across the
-// head, the others taking pieces in turn.
-template <typename T, int HD>
+// Joins the pieces of sequences with several: 4 TX dimensions of the heads' row per
+// block, TX threads across them, the 256 / TX others taking pieces in turn.
+template <typename T, int HD, int TX>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttentionParams p, Cut cut) {
-    constexpr int TX = HD / 4, TY = 256 / TX;
-    __shared__ float sa[TY][HD], sl[TY], smax[TY];
-    const int h = blockIdx.x, s = blockIdx.y;
-    const int i0 = cut.at[s], n = cut.at[s + 1] - i0;
+    constexpr int TY = 256 / TX;
+    __shared__ f32x4 sa[TY][TX];
+    __shared__ float sm[TY][TX];
+    const int s = blockIdx.y;
+    const int i0 = cut.at[2 * s], n = cut.at[2 * s + 1];
     if (n <= 1) return;
     const int x = threadIdx.x % TX, y = threadIdx.x / TX;
-    const float* ml = cut.ml + ((int64_t)i0 * p.n_heads + h) * 2;
+    const int d = (blockIdx.x * TX + x) * 4, h = d / HD;
+    const int64_t rows = p.n_heads;
+    const float2* ml = (const float2*)cut.ml + i0 * rows + h;
+    const float* acc = cut.acc + i0 * rows * HD + d;
     float M = -INFINITY;
-    for (int i = y; i < n; i += TY) M = fmaxf(M, ml[(int64_t)i * p.n_heads * 2]);
-    if (x == 0) smax[y] = M;
+#pragma unroll 4
+    for (int i = y; i < n; i += TY) M = fmaxf(M, ml[i * rows].x);
+    sm[y][x] = M;
     __syncthreads();
-    M = smax[0];
-    for (int i = 1; i < TY; ++i) M = fmaxf(M, smax[i]);
+#pragma unroll
+    for (int j = 0; j < TY; ++j) M = fmaxf(M, sm[j][x]);
     f32x4 a = f32x4{0.f, 0.f, 0.f, 0.f};
     float L = 0.f;
+#pragma unroll 4
     for (int i = y; i < n; i += TY) {
-        const float f = __builtin_amdgcn_exp2f(ml[(int64_t)i * p.n_heads * 2] - M);
-        L += f * ml[(int64_t)i * p.n_heads * 2 + 1];
-        const f32x4 v = *(const f32x4*)(cut.acc + ((int64_t)(i0 + i) * p.n_heads + h) * HD + 4 * x);
+        const float2 w = ml[i * rows];
+        const f32x4 v = *(const f32x4*)(acc + i * rows * HD);
+        const float f = __builtin_amdgcn_exp2f(w.x - M);
+        L += f * w.y;
+#pragma unroll
         for (int r = 0; r < 4; ++r) a[r] += f * v[r];
     }
-    *(f32x4*)&sa[y][4 * x] = a;
-    if (x == 0) sl[y] = L;
+    __syncthreads();  // the maxima were read
+    sa[y][x] = a;
+    sm[y][x] = L;
     __syncthreads();
-    if (threadIdx.x < HD) {
-        float o = 0.f;
-        L = 0.f;
-        for (int i = 0; i < TY; ++i) {
-            o += sa[i][threadIdx.x];
-            L += sl[i];
+    if (y == 0) {
+#pragma unroll
+        for (int j = 1; j < TY; ++j) {
+            L += sm[j][x];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) a[r] += sa[j][x][r];
         }
-        ((T*)p.out)[s * p.ld_out + (int64_t)h * HD + threadIdx.x] = (T)(o / L);
+        const float inv = 1.f / L;
+        *(u32x2*)(p.out + s * p.ld_out + d) = pack4<T>(a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv);
     }
+}
+
+template <typename T, int HD>
+void launch_join(const PagedAttentionParams& p, const Cut& cut, hipStream_t s) {
+    // as wide as leaves 512 blocks; the widest one (64) keeps a batch's launch small
+    const int quads = p.n_heads * HD / 4;
+    const dim3 block(256);
+    if ((int64_t)(quads / 16) * p.tab.rows < 512 || quads % 16)
+        PB_LAUNCH((paged_join_kernel<T, HD, 8>), dim3(quads / 8, p.tab.rows), block, 0, s, p, cut);
+    else if ((int64_t)(quads / 64) * p.tab.rows < 512 || quads % 64)
+        PB_LAUNCH((paged_join_kernel<T, HD, 16>), dim3(quads / 16, p.tab.rows), block, 0, s, p, cut);
+    else
+        PB_LAUNCH((paged_join_kernel<T, HD, 64>), dim3(quads / 64, p.tab.rows), block, 0, s, p, cut);
 }
 
 // Most pieces a call can have: PIECES blocks' worth and the remainder of each
@@ -433,38 +518,38 @@ int64_t most_pieces(int rows, int hb, int width, int page_size) {
 }
 
 size_t cut_bytes(int rows, int64_t pieces, int n_heads, int hd) {
-    return (((size_t)rows + 1) * 4 + 15) / 16 * 16 + (size_t)pieces * n_heads * (hd + 2) * 4;
+    return ((size_t)rows * 8 + 15) / 16 * 16 + (size_t)pieces * n_heads * (hd + 2) * 4;
 }
 
 template <typename T, int HD>
 hipError_t launch(const PagedAttentionParams& p, hipStream_t s) {
     const int group = p.n_heads / p.pool.n_kv_heads;
-    const int nq = group <= 16 ? 1 : group <= 32 ? 2 : 4;
+    const int nq = group <= 16 ? 1 : 2;
     Cut cut{};
     cut.qb = (group + 16 * nq - 1) / (16 * nq);
     const int hb = p.pool.n_kv_heads * cut.qb;
     int64_t items = p.tab.rows;
     const int64_t most = most_pieces(p.tab.rows, hb, p.tab.width, p.pool.page_size);
-    if (most > p.tab.rows && p.ws && p.ws_bytes >= cut_bytes(p.tab.rows, most, p.n_heads, HD)) {
+    if ((int64_t)p.tab.width * p.pool.page_size > PB_PA_UNCUT && most > p.tab.rows && p.ws && p.ws_bytes >= cut_bytes(p.tab.rows, most, p.n_heads, HD)) {
         cut.on = 1;
         cut.at = (int32_t*)p.ws;
-        cut.acc = (float*)((char*)p.ws + (((size_t)p.tab.rows + 1) * 4 + 15) / 16 * 16);
+        cut.acc = (float*)((char*)p.ws + ((size_t)p.tab.rows * 8 + 15) / 16 * 16);
         cut.ml = cut.acc + (size_t)most * p.n_heads * HD;
         items = most;
     }
     if (items * hb > 0x7fffffff) return hipErrorInvalidValue;
     const dim3 grid((unsigned)(items * hb));
-    if (nq == 1) PB_LAUNCH((paged_attention_kernel<T, HD, 1>), grid, dim3(64 * NW), 0, s, p, cut);
-    else if (nq == 2) PB_LAUNCH((paged_attention_kernel<T, HD, 2>), grid, dim3(64 * NW), 0, s, p, cut);
-    else PB_LAUNCH((paged_attention_kernel<T, HD, 4>), grid, dim3(64 * NW), 0, s, p, cut);
-    if (cut.on) PB_LAUNCH((paged_join_kernel<T, HD>), dim3(p.n_heads, p.tab.rows), dim3(256), 0, s, p, cut);
+    if (nq == 1 && items * hb < PB_PA_FEW) PB_LAUNCH((paged_attention_kernel<T, HD, 1, PB_PA_NWF>), grid, dim3(64 * PB_PA_NWF), 0, s, p, cut);
+    else if (nq == 1) PB_LAUNCH((paged_attention_kernel<T, HD, 1, 4>), grid, dim3(256), 0, s, p, cut);
+    else PB_LAUNCH((paged_attention_kernel<T, HD, 2, 4>), grid, dim3(256), 0, s, p, cut);
+    if (cut.on) launch_join<T, HD>(p, cut, s);
     return hipGetLastError();
 }
 
 }  // namespace
 
 size_t paged_attention_workspace(int n_seqs, int n_heads, int n_kv_heads, int hd, int width, int page_size) {
-    const int group = n_heads / n_kv_heads, nq = group <= 16 ? 1 : group <= 32 ? 2 : 4;
+    const int group = n_heads / n_kv_heads, nq = group <= 16 ? 1 : 2;
     const int64_t most = most_pieces(n_seqs, n_kv_heads * ((group + 16 * nq - 1) / (16 * nq)), width, page_size);
     return most > n_seqs ? cut_bytes(n_seqs, most, n_heads, hd) : 0;
 }

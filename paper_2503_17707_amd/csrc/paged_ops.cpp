@@ -49,8 +49,10 @@ int make_pool(const char* op, int32_t dtype, const pb_kv_pool* c, pb::PagePool* 
                       c->n_pages, c->page_size, c->n_kv_heads, c->head_dim);
     if (!c->base || !aligned(c->base, 16)) return refuse("%s: pool base must be non-NULL and 16-byte aligned", op);
     if (!stride_ok(c->page_stride, c->n_pages, c->head_dim) || !stride_ok(c->v_offset, 2, c->head_dim) ||
-        !stride_ok(c->head_stride, c->n_kv_heads, c->head_dim) || !stride_ok(c->token_stride, c->page_size, c->head_dim))
-        return refuse("%s: pool strides %lld, %lld, %lld, %lld must be multiples of 8 and at least head_dim", op,
+        !stride_ok(c->head_stride, c->n_kv_heads, c->head_dim) || !stride_ok(c->token_stride, c->page_size, c->head_dim) ||
+        (c->page_size > 1 && c->token_stride > 0x7fffffff))
+        return refuse("%s: pool strides %lld, %lld, %lld, %lld must be multiples of 8 and at least head_dim "
+                      "(token_stride < 2^31)", op,
                       (long long)c->page_stride, (long long)c->v_offset, (long long)c->head_stride,
                       (long long)c->token_stride);
     out->base = (uint16_t*)c->base;
