@@ -3,10 +3,22 @@
 //
 // log softmax(l)[v] = l[v] - m - log sum exp(l - m): a row's order is its logits'
 // order, so a row offers its W largest logits and its log sum, and only those are
-// compared across rows.  The sum of exponentials runs in fp32 per thread and is
-// joined in 64 bits; a candidate's score, score + (l - m) - log sum, is formed and
-// compared in 64 bits, because candidates of different rows can lie closer than
-// fp32 tells apart at scores of tens.
+// compared across rows.  What bounds it is reading the logits once; the two
+// launches then cost their latency:
+//
+//  chunks  One block per (row, chunk of 256 R logits), the chunk in registers.  The
+//          W-th largest of the 256 threads' maxima is a value that at least W
+//          logits reach and that only W threads (and ties) hold any above: found by
+//          bisection on the bits, with ballots, it leaves a handful of candidates,
+//          each placed by counting those before it.  The chunk's maximum and sum of
+//          exponentials come from the same registers.
+//  join    One block per prompt over the sorted lists of its rows' chunks: the same
+//          idea, the W-th largest list head keeps all but W lists (and ties) out.
+//
+// Sums of exponentials run in fp32 within a chunk and are joined in 64 bits; a
+// candidate's score, score + ((l - m) - log sum), is formed and compared in 64 bits,
+// because candidates of different rows can lie closer than fp32 tells apart at
+// scores of tens.
 #include "common.h"
 #include "paged.h"
 
@@ -15,122 +27,340 @@ namespace pb {
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
+constexpr int NT = 256;       // threads of a chunk's block
+constexpr int MOST = 1024;    // candidates of a chunk: 32 threads' 32 logits
+constexpr int LISTS = 4096;   // lists of a prompt: 32 rows of 2^20 logits in 128 chunks
 
 // What a logit counts as: NaN is no candidate, +inf the largest float.
-__device__ inline float clean(float x) { return x == x ? fminf(x, 3.402823466e38f) : -INFINITY; }
+__device__ inline float clean(float x) {
+    return __builtin_amdgcn_fmed3f(x == x ? x : -INFINITY, -INFINITY, 3.402823466e38f);
+}
 
-struct RowBest {
-    float* val;    // [rows][W], descending; -inf: none left
-    int32_t* idx;  // [rows][W]
-    double* lse;   // [rows], log sum exp(l - largest)
+// Unsigned keys in the order of the floats (-0 and +0 alike).
+__device__ inline uint32_t key_of(float x) {
+    const uint32_t b = __float_as_uint(x + 0.f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+constexpr uint32_t KEY_NONE = 0x007fffffu;  // of -inf
+__device__ inline float float_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
+
+// A logit and its token as one key: of equal logits the lower token is the larger key.
+__device__ inline uint64_t entry_of(float x, int v) { return (uint64_t)key_of(x) << 32 | (uint32_t)~v; }
+
+// How many of n keys in LDS are larger.
+__device__ inline int rank_of(const uint64_t* keys, int n, uint64_t mine) {
+    int rank = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) rank += keys[j] > mine;
+    return rank;
+}
+
+struct ChunkBest {
+    float2* ms;    // [rows][chunks] maximum and sum of exponentials
+    float* val;    // [rows][chunks][W], descending; -inf: none left
+    int32_t* idx;  // [rows][chunks][W]
 };
 
-__host__ __device__ inline RowBest row_best(void* ws, int rows, int W) {
-    RowBest r;
-    r.lse = (double*)ws;
-    r.val = (float*)(r.lse + rows);
-    r.idx = (int32_t*)(r.val + (size_t)rows * W);
+__host__ __device__ inline ChunkBest chunk_best(void* ws, size_t lists, int W) {
+    ChunkBest r;
+    r.ms = (float2*)ws;
+    r.val = (float*)(r.ms + lists);
+    r.idx = (int32_t*)(r.val + lists * W);
     return r;
 }
 
 // (a, i) comes before (b, j)
-__device__ inline bool before(float a, int i, float b, int j) { return a > b || (a == b && i < j); }
+template <typename K> __device__ inline bool before(K a, int i, K b, int j) { return a > b || (a == b && i < j); }
 
-__global__ __launch_bounds__(1024) void beam_rows_kernel(BeamParams p) {
-    __shared__ float sv[16];
-    __shared__ int si[16];
-    __shared__ double ss[16];
-    const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const float* x = p.logits + row * p.ld;
-    const RowBest out = row_best(p.ws, p.B * p.W, p.W);
-    float last = INFINITY;
-    int last_i = -1;
-    float m = 0.f;
-    for (int r = 0; r < p.W; ++r) {
-        float bv = -INFINITY;
-        int bi = 0x7fffffff;
-        for (int v = tid; v < p.V; v += 1024) {
-            const float a = clean(x[v]);
-            if (before(last, last_i, a, v) && before(a, v, bv, bi)) bv = a, bi = v;
-        }
-        for (int o = 32; o > 0; o >>= 1) {
-            const float ov = __shfl_xor(bv, o, 64);
-            const int oi = __shfl_xor(bi, o, 64);
-            if (before(ov, oi, bv, bi)) bv = ov, bi = oi;
-        }
-        __syncthreads();
-        if (lane == 0) sv[wave] = bv, si[wave] = bi;
-        __syncthreads();
-        bv = sv[0], bi = si[0];
-        for (int w = 1; w < 16; ++w)
-            if (before(sv[w], si[w], bv, bi)) bv = sv[w], bi = si[w];
-        if (r == 0) m = bv;
-        if (tid == 0) {
-            out.val[(size_t)row * p.W + r] = bv;
-            out.idx[(size_t)row * p.W + r] = bi;
-        }
-        last = bv, last_i = bi;
-    }
-    float sum = 0.f;
-    for (int v = tid; v < p.V; v += 1024) {
-        const float a = clean(x[v]);
-        if (a > -INFINITY) sum += __builtin_amdgcn_exp2f((a - m) * LOG2E);
-    }
-    double d = sum;
-    for (int o = 32; o > 0; o >>= 1) d += __shfl_xor(d, o, 64);
-    if (lane == 0) ss[wave] = d;
-    __syncthreads();
-    if (tid == 0) {
-        d = 0;
-        for (int w = 0; w < 16; ++w) d += ss[w];
-        out.lse[row] = log(d);
-    }
+// Maximum over the wave, in every lane, without LDS: quads, rows of 16, then the rows.
+__device__ inline float wave_max_dpp(float v) {
+    auto step = [&](int x) { v = fmaxf(v, __int_as_float(x)); };
+    step(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0xB1, 0xf, 0xf, false));   // quad_perm 1 0 3 2
+    step(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x4E, 0xf, 0xf, false));   // quad_perm 2 3 0 1
+    step(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x141, 0xf, 0xf, false));  // row_half_mirror
+    step(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x140, 0xf, 0xf, false));  // row_mirror
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// One block per prompt: its at most W W candidates, one per thread, each placed
-// by how many come before it.
-__global__ __launch_bounds__(1024) void beam_join_kernel(BeamParams p) {
-    __shared__ double sc[1024];
-    __shared__ int id[1024];
-    const int b = blockIdx.x, tid = threadIdx.x, W = p.W, n = W * W;
-    const RowBest in = row_best(p.ws, p.B * W, W);
-    const int w = tid / W, k = tid % W;
-    double score = -INFINITY;
-    int token = p.pad;
-    bool grows = false;
-    if (tid < n) {
-        const int row = b * W + w;
-        const float own = p.scores[row];
-        if (own - own == 0.f) {  // finite
-            if (p.alive[row] == 0) {
-                if (k == 0) score = own;
-            } else {
-                const float v = in.val[(size_t)row * W + k];
-                if (v > -INFINITY) {
-                    token = in.idx[(size_t)row * W + k];
-                    score = (double)own + (((double)v - (double)in.val[(size_t)row * W]) - in.lse[row]);
-                    grows = token != p.eos;
-                }
-            }
+// A value t that at least `want` of the wave's 64 N keys reach, and at most `most`
+// of them unless more are equal (then t is the want-th largest itself; 0 if there
+// are no `want` keys).  hi: the largest key.  The want-th largest of a few hundred
+// shares the largest one's leading bits: the common part is found first, upwards
+// from 14 of them, then bits are added until few enough keys are left.
+template <int N>
+__device__ inline uint32_t reach(const uint32_t (&key)[N], uint32_t hi, int want, int most) {
+    auto count = [&](uint32_t t) {
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) n += __popcll(__ballot(key[i] >= t));
+        return n;
+    };
+    int b = 18, n = 0;
+    uint32_t t = 0;
+    for (; b < 32; b += 2) {
+        t = hi >> b << b;
+        n = count(t);
+        if (n >= want) break;
+    }
+    if (b >= 32) {
+        b = 32;
+        t = 0;
+        n = 64 * N;
+    }
+    while (n > most && b > 0) {
+        --b;
+        const uint32_t trial = t | (1u << b);
+        const int c = count(trial);
+        if (c >= want) {
+            t = trial;
+            n = c;
         }
     }
-    const int flat = w * p.V + token;  // W V < 2^31 (checked by the entry point)
-    sc[tid] = score;
-    id[tid] = flat;
+    return t;
+}
+
+template <int R>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(5))) void beam_chunks_kernel(BeamParams p, int chunks) {
+    __shared__ __attribute__((aligned(16))) float smax[NT];
+    __shared__ float ssum[NT / 64];
+    __shared__ uint64_t cand[MOST];
+    __shared__ int cn, eq[NT / 64];
+    const int row = blockIdx.x / chunks, chunk = blockIdx.x % chunks;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int W = p.W, v0 = chunk * NT * R + tid;
+    const ChunkBest out = chunk_best(p.ws, (size_t)p.B * W * chunks, W);
+    const size_t list = (size_t)row * chunks + chunk;
+    const float* l = p.logits + row * p.ld;
+    float x[R], mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < R; ++i) x[i] = l[min(v0 + i * NT, p.V - 1)];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        x[i] = clean(x[i]);
+        if ((chunk + 1) * NT * R > p.V && v0 + i * NT >= p.V) x[i] = -INFINITY;
+        mx = fmaxf(mx, x[i]);
+    }
+    smax[tid] = mx;
+    if (tid == 0) cn = 0;
     __syncthreads();
-    int rank = 0;
-    if (score > -INFINITY)
-        for (int i = 0; i < n; ++i) rank += sc[i] > score || (sc[i] == score && id[i] < flat);
-    int found = __syncthreads_count(score > -INFINITY);
-    if (score > -INFINITY && rank < W) {
-        const int o = b * W + rank;
-        p.out_scores[o] = (float)score;
+    const f32x4 four = *(const f32x4*)&smax[4 * lane];
+    const float m = wave_max_dpp(fmaxf(fmaxf(four[0], four[1]), fmaxf(four[2], four[3])));
+    const uint32_t keys[4] = {key_of(four[0]), key_of(four[1]), key_of(four[2]), key_of(four[3])};
+    // most threads whose logits all fit
+    const uint32_t t = max(reach(keys, key_of(m), W, min(W + W / 2, MOST / R)), KEY_NONE + 1);
+    float sum = 0.f;
+    if (m > -INFINITY) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) sum += __builtin_amdgcn_exp2f((x[i] - m) * LOG2E);
+        const float least = float_of(t);
+        if (mx >= least) {
+            int mine = 0;
+#pragma unroll
+            for (int i = 0; i < R; ++i) mine += x[i] >= least;
+            int at = atomicAdd(&cn, mine);
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+                if (x[i] >= least) {
+                    if (at < MOST) cand[at] = entry_of(x[i], v0 + i * NT);
+                    ++at;
+                }
+        }
+    }
+    sum = wave_sum(sum);
+    if (lane == 0) ssum[wave] = sum;
+    __syncthreads();
+    int n = cn;
+    if (n > MOST) {
+        // Too many equal ones.  Those above t are at most (W - 1) R; of those at t
+        // the W lowest are enough, taken in ascending order.
+        __syncthreads();
+        if (tid == 0) cn = 0;
+        __syncthreads();
+        for (int i = 0; i < R; ++i) {
+            float v = 0.f;
+#pragma unroll
+            for (int j = 0; j < R; ++j) v = j == i ? x[j] : v;
+            if (key_of(v) > t) {
+                cand[atomicAdd(&cn, 1)] = entry_of(v, v0 + i * NT);
+            }
+        }
+        __syncthreads();
+        n = cn;
+        int taken = 0;
+        for (int i = 0; i < R && taken < W; ++i) {
+            float v = 0.f;
+#pragma unroll
+            for (int j = 0; j < R; ++j) v = j == i ? x[j] : v;
+            const bool mine = key_of(v) == t;
+            const uint64_t b = __ballot(mine);
+            if (lane == 0) eq[wave] = __popcll(b);
+            __syncthreads();
+            int at = taken + __popcll(b & (((uint64_t)1 << lane) - 1)), all = 0;
+            for (int w = 0; w < NT / 64; ++w) {
+                if (w < wave) at += eq[w];
+                all += eq[w];
+            }
+            if (mine && at < W) cand[n + at] = entry_of(v, v0 + i * NT);
+            taken += all;
+            __syncthreads();
+        }
+        n += min(taken, W);
+    }
+    __syncthreads();
+    for (int c = tid; c < n; c += NT) {
+        const uint64_t e = cand[c];
+        const int rank = rank_of(cand, n, e);
+        if (rank < W) {
+            out.val[list * W + rank] = float_of((uint32_t)(e >> 32));
+            out.idx[list * W + rank] = ~(uint32_t)e;
+        }
+    }
+    for (int c = n + tid; c < W; c += NT) {
+        out.val[list * W + c] = -INFINITY;
+        out.idx[list * W + c] = 0;
+    }
+    if (tid == 0) out.ms[list] = make_float2(m, (ssum[0] + ssum[1]) + (ssum[2] + ssum[3]));
+}
+
+constexpr int TIED = 64; // lists whose heads may pass the bisection: the W and ties
+
+template <int N>
+__device__ inline uint32_t heads_reach(const uint32_t* key, int lists, int W) {
+    const int lane = threadIdx.x & 63;
+    uint32_t k[N], hi = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        k[i] = lane + 64 * i < lists ? key[lane + 64 * i] : 0;
+        hi = max(hi, k[i]);
+    }
+    for (int o = 32; o > 0; o >>= 1) hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, 64));
+    return reach(k, hi, W, W + W / 4);
+}
+
+template <int JT>
+__global__ __launch_bounds__(JT) void beam_join_kernel(BeamParams p, int chunks) {
+    __shared__ double lse[BEAM_MAX_WIDTH];
+    __shared__ float row_max[BEAM_MAX_WIDTH], own[BEAM_MAX_WIDTH];
+    __shared__ uint32_t key[LISTS], threshold;
+    __shared__ int live[BEAM_MAX_WIDTH], pick[TIED], picks;
+    __shared__ double sc[TIED * BEAM_MAX_WIDTH];
+    __shared__ int id[TIED * BEAM_MAX_WIDTH], cn;
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, W = p.W;
+    const int lists = W * chunks;
+    const ChunkBest in = chunk_best(p.ws, (size_t)p.B * lists, W);
+    const size_t first = (size_t)b * lists;
+    if (tid == 0) picks = cn = 0;
+    if (tid < W) {
+        own[tid] = p.scores[b * W + tid];
+        live[tid] = p.alive[b * W + tid];
+    }
+    // the heads of this thread's first list are on their way meanwhile
+    const float head_val = tid < lists ? in.val[(first + tid) * W] : 0.f;
+    const int head_idx = tid < lists ? in.idx[(first + tid) * W] : 0;
+    // the rows' log sums, g lanes to a row
+    int g = 4;
+    while (g < 64 && g < chunks) g *= 2;
+    for (int w = tid / g; w < (W + 64 / g - 1) / (64 / g) * (64 / g); w += JT / g) {  // whole waves
+        const float2* ms = in.ms + first + min(w, W - 1) * chunks;
+        float m = -INFINITY;
+        for (int c = tid % g; c < chunks; c += g) m = fmaxf(m, ms[c].x);
+        for (int o = g / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+        double sum = 0.0;
+        for (int c = tid % g; c < chunks; c += g) {
+            const float2 v = ms[c];
+            sum += v.x == -INFINITY ? 0.0 : (double)v.y * exp((double)v.x - (double)m);
+        }
+        for (int o = g / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+        if (tid % g == 0 && w < W) {
+            row_max[w] = m;
+            lse[w] = log(sum);
+        }
+    }
+    __syncthreads();
+    // score of a list's k-th entry and its place w V + v; an ended hypothesis stands
+    // at the head of its first list, as token pad
+    auto score_as = [&](int i, int k, int& place, float v, int v_idx) -> double {
+        const int w = i / chunks;
+        place = w * p.V + p.pad;
+        if (!(own[w] - own[w] == 0.f)) return -INFINITY;
+        if (live[w] == 0) return i % chunks == 0 && k == 0 ? (double)own[w] : -INFINITY;
+        if (v == -INFINITY) return -INFINITY;
+        place = w * p.V + v_idx;
+        return (double)own[w] + (((double)v - (double)row_max[w]) - lse[w]);
+    };
+    auto score_of = [&](int i, int k, int& place) {
+        return score_as(i, k, place, in.val[(first + i) * W + k], in.idx[(first + i) * W + k]);
+    };
+    for (int i = tid; i < lists; i += JT) {
+        int place;
+        key[i] = key_of((float)(i == tid ? score_as(i, 0, place, head_val, head_idx) : score_of(i, 0, place)));
+    }
+    __syncthreads();
+    // the W-th largest head, about, to fp32 (rounding keeps the order)
+    if (wave == 0) {
+        const uint32_t v = lists <= 64    ? heads_reach<1>(key, lists, W)
+                           : lists <= 256 ? heads_reach<4>(key, lists, W)
+                           : lists <= 512 ? heads_reach<8>(key, lists, W)
+                                          : heads_reach<LISTS / 64>(key, lists, W);
+        if (lane == 0) threshold = v;
+    }
+    __syncthreads();
+    const uint32_t t = max(threshold, KEY_NONE + 1);
+    for (int i = tid; i < lists; i += JT)
+        if (key[i] >= t) {
+            const int at = atomicAdd(&picks, 1);
+            if (at < TIED) pick[at] = i;
+        }
+    __syncthreads();
+    int n = picks;
+    if (n > TIED) {
+        // Many heads alike to fp32: the W that come first in 64 bits.
+        __syncthreads();
+        if (tid == 0) picks = 0;
+        __syncthreads();
+        for (int i = tid; i < lists; i += JT) {
+            if (key[i] < t) continue;
+            int pi, pj, rank = 0;
+            const double si = score_of(i, 0, pi);
+            for (int j = 0; j < lists && rank < W; ++j)
+                if (key[j] >= t) {
+                    const double sj = score_of(j, 0, pj);
+                    rank += before(sj, pj, si, pi);
+                }
+            if (rank < W) pick[atomicAdd(&picks, 1)] = i;
+        }
+        __syncthreads();
+        n = picks;
+    }
+    // their entries that reach the W-th head too
+    for (int i = tid; i < n * W; i += JT) {
+        int place;
+        const double s = score_of(pick[i / W], i % W, place);
+        if (s > -INFINITY && key_of((float)s) >= t) {
+            const int at = atomicAdd(&cn, 1);
+            sc[at] = s;
+            id[at] = place;
+        }
+    }
+    __syncthreads();
+    n = cn;
+    // (scores and alive are in LDS: the outputs may be the same arrays)
+    for (int c = tid; c < n; c += JT) {
+        int rank = 0;
+#pragma unroll 4
+        for (int i = 0; i < n; ++i) rank += before(sc[i], id[i], sc[c], id[c]);
+        if (rank >= W) continue;
+        const int o = b * W + rank, w = id[c] / p.V, token = id[c] - w * p.V;
+        p.out_scores[o] = (float)sc[c];
         p.out_tokens[o] = token;
         p.out_parents[o] = b * W + w;
-        p.out_alive[o] = grows;
+        p.out_alive[o] = live[w] != 0 && token != p.eos;
     }
-    if (tid >= found && tid < W) {
-        const int o = b * W + tid;
+    for (int i = n + tid; i < W; i += JT) {  // places that no candidate takes
+        const int o = b * W + i;
         p.out_scores[o] = -INFINITY;
         p.out_tokens[o] = p.pad;
         p.out_parents[o] = -1;
@@ -138,14 +368,36 @@ __global__ __launch_bounds__(1024) void beam_join_kernel(BeamParams p) {
     }
 }
 
+#ifndef PB_BEAM_BLOCKS
+#define PB_BEAM_BLOCKS 512
+#endif
+// Logits per thread: the most (fewest lists to join) that leave PB_BEAM_BLOCKS blocks,
+// and enough that a row has at most 64 lists (128 of 2^20 logits).
+int logits_per_thread(int64_t rows, int V) {
+    int r = 32;
+    while (r > 4 && rows * ((V + NT * r - 1) / (NT * r)) < PB_BEAM_BLOCKS) r /= 2;
+    while (r < 32 && (V + NT * r - 1) / (NT * r) > 64) r *= 2;
+    return r;
+}
+
 }  // namespace
 
-size_t beam_select_workspace(int B, int W, int) { return (size_t)B * W * (8 + (size_t)W * 8); }
+size_t beam_select_workspace(int B, int W, int V) {
+    const int r = logits_per_thread((int64_t)B * W, V);
+    return (size_t)B * W * ((V + NT * r - 1) / (NT * r)) * (8 + (size_t)W * 8);
+}
 
 hipError_t launch_beam_select(const BeamParams& p, hipStream_t s) {
     if (p.B <= 0) return hipSuccess;
-    PB_LAUNCH(beam_rows_kernel, dim3(p.B * p.W), dim3(1024), 0, s, p);
-    PB_LAUNCH(beam_join_kernel, dim3(p.B), dim3(1024), 0, s, p);
+    const int r = logits_per_thread((int64_t)p.B * p.W, p.V), chunks = (p.V + NT * r - 1) / (NT * r);
+    if ((int64_t)p.B * p.W * chunks > 0x7fffffff) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)(p.B * p.W * chunks));
+    if (r == 32) PB_LAUNCH(beam_chunks_kernel<32>, grid, dim3(NT), 0, s, p, chunks);
+    else if (r == 16) PB_LAUNCH(beam_chunks_kernel<16>, grid, dim3(NT), 0, s, p, chunks);
+    else if (r == 8) PB_LAUNCH(beam_chunks_kernel<8>, grid, dim3(NT), 0, s, p, chunks);
+    else PB_LAUNCH(beam_chunks_kernel<4>, grid, dim3(NT), 0, s, p, chunks);
+    if (p.W * chunks <= 256) PB_LAUNCH(beam_join_kernel<256>, dim3(p.B), dim3(256), 0, s, p, chunks);
+    else PB_LAUNCH(beam_join_kernel<1024>, dim3(p.B), dim3(1024), 0, s, p, chunks);
     return hipGetLastError();
 }
 

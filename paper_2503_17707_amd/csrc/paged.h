@@ -80,7 +80,7 @@ struct BeamParams {
     int32_t *out_tokens, *out_parents, *out_alive;
     void* ws;
 };
-constexpr int BEAM_MAX_WIDTH = 32;
+constexpr int BEAM_MAX_WIDTH = 32, BEAM_MAX_VOCAB = 1 << 20;
 size_t beam_select_workspace(int B, int W, int V);
 hipError_t launch_beam_select(const BeamParams& p, hipStream_t s);
 

@@ -135,19 +135,6 @@ __device__ __forceinline__ Span span_of(const PagedAttentionParams& p, int s) {
     return r;
 }
 
-// Sum over the block's 64 NW threads.
-template <int NW>
-__device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* lds) {
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    const int wave = threadIdx.x >> 6;
-    if ((threadIdx.x & 63) == 0) lds[wave] = v;
-    __syncthreads();
-    v = 0;
-    for (int w = 0; w < NW; ++w) v += lds[w];
-    __syncthreads();
-    return v;
-}
-
 // Pieces of this call are at most so long: PIECES blocks of it hold all tokens of
 // all heads, but none is shorter than SHORTEST (twice that once there are more
 // blocks than CUs).
@@ -176,8 +163,6 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
     __shared__ __attribute__((aligned(16))) uint8_t sv[NW * WB];  // each wave's values, later its output
     __shared__ int64_t places[IDS];      // elements from the pool's base to each page
     __shared__ float wm[NW][16 * NQ], wl[NW][16 * NQ];
-    __shared__ int64_t red[NW];
-    __shared__ int found[3];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int lr = lane & 15, lg = lane >> 4;
@@ -187,56 +172,51 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
     int s = blockIdx.x / hb, piece = 0, pieces = 1, slot = 0;
 
     if (cut.on) {
-        // Which piece of which sequence: every block works the cut out for itself
-        // from the lengths (a scan over them).  A sequence's pieces are equally long;
-        // the long pieces come first, so that the short ones fill the end.
-        const int S = p.tab.rows, per = (S + 64 * NW - 1) / (64 * NW);
-        const int s0 = min(tid * per, S), s1 = min(s0 + per, S);
+        // Which piece of which sequence: every wave works the cut out for itself from
+        // the lengths (a scan over them, without a barrier).  A sequence's pieces are
+        // equally long; the long pieces come first, so that the short ones fill the end.
+        const int S = p.tab.rows, per = (S + 63) / 64;
+        const int s0 = min(lane * per, S), s1 = min(s0 + per, S);
         int64_t sum = 0;
         for (int i = s0; i < s1; ++i) sum += span_of(p, i).n;
-        const int len_c = piece_length(block_sum<NW>(sum, red), hb);
+        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+        const int len_c = piece_length(sum, hb);
         auto is_long = [&](int n, int k) { return n >= (int64_t)k * (len_c / 2); };
-        int64_t mine = 0;  // pieces of long sequences, of short ones in the upper half
+        int n_long = 0, n_short = 0;  // pieces of this lane's sequences
         for (int i = s0; i < s1; ++i) {
             const int n = span_of(p, i).n, k = pieces_of(n, len_c);
-            mine += (int64_t)k << (is_long(n, k) ? 0 : 32);
+            if (is_long(n, k)) n_long += k; else n_short += k;
         }
-        int64_t x = mine;
+        int at_long = n_long, at_short = n_short;
         for (int o = 1; o < 64; o <<= 1) {
-            const int64_t y = __shfl_up(x, o, 64);
-            if (lane >= o) x += y;
+            const int y = __shfl_up(at_long, o, 64), z = __shfl_up(at_short, o, 64);
+            if (lane >= o) at_long += y, at_short += z;
         }
-        if (lane == 63) red[wave] = x;
-        if (tid == 0) found[0] = -1;
-        __syncthreads();
-        int64_t all = 0;
-        for (int w = 0; w < NW; ++w) {
-            if (w < wave) x += red[w];
-            all += red[w];
-        }
-        x -= mine;
-        int at_long = (int)(uint32_t)x, at_short = (int)(x >> 32) + (int)(uint32_t)all;
+        at_short += __shfl(at_long, 63, 64) - n_short;
+        at_long -= n_long;
         const int item = blockIdx.x / hb;
+        int mine = -1;
         for (int i = s0; i < s1; ++i) {
             const int n = span_of(p, i).n, k = pieces_of(n, len_c);
             int& at = is_long(n, k) ? at_long : at_short;
             if (item >= at && item < at + k) {
-                found[0] = i;
-                found[1] = item - at;
-                found[2] = k;
+                mine = i;
+                piece = item - at;
+                pieces = k;
             }
-            if (blockIdx.x == 0) {
+            if (blockIdx.x == 0 && wave == 0) {
                 cut.at[2 * i] = at;
                 cut.at[2 * i + 1] = k;
             }
             at += k;
         }
-        __syncthreads();
-        s = found[0];
-        piece = found[1];
-        pieces = found[2];
+        const uint64_t who = __ballot(mine >= 0);
+        if (!who) return;  // the grid is sized for the most pieces there can be
+        const int l = __ffsll((unsigned long long)who) - 1;
+        s = __builtin_amdgcn_readlane(mine, l);
+        piece = __builtin_amdgcn_readlane(piece, l);
+        pieces = __builtin_amdgcn_readlane(pieces, l);
         slot = item;
-        if (s < 0) return;  // the grid is sized for the most pieces there can be
     }
 
     const Span sp = span_of(p, s);

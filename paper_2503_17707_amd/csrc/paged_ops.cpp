@@ -140,7 +140,7 @@ extern "C" int pb_op_paged_attention(int32_t dtype, const void* q, int64_t ld_q,
 }
 
 static bool beam_ok(int32_t B, int32_t W, int32_t V) {
-    return B >= 0 && B <= 65535 && W >= 1 && W <= pb::BEAM_MAX_WIDTH && V >= 1 && (int64_t)W * V < ((int64_t)1 << 31);
+    return B >= 0 && B <= 65535 && W >= 1 && W <= pb::BEAM_MAX_WIDTH && V >= 1 && V <= pb::BEAM_MAX_VOCAB;
 }
 
 extern "C" size_t pb_op_beam_select_workspace(int32_t B, int32_t W, int32_t V) {
@@ -152,7 +152,7 @@ extern "C" int pb_op_beam_select(const float* logits, int64_t ld_logits, const f
                                  int32_t* out_tokens, int32_t* out_parents, int32_t* out_alive, void* workspace,
                                  size_t workspace_bytes, void* stream) {
     const char* op = "pb_op_beam_select";
-    if (!beam_ok(B, W, V)) return refuse("%s: B=%d W=%d V=%d (W 1..%d, W V < 2^31)", op, B, W, V, pb::BEAM_MAX_WIDTH);
+    if (!beam_ok(B, W, V)) return refuse("%s: B=%d W=%d V=%d (W 1..%d, V 1..2^20)", op, B, W, V, pb::BEAM_MAX_WIDTH);
     if (eos < -1 || eos >= V || pad < 0 || pad >= V) return refuse("%s: eos=%d pad=%d outside the vocabulary", op, eos, pad);
     if (B == 0) return PB_OK;
     if (!logits || !aligned(logits, 4) || ((int64_t)B * W > 1 && ld_logits < V))

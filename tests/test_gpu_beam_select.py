@@ -57,7 +57,7 @@ def test_widths(B, W, V):
 
 
 @pytest.mark.parametrize("V", [3, 4, 5, 63, 64, 65, 255, 1023, 1024, 1025, 4095, 4097, 8191, 8193, 32000, 65537, 128256,
-                               262147])
+                               262147, 1 << 20])
 def test_vocabularies(V):
     rs = np.random.RandomState(V)
     _run(*_random(rs, 2, 4, V))

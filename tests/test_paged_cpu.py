@@ -85,7 +85,7 @@ def test_attention_refusals(bad):
 
 
 @pytest.mark.parametrize("bad", [dict(logits=None), dict(logits=P + 2), dict(ld=99), dict(scores=None), dict(alive=None),
-                                 dict(B=-1), dict(B=65536), dict(W=0), dict(W=33), dict(V=0), dict(V=1 << 30), dict(eos=-2),
+                                 dict(B=-1), dict(B=65536), dict(W=0), dict(W=33), dict(V=0), dict(V=(1 << 20) + 1, ld=1 << 21), dict(eos=-2),
                                  dict(eos=100), dict(pad=-1), dict(pad=100), dict(o=(None, P, P, P)), dict(o=(P, P, P, None)),
                                  dict(ws=None), dict(ws=P + 8), dict(ws_bytes=16)], ids=str)
 def test_select_refusals(bad):
