@@ -47,11 +47,13 @@ __device__ inline float float_of(uint32_t key) { return __uint_as_float(key & 0x
 // A logit and its token as one key: of equal logits the lower token is the larger key.
 __device__ inline uint64_t entry_of(float x, int v) { return (uint64_t)key_of(x) << 32 | (uint32_t)~v; }
 
-// How many of n keys in LDS are larger.
+// How many of n keys in LDS are larger, counted by the G lanes that share `mine`.
+template <int G>
 __device__ inline int rank_of(const uint64_t* keys, int n, uint64_t mine) {
     int rank = 0;
-#pragma unroll 8
-    for (int j = 0; j < n; ++j) rank += keys[j] > mine;
+#pragma unroll 4
+    for (int j = threadIdx.x % G; j < n; j += G) rank += keys[j] > mine;
+    for (int o = 1; o < G; o <<= 1) rank += __shfl_xor(rank, o, 64);
     return rank;
 }
 
@@ -85,19 +87,14 @@ __device__ inline float wave_max_dpp(float v) {
     return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// A value t that at least `want` of the wave's 64 N keys reach, and at most `most`
-// of them unless more are equal (then t is the want-th largest itself; 0 if there
-// are no `want` keys).  hi: the largest key.  The want-th largest of a few hundred
+// A value t that at least `want` of `keys` keys reach, and at most `most` of them
+// unless more are equal (then t is the want-th largest itself; 0 if there are no
+// `want` keys).  hi: the largest key; count(t): how many reach t, the same in every
+// lane.  The want-th largest of a few hundred
 // shares the largest one's leading bits: the common part is found first, upwards
 // from 14 of them, then bits are added until few enough keys are left.
-template <int N>
-__device__ inline uint32_t reach(const uint32_t (&key)[N], uint32_t hi, int want, int most) {
-    auto count = [&](uint32_t t) {
-        int n = 0;
-#pragma unroll
-        for (int i = 0; i < N; ++i) n += __popcll(__ballot(key[i] >= t));
-        return n;
-    };
+template <typename Count>
+__device__ inline uint32_t reach(Count count, int keys, uint32_t hi, int want, int most) {
     int b = 18, n = 0;
     uint32_t t = 0;
     for (; b < 32; b += 2) {
@@ -108,7 +105,7 @@ __device__ inline uint32_t reach(const uint32_t (&key)[N], uint32_t hi, int want
     if (b >= 32) {
         b = 32;
         t = 0;
-        n = 64 * N;
+        n = keys;
     }
     while (n > most && b > 0) {
         --b;
@@ -146,11 +143,14 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(5))) void be
     smax[tid] = mx;
     if (tid == 0) cn = 0;
     __syncthreads();
+    // the W-th largest of the maxima of every four threads is a little lower than
+    // that of all, and found with one ballot a step
     const f32x4 four = *(const f32x4*)&smax[4 * lane];
-    const float m = wave_max_dpp(fmaxf(fmaxf(four[0], four[1]), fmaxf(four[2], four[3])));
-    const uint32_t keys[4] = {key_of(four[0]), key_of(four[1]), key_of(four[2]), key_of(four[3])};
-    // most threads whose logits all fit
-    const uint32_t t = max(reach(keys, key_of(m), W, min(W + W / 2, MOST / R)), KEY_NONE + 1);
+    const float of4 = fmaxf(fmaxf(four[0], four[1]), fmaxf(four[2], four[3]));
+    const float m = wave_max_dpp(of4);
+    const uint32_t key4 = key_of(of4);
+    uint32_t t = reach([&](uint32_t least) { return __popcll(__ballot(key4 >= least)); }, 64, key_of(m), W, W);
+    t = max(t, KEY_NONE + 1);
     float sum = 0.f;
     if (m > -INFINITY) {
 #pragma unroll
@@ -174,8 +174,16 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(5))) void be
     __syncthreads();
     int n = cn;
     if (n > MOST) {
-        // Too many equal ones.  Those above t are at most (W - 1) R; of those at t
-        // the W lowest are enough, taken in ascending order.
+        // Many equal ones, or the best side by side in few groups of four threads.  By
+        // all the threads' maxima those above t are at most MOST; of those at t the W
+        // lowest are enough, taken in ascending order.
+        auto count = [&](uint32_t least) {
+            int c = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) c += __popcll(__ballot(key_of(four[i]) >= least));
+            return c;
+        };
+        t = max(reach(count, NT, key_of(m), W, W), KEY_NONE + 1);
         __syncthreads();
         if (tid == 0) cn = 0;
         __syncthreads();
@@ -210,10 +218,11 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(5))) void be
         n += min(taken, W);
     }
     __syncthreads();
-    for (int c = tid; c < n; c += NT) {
-        const uint64_t e = cand[c];
-        const int rank = rank_of(cand, n, e);
-        if (rank < W) {
+    for (int c0 = 0; c0 < n; c0 += NT / 4) {
+        const int c = c0 + tid / 4;
+        const uint64_t e = cand[min(c, n - 1)];
+        const int rank = rank_of<4>(cand, n, e);
+        if (c < n && tid % 4 == 0 && rank < W) {
             out.val[list * W + rank] = float_of((uint32_t)(e >> 32));
             out.idx[list * W + rank] = ~(uint32_t)e;
         }
@@ -226,19 +235,6 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(5))) void be
 }
 
 constexpr int TIED = 64; // lists whose heads may pass the bisection: the W and ties
-
-template <int N>
-__device__ inline uint32_t heads_reach(const uint32_t* key, int lists, int W) {
-    const int lane = threadIdx.x & 63;
-    uint32_t k[N], hi = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        k[i] = lane + 64 * i < lists ? key[lane + 64 * i] : 0;
-        hi = max(hi, k[i]);
-    }
-    for (int o = 32; o > 0; o >>= 1) hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, 64));
-    return reach(k, hi, W, W + W / 4);
-}
 
 template <int JT>
 __global__ __launch_bounds__(JT) void beam_join_kernel(BeamParams p, int chunks) {
@@ -265,14 +261,13 @@ __global__ __launch_bounds__(JT) void beam_join_kernel(BeamParams p, int chunks)
     while (g < 64 && g < chunks) g *= 2;
     for (int w = tid / g; w < (W + 64 / g - 1) / (64 / g) * (64 / g); w += JT / g) {  // whole waves
         const float2* ms = in.ms + first + min(w, W - 1) * chunks;
-        float m = -INFINITY;
-        for (int c = tid % g; c < chunks; c += g) m = fmaxf(m, ms[c].x);
+        const float2 mine = tid % g < chunks ? ms[tid % g] : make_float2(-INFINITY, 0.f);
+        float m = mine.x;
+        for (int c = tid % g + g; c < chunks; c += g) m = fmaxf(m, ms[c].x);
         for (int o = g / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-        double sum = 0.0;
-        for (int c = tid % g; c < chunks; c += g) {
-            const float2 v = ms[c];
-            sum += v.x == -INFINITY ? 0.0 : (double)v.y * exp((double)v.x - (double)m);
-        }
+        auto term = [&](float2 v) { return v.x == -INFINITY ? 0.0 : (double)v.y * exp((double)v.x - (double)m); };
+        double sum = term(mine);
+        for (int c = tid % g + g; c < chunks; c += g) sum += term(ms[c]);
         for (int o = g / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
         if (tid % g == 0 && w < W) {
             row_max[w] = m;
@@ -301,10 +296,17 @@ __global__ __launch_bounds__(JT) void beam_join_kernel(BeamParams p, int chunks)
     __syncthreads();
     // the W-th largest head, about, to fp32 (rounding keeps the order)
     if (wave == 0) {
-        const uint32_t v = lists <= 64    ? heads_reach<1>(key, lists, W)
-                           : lists <= 256 ? heads_reach<4>(key, lists, W)
-                           : lists <= 512 ? heads_reach<8>(key, lists, W)
-                                          : heads_reach<LISTS / 64>(key, lists, W);
+        // from the lanes' maxima of every 64th head: at least W heads reach it
+        uint32_t top = 0;
+        for (int i = lane; i < lists; i += 64) top = max(top, key[i]);
+        const uint32_t hi = key_of(wave_max_dpp(top ? float_of(top) : -INFINITY));
+        uint32_t v = reach([&](uint32_t least) { return __popcll(__ballot(top >= least)); }, 64, hi, W, W);
+        auto count = [&](uint32_t least) {
+            int n = 0;
+            for (int i = 0; i < lists; i += 64) n += __popcll(__ballot(i + lane < lists && key[i + lane] >= least));
+            return n;
+        };
+        if (lists > 64 && count(v) > TIED) v = reach(count, lists, hi, W, TIED);
         if (lane == 0) threshold = v;
     }
     __syncthreads();
@@ -348,11 +350,23 @@ __global__ __launch_bounds__(JT) void beam_join_kernel(BeamParams p, int chunks)
     __syncthreads();
     n = cn;
     // (scores and alive are in LDS: the outputs may be the same arrays)
-    for (int c = tid; c < n; c += JT) {
-        int rank = 0;
+    constexpr int G = 8;  // lanes that share a candidate's count
+    for (int c0 = 0; c0 < n; c0 += JT / G) {
+        const int c = min(c0 + tid / G, n - 1);
+        const double s = sc[c];
+        int rank = 0, same = 0;
 #pragma unroll 4
-        for (int i = 0; i < n; ++i) rank += before(sc[i], id[i], sc[c], id[c]);
-        if (rank >= W) continue;
+        for (int j = tid % G; j < n; j += G) {
+            rank += sc[j] > s;
+            same += sc[j] == s;
+        }
+        for (int o = 1; o < G; o <<= 1) {
+            rank += __shfl_xor(rank, o, 64);
+            same += __shfl_xor(same, o, 64);
+        }
+        if (same > 1)  // the lowest place first
+            for (int j = 0; j < n; ++j) rank += sc[j] == s && id[j] < id[c];
+        if (rank >= W || c0 + tid / G >= n || tid % G) continue;
         const int o = b * W + rank, w = id[c] / p.V, token = id[c] - w * p.V;
         p.out_scores[o] = (float)sc[c];
         p.out_tokens[o] = token;
