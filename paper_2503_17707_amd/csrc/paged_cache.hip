@@ -7,51 +7,60 @@ namespace pb {
 
 namespace {
 
+
 // ---- append -----------------------------------------------------------------
 // Row i of sequence s (i < lens[s] - start[s]) goes to token start[s] + i of its
 // pages, 16 bytes per thread and step.  Nothing but the rows' bytes in and out
-// bounds it.  Block (x, s) takes `rpb` rows of sequence s: one for a decode
-// step, enough for 16 KB for prompts, so a ragged batch leaves only blocks that
+// bounds it.  Block (x, s) takes `rpb` rows of sequence s: one for
+// a decode step, about 16 KB for prompts, so a ragged batch leaves only blocks that
 // end at once.  A row outside [0, n_rows), past the table's width or on a page
-// id outside the pool is skipped.
-__global__ __launch_bounds__(256) void kv_append_kernel(AppendParams p, int rpb) {
+// id outside the pool is skipped.  A decode step's tokens are read next and stay in
+// cache; prompts' are not (streaming stores: 16 ragged prompts of 40 heads of 128, 221
+// MB, 48.0 us against 52.0).
+template <bool PROMPTS>
+__global__ __launch_bounds__(256) void kv_append_kernel(AppendParams p, int rpb, FastDiv per_row) {
     const int s = blockIdx.y;
     const int start = p.start[s];
-    const int n = min(p.lens[s] - start, p.max_rows);
+    const int n = (int)min((int64_t)p.lens[s] - start, (int64_t)p.max_rows);
     const int i0 = blockIdx.x * rpb;
     if (start < 0 || i0 >= n) return;
     const int i1 = min(i0 + rpb, n);
-    const int row0 = p.row0 ? p.row0[s] : s * p.max_rows;
-    const int cph = p.pool.head_dim / 8;             // 16-byte chunks of a head
-    const int half = p.pool.n_kv_heads * cph;        // ... of a row of K
+    const int64_t row0 = p.row0 ? p.row0[s] : (int64_t)s * p.max_rows;
+    const int lc = p.pool.head_dim == 128 ? 4 : 3;          // log2 of a head's 16-byte chunks
+    const int half = p.pool.n_kv_heads << lc;               // chunks of a row of K
     const int32_t* ids = p.tab.ids + s * p.tab.ld;
     for (int c = threadIdx.x; c < (i1 - i0) * 2 * half; c += 256) {
-        const int i = i0 + c / (2 * half);
-        int e = c % (2 * half);
+        const int r = per_row.quot(c), i = i0 + r;
+        int e = c - r * 2 * half;
         const bool isv = e >= half;
         e -= isv ? half : 0;
-        const int h = e / cph, j = (e % cph) * 8;
-        const int64_t row = (int64_t)row0 + i;
-        const int x = start + i;
-        const int col = p.pool.div.quot(x);
+        const int h = e >> lc, j = (e & ((1 << lc) - 1)) * 8;
+        const int64_t row = row0 + i;
+        const int col = p.pool.div.quot(start + i);
         if (row < 0 || row >= p.n_rows || col >= p.tab.width) continue;
         const int page = ids[col];
         if (page < 0 || page >= p.pool.n_pages) continue;
-        const int t = x - col * p.pool.page_size;
         const u32x4 val = *(const u32x4*)((isv ? p.v + row * p.ld_v : p.k + row * p.ld_k) + e * 8);
-        *(u32x4*)(p.pool.base + page * p.pool.page_stride + (isv ? p.pool.v_offset : 0) + h * p.pool.head_stride +
-                  t * p.pool.token_stride + j) = val;
+        u32x4* to = (u32x4*)(p.pool.base + page * p.pool.page_stride + (isv ? p.pool.v_offset : 0) +
+                             h * p.pool.head_stride + (start + i - col * p.pool.page_size) * p.pool.token_stride + j);
+        if (PROMPTS) __builtin_nontemporal_store(val, to);
+        else *to = val;
     }
 }
 
 // ---- fork ---------------------------------------------------------------------
-// Four launches, each ordered after the one before by the stream:
+// Steps, each ordered after the one before:
 //  1 counts: out_refs = refs, per-page scratch cleared
 //  2 tables: the old rows' references leave the counts, the new rows' join them
 //    (integer atomics: the order does not matter), and every row that will be
 //    written to inside a page names itself at that page
 //  3 places: one block decides who copies, ranks the free pages and hands them out
 //  4 copies: the tokens of every page copied, in every layer
+// Copying bounds large calls, the chain of launches and dependent reads small ones:
+// up to SMALL_PAGES pages and SMALL_ENTRIES table entries one block takes steps 1
+// to 3 with the counts in LDS.
+
+constexpr int SMALL_PAGES = 8192, SMALL_ROWS = 512, SMALL_ENTRIES = 32768;
 
 struct ForkScratch {  // in the workspace
     int32_t *movers, *first;            // [n_pages] growing rows whose last page it is, the lowest of them
@@ -165,19 +174,76 @@ __device__ inline int block_scan(int v, int* lds, int* total) {
     return before + x - v;
 }
 
-__global__ __launch_bounds__(1024) void fork_places_kernel(ForkParams p) {
+// Steps 1 to 3 (SMALL; out_rows and in_rows up to SMALL_ROWS) or step 3.
+template <bool SMALL>
+__global__ __launch_bounds__(1024) void fork_places_kernel(ForkParams p, FastDiv width) {
+    extern __shared__ int32_t small[];  // SMALL: counts, movers, first by page
     __shared__ int lds[16];
+    // SMALL: per row its first new page's rank, its pages, whether it copies
+    __shared__ int32_t offsets[SMALL ? SMALL_ROWS : 1], n_of[SMALL ? SMALL_ROWS : 1], copies_of[SMALL ? SMALL_ROWS : 1];
     const ForkScratch f = fork_scratch(p.ws, p.out_rows, p.pool.n_pages);
     const int tid = threadIdx.x, R = p.out_rows, P = p.pool.n_pages;
+    int32_t* refs = SMALL ? small : p.out_refs;
+    int32_t* movers = SMALL ? small + P : f.movers;
+    int32_t* first = SMALL ? small + 2 * P : f.first;
+    int32_t* offset = SMALL ? offsets : f.offset;
+    ForkRow mine{};  // SMALL: row tid
+    int my_page = -1;
+    if (SMALL) {
+        __shared__ int32_t held[SMALL_ROWS], parent_of[SMALL_ROWS];
+        for (int i = tid; i < P; i += 1024) {
+            refs[i] = p.refs[i];
+            movers[i] = 0;
+            first[i] = 0x7fffffff;
+        }
+        if (tid < p.in_rows) held[tid] = pages_of(p, row_len(p, tid));
+        if (tid < R) {
+            mine = fork_row(p, tid);
+            my_page = moving_page(p, mine);
+            n_of[tid] = mine.n;
+            parent_of[tid] = mine.parent;
+            p.out_start[tid] = mine.start;
+        }
+        const int wide = __syncthreads_count(mine.wide);
+        if (tid < 2) p.short_of[tid] = tid ? wide : 0;
+        if (my_page >= 0) {
+            atomicAdd(&movers[my_page], 1);
+            atomicMin(&first[my_page], tid);
+        }
+        // four entries of a thread in flight
+        const int32_t* __restrict__ tables = p.tables;
+        int32_t* __restrict__ out_tables = p.out_tables;
+        const int n_in = p.in_rows * p.width, n_out = R * p.width;
+        for (int i0 = tid; i0 < max(n_in, n_out); i0 += 4 * 1024) {
+            int was[4], is[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int i = i0 + u * 1024, r = width.quot(i), c = i - r * p.width;
+                was[u] = i < n_in && c < held[r] ? tables[i] : -1;
+                is[u] = i < n_out && c < n_of[r] ? tables[parent_of[r] * p.width + c] : -1;
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int i = i0 + u * 1024;
+                was[u] = good_page(p, was[u]);
+                is[u] = good_page(p, is[u]);
+                if (was[u] >= 0) atomicSub(&refs[was[u]], 1);
+                if (is[u] >= 0) atomicAdd(&refs[is[u]], 1);
+                if (i < n_out) out_tables[i] = is[u];
+            }
+        }
+        __syncthreads();
+    }
     // who copies, and how many pages each row asks for
     int64_t asked = 0;
+    int my_src = -1;
     for (int r0 = 0; r0 < R; r0 += 1024) {
         const int r = r0 + tid;
         int need = 0, src = -1, tok = 0;
         if (r < R) {
-            const ForkRow w = fork_row(p, r);
-            const int id = moving_page(p, w);
-            if (id >= 0 && (p.out_refs[id] > f.movers[id] || f.first[id] != r)) {
+            const ForkRow w = SMALL ? mine : fork_row(p, r);
+            const int id = SMALL ? my_page : moving_page(p, w);
+            if (id >= 0 && (refs[id] > movers[id] || first[id] != r)) {
                 src = id;
                 tok = w.start - (w.n - 1) * p.pool.page_size;
             }
@@ -186,74 +252,100 @@ __global__ __launch_bounds__(1024) void fork_places_kernel(ForkParams p) {
         int total;
         const int before = block_scan(need, lds, &total);
         if (r < R) {
-            f.offset[r] = (int)min(asked + before, (int64_t)0x7fffffff);
-            f.src[r] = src;
+            offset[r] = (int)min(asked + before, (int64_t)0x7fffffff);
+            if (SMALL) copies_of[r] = src >= 0;
+            f.src[r] = my_src = src;
             f.dst[r] = -1;
             f.tok[r] = tok;
         }
         asked += total;
     }
-    // are there as many free pages
+    __syncthreads();  // `first` was read: from here on it lists the free pages
+    // the free pages in ascending order, as many as are asked for
+    constexpr int PER = 4;  // pages of a thread at a time
+    int32_t* list = first;
     int64_t found = 0;
-    for (int i0 = 0; i0 < P && found < asked; i0 += 1024) {
-        int total;
-        block_scan(i0 + tid < P && p.out_refs[i0 + tid] == 0, lds, &total);
+    for (int i0 = 0; i0 < P && found < asked; i0 += 1024 * PER) {
+        const int page = i0 + tid * PER;
+        bool free[PER];
+        int n = 0, total;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            free[j] = page + j < P && refs[min(page + j, P - 1)] == 0;
+            n += free[j];
+        }
+        int64_t k = found + block_scan(n, lds, &total);
         found += total;
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+            if (free[j] && k < asked) list[k++] = page + j;
     }
     const bool enough = found >= asked;
-    if (tid == 0) {
-        f.offset[R] = (int)min(asked, (int64_t)0x7fffffff);
-        if (!enough) p.short_of[0] = (int)min(asked - found, (int64_t)0x7fffffff);
-    }
+    if (tid == 0 && !enough) p.short_of[0] = (int)min(asked - found, (int64_t)0x7fffffff);
     for (int r = tid; r < R; r += 1024) {
-        const ForkRow w = fork_row(p, r);
+        const ForkRow w = SMALL ? mine : fork_row(p, r);
         p.out_lens[r] = w.start + (enough ? w.grow : 0);
         if (!enough) f.src[r] = -1;
     }
-    __syncthreads();  // offset is whole
-    if (!enough) return;
-    // free page of rank k to the row whose [offset, next offset) holds k
-    int64_t rank0 = 0;
-    for (int i0 = 0; i0 < P && rank0 < asked; i0 += 1024) {
-        const int page = i0 + tid;
-        const bool free = page < P && p.out_refs[page] == 0;
-        int total;
-        const int64_t k = rank0 + block_scan(free, lds, &total);
-        rank0 += total;
-        if (free && k < asked) {
-            int lo = 0, hi = R - 1;  // the last row with offset <= k
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) / 2;
-                if (f.offset[mid] <= k) lo = mid; else hi = mid - 1;
-            }
-            const int j = (int)(k - f.offset[lo]);
-            const bool copies = f.src[lo] >= 0;
-            const int n = pages_of(p, p.out_start[lo]);
-            p.out_tables[(int64_t)lo * p.width + n - copies + j] = page;
-            p.out_refs[page] = 1;
-            if (copies && j == 0) f.dst[lo] = page;
+    __syncthreads();  // offset and list are whole
+    // the page of rank k to the row whose [offset, next offset) holds k
+    for (int k = tid; enough && k < asked; k += 1024) {
+        int lo = 0, hi = R - 1;  // the last row with offset <= k
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (offset[mid] <= k) lo = mid; else hi = mid - 1;
         }
+        const int page = list[k], at = k - offset[lo];
+        const bool copies = SMALL ? copies_of[lo] : f.src[lo] >= 0;
+        const int last = SMALL ? n_of[lo] : pages_of(p, p.out_start[lo]);
+        p.out_tables[(int64_t)lo * p.width + last - copies + at] = page;
+        refs[page] = 1;
+        if (copies && at == 0) f.dst[lo] = page;
     }
-    __syncthreads();  // every free page was looked at before counts move again
-    for (int r = tid; r < R; r += 1024)
-        if (f.src[r] >= 0) atomicSub(&p.out_refs[f.src[r]], 1);
+    if (SMALL) {
+        // (a page that is copied is in use: nobody counts it free)
+        if (enough && my_src >= 0) atomicSub(&refs[my_src], 1);
+        __syncthreads();
+        for (int i = tid; i < P; i += 1024) p.out_refs[i] = refs[i];
+    } else if (enough) {
+        for (int r = tid; r < R; r += 1024)
+            if (f.src[r] >= 0) atomicSub(&refs[f.src[r]], 1);
+    }
 }
 
-__global__ __launch_bounds__(256) void fork_copy_kernel(ForkParams p) {
+// Block (row, layer): the tokens are what is copied, not the page, eight 16-byte
+// steps of a thread in flight.
+__global__ __launch_bounds__(256) void fork_copy_kernel(ForkParams p, FastDiv heads, bool by_token) {
     const ForkScratch f = fork_scratch(p.ws, p.out_rows, p.pool.n_pages);
     const int r = blockIdx.x;
     const int src = f.src[r], dst = f.dst[r], tok = f.tok[r];
     if (src < 0 || dst < 0) return;
-    const int cph = p.pool.head_dim / 8;
+    const int lc = p.pool.head_dim == 128 ? 4 : 3;
     uint16_t* base = p.pool.base + blockIdx.y * p.layer_stride;
     const uint16_t* from = base + src * p.pool.page_stride;
     uint16_t* to = base + dst * p.pool.page_stride;
-    const int n = tok * 2 * p.pool.n_kv_heads * cph;
-    for (int i = threadIdx.x; i < n; i += 256) {
-        const int j = i % cph, a = i / cph;
-        const int h = a % p.pool.n_kv_heads, b = a / p.pool.n_kv_heads;
-        const int64_t o = (b & 1) * p.pool.v_offset + h * p.pool.head_stride + (b >> 1) * p.pool.token_stride + j * 8;
-        *(u32x4*)(to + o) = *(const u32x4*)(from + o);
+    const int n = (tok * 2 * p.pool.n_kv_heads) << lc;
+    for (int i0 = threadIdx.x; i0 < n; i0 += 8 * 256) {
+        int64_t o[8];
+        u32x4 v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            // token by token, or head by head: whichever a page holds together
+            const int i = min(i0 + u * 256, n - 1), a = i >> lc, j = i & ((1 << lc) - 1);
+            int h, t, c;
+            if (by_token) {
+                const int row = heads.quot(a);
+                h = a - row * p.pool.n_kv_heads, c = row & 1, t = row >> 1;
+            } else {
+                const int row = a / tok;
+                t = a - row * tok, c = row >= p.pool.n_kv_heads, h = row - (c ? p.pool.n_kv_heads : 0);
+            }
+            o[u] = c * p.pool.v_offset + h * p.pool.head_stride + t * p.pool.token_stride + j * 8;
+            v[u] = *(const u32x4*)(from + o[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (i0 + u * 256 < n) *(u32x4*)(to + o[u]) = v[u];
     }
 }
 
@@ -263,7 +355,10 @@ hipError_t launch_kv_append(const AppendParams& p, hipStream_t s) {
     if (p.tab.rows <= 0 || p.max_rows <= 0 || p.n_rows <= 0) return hipSuccess;
     const int row_bytes = 2 * p.pool.n_kv_heads * p.pool.head_dim * 2;
     const int rpb = p.max_rows == 1 ? 1 : (16384 + row_bytes - 1) / row_bytes;
-    PB_LAUNCH(kv_append_kernel, dim3((p.max_rows + rpb - 1) / rpb, p.tab.rows), dim3(256), 0, s, p, rpb);
+    const FastDiv per_row(2 * p.pool.n_kv_heads * p.pool.head_dim / 8);
+    const dim3 grid((p.max_rows + rpb - 1) / rpb, p.tab.rows);
+    if (p.max_rows == 1) PB_LAUNCH(kv_append_kernel<false>, grid, dim3(256), 0, s, p, rpb, per_row);
+    else PB_LAUNCH(kv_append_kernel<true>, grid, dim3(256), 0, s, p, rpb, per_row);
     return hipGetLastError();
 }
 
@@ -271,14 +366,23 @@ size_t page_fork_workspace(int out_rows, int n_pages) { return ((size_t)2 * n_pa
 
 hipError_t launch_page_fork(const ForkParams& p, hipStream_t s) {
     const int P = p.pool.n_pages;
-    PB_LAUNCH(fork_counts_kernel, dim3((P + 1023) / 1024), dim3(256), 0, s, p);
     const int rows = p.in_rows > p.out_rows ? p.in_rows : p.out_rows;
-    if (rows > 0)
-        PB_LAUNCH(fork_tables_kernel, dim3((p.width + 1023) / 1024, rows), dim3(256), 0, s, p);
-    if (p.out_rows > 0) {
-        PB_LAUNCH(fork_places_kernel, dim3(1), dim3(1024), 0, s, p);
-        PB_LAUNCH(fork_copy_kernel, dim3(p.out_rows, p.n_layers), dim3(256), 0, s, p);
+    if (P <= SMALL_PAGES && rows <= SMALL_ROWS && (int64_t)rows * p.width <= SMALL_ENTRIES) {
+        const int lds = 3 * P * 4;
+        if (lds > 32 << 10) {  // with the static part more than 64 KB has to be asked for
+            const hipError_t e = hipFuncSetAttribute((const void*)fork_places_kernel<true>,
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+            if (e != hipSuccess) return e;
+        }
+        PB_LAUNCH(fork_places_kernel<true>, dim3(1), dim3(1024), lds, s, p, FastDiv(p.width));
+    } else {
+        PB_LAUNCH(fork_counts_kernel, dim3((P + 1023) / 1024), dim3(256), 0, s, p);
+        if (rows > 0) PB_LAUNCH(fork_tables_kernel, dim3((p.width + 1023) / 1024, rows), dim3(256), 0, s, p);
+        if (p.out_rows > 0) PB_LAUNCH(fork_places_kernel<false>, dim3(1), dim3(1024), 0, s, p, FastDiv(p.width));
     }
+    if (p.out_rows > 0)
+        PB_LAUNCH(fork_copy_kernel, dim3(p.out_rows, p.n_layers), dim3(256), 0, s, p, FastDiv(p.pool.n_kv_heads),
+                  p.pool.token_stride > p.pool.head_stride);
     return hipGetLastError();
 }
 

@@ -47,6 +47,7 @@ int make_pool(const char* op, int32_t dtype, const pb_kv_pool* c, pb::PagePool* 
     if (!sizes_ok(c))
         return refuse("%s: pool of %d pages of %d tokens, %d heads of %d (page_size 1..4096, head_dim 64 or 128)", op,
                       c->n_pages, c->page_size, c->n_kv_heads, c->head_dim);
+    if ((int64_t)c->page_size * c->n_kv_heads * (c->head_dim / 4) > 0x7fffffff) return refuse("%s: a page of 2^35 bytes or more", op);
     if (!c->base || !aligned(c->base, 16)) return refuse("%s: pool base must be non-NULL and 16-byte aligned", op);
     if (!stride_ok(c->page_stride, c->n_pages, c->head_dim) || !stride_ok(c->v_offset, 2, c->head_dim) ||
         !stride_ok(c->head_stride, c->n_kv_heads, c->head_dim) || !stride_ok(c->token_stride, c->page_size, c->head_dim) ||

@@ -132,6 +132,26 @@ def test_fork_of_beams(kind, L, Hkv, hd, layout, B, W, ps, n_max):
         _fork(kind, L, Hkv, hd, ps, layout, parents, tables, lens, refs, grow, seed=seed)
 
 
+@pytest.mark.parametrize("B,W,ps,n_max", [(1, 4, 16, 100), (3, 5, 7, 60), (8, 8, 4, 100)])
+def test_fork_in_a_pool_of_many_pages(B, W, ps, n_max):
+    """The same forks with more pages than one block's LDS counts."""
+    rs = np.random.RandomState(B + W)
+    for seed in range(3):
+        tables, lens, refs = _state(rs, B, W, ps, n_max, 3 * B * W + 9)
+        R = B * W
+        parents = np.repeat(np.arange(B) * W, W) + rs.randint(0, W, R)
+        parents[rs.rand(R) < 0.1] = -1
+        grow = np.where(rs.rand(R) < 0.8, rs.choice([1, 1, 2, 3 * ps]), 0)
+        used = np.ones(9000, refs.dtype)
+        a = _fork("f16", 2, 1, 64, ps, "heads", parents, tables, lens, refs, grow, seed=seed)
+        b = _fork("f16", 2, 1, 64, ps, "heads", parents, tables, lens, np.concatenate([refs, used]), grow, seed=seed)
+        for x, y in zip(a[:3], b[:3]):
+            assert np.array_equal(x, y)
+        few = np.where(np.cumsum(refs == 0) > 3, np.maximum(refs, 1), refs)  # three free pages are left
+        _fork("f16", 1, 1, 64, ps, "heads", parents, tables, lens, few, grow, seed=seed)
+        _fork("f16", 1, 1, 64, ps, "heads", parents, tables, lens, np.concatenate([few, used]), grow, seed=seed)
+
+
 @pytest.mark.parametrize("R_in,R_out", [(1, 7), (3, 12), (9, 2), (1500, 1300)])
 def test_fork_to_another_number_of_rows(R_in, R_out):
     rs = np.random.RandomState(R_in)
