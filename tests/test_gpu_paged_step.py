@@ -1,0 +1,246 @@
+"""The paged operators as they are used together: prompts admitted, beams forked,
+tokens appended, attended to and selected over many steps, each hypothesis against
+its own history; the same step recorded as a graph; other streams."""
+import numpy as np
+import pytest
+
+from gpu_common import log
+
+pytestmark = pytest.mark.gpu
+
+
+class Beams:
+    """Device state of a beam search: two sets of tables, one pool per layer."""
+
+    def __init__(self, kind, B, W, L, H, Hkv, hd, ps, V, max_len, layout, seed, n_pages=None):
+        import torch
+
+        from paged_common import CODE, DT, make_pool
+        from paper_2503_17707_amd import binding as pb
+
+        self.pb, self.torch = pb, torch
+        self.B, self.W, self.L, self.H, self.Hkv, self.hd, self.ps, self.V = B, W, L, H, Hkv, hd, ps, V
+        self.code, self.dt, R = CODE[kind], DT[kind], B * W
+        self.width = -(-max_len // ps)
+        self.n_pages = n_pages or R * self.width
+        self.pool = make_pool(seed, kind, (L, self.n_pages), Hkv, ps, hd, layout)
+        self.pool.fill_(float("nan"))
+        i32 = dict(dtype=torch.int32, device="cuda")
+        self.sets = [dict(tables=torch.full((R, self.width), -1, **i32), start=torch.zeros(R, **i32),
+                          lens=torch.zeros(R, **i32), refs=torch.zeros(self.n_pages, **i32)) for _ in range(2)]
+        self.short = torch.zeros(2, **i32)
+        self.parents, self.tokens, self.alive = (torch.zeros(B, W, **i32) for _ in range(3))
+        self.scores = torch.zeros(B, W, device="cuda")
+        self.logits = torch.zeros(R, V, device="cuda")
+        self.qkv = torch.zeros(L, R, (H + 2 * Hkv) * hd, dtype=self.dt, device="cuda")
+        self.out = torch.zeros(L, R, H, hd, dtype=self.dt, device="cuda")
+        need = max(pb.page_fork_workspace(R, self.n_pages), pb.beam_select_workspace(B, W, V),
+                   pb.paged_attention_workspace(R, H, self.pool[0], self.width))
+        self.ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+
+    def split(self, l):
+        a, b = self.H * self.hd, (self.H + self.Hkv) * self.hd
+        x = self.qkv[l]
+        return [x[:, i:j].unflatten(1, (-1, self.hd)) for i, j in ((0, a), (a, b), (b, x.shape[1]))]
+
+    def step(self, i, eos):
+        """Fork set i into the other one, append, attend, select."""
+        pb, a, b = self.pb, self.sets[i], self.sets[1 - i]
+        pb.op_page_fork(self.code, self.pool, self.parents.view(-1), a["tables"], a["lens"], a["refs"], self.alive.view(-1),
+                        b["tables"], b["start"], b["lens"], b["refs"], self.short, self.ws)
+        for l in range(self.L):
+            q, k, v = self.split(l)
+            pb.op_kv_append(self.code, k, v, self.pool[l], b["tables"], b["start"], b["lens"])
+            pb.op_paged_attention(self.code, q, self.pool[l], b["tables"], b["lens"], self.out[l], scale=self.hd ** -0.5,
+                                  workspace=self.ws)
+        pb.op_beam_select(self.logits, self.scores, self.alive, self.scores, self.tokens, self.parents, self.alive, eos=eos,
+                          pad=0, workspace=self.ws)
+
+    def admit(self, prompts, prompt_kv):
+        """Prompts' pages for rows 0 .. B-1 of set 0, their keys and values, and beams on them."""
+        torch, pb, B, W, R = self.torch, self.pb, self.B, self.W, self.B * self.W
+        i32 = dict(dtype=torch.int32, device="cuda")
+        lens = torch.tensor(prompts, **i32)
+        one = dict(tables=torch.full((B, self.width), -1, **i32), start=torch.zeros(B, **i32), lens=torch.zeros(B, **i32),
+                   refs=torch.zeros(self.n_pages, **i32))
+        pb.op_page_fork(self.code, self.pool, torch.arange(B, **i32), torch.full((B, self.width), -1, **i32),
+                        torch.zeros(B, **i32), torch.zeros(self.n_pages, **i32), lens, one["tables"], one["start"],
+                        one["lens"], one["refs"], self.short, self.ws)
+        assert self.short.tolist() == [0, 0] and one["lens"].tolist() == list(prompts)
+        row0 = torch.tensor(np.concatenate([[0], np.cumsum(prompts)[:-1]]), **i32)
+        for l in range(self.L):
+            k, v = prompt_kv[l]
+            pb.op_kv_append(self.code, k, v, self.pool[l], one["tables"], one["start"], one["lens"], row0=row0)
+        s = self.sets[0]
+        pb.op_page_fork(self.code, self.pool, torch.arange(R, **i32) // W, one["tables"], one["lens"], one["refs"],
+                        torch.zeros(R, **i32), s["tables"], s["start"], s["lens"], s["refs"], self.short, self.ws)
+        self.parents.copy_(torch.arange(R, **i32).view(B, W))
+        self.alive.fill_(1)
+        self.scores.fill_(-float("inf"))
+        self.scores[:, 0] = 0
+
+
+def _kv(torch, g, dt, rows, Hkv, hd):
+    return [torch.randn((rows, Hkv, hd), generator=g).to(dt).cuda() for _ in range(2)]
+
+
+@pytest.mark.parametrize("kind,layout,B,W,L,H,Hkv,hd,ps,prompts", [
+    ("f16", "rows", 2, 4, 2, 4, 2, 64, 8, (5, 19)),
+    ("bf16", "heads", 3, 3, 1, 6, 6, 128, 16, (16, 1, 31)),
+    ("f16", "gaps", 1, 8, 2, 16, 1, 64, 5, (23,)),
+])
+def test_beam_search_against_histories(kind, layout, B, W, L, H, Hkv, hd, ps, prompts):
+    import torch
+
+    from paged_common import attention64, select64
+
+    log("beam search", kind, layout, B, W, L, H, Hkv, hd, ps, prompts)
+    V, eos, R, steps = 61, 2, B * W, 24
+    s = Beams(kind, B, W, L, H, Hkv, hd, ps, V, max(prompts) + steps + 1, layout, 1)
+    g = torch.Generator().manual_seed(7)
+    prompt_kv = [_kv(torch, g, s.dt, sum(prompts), Hkv, hd) for _ in range(L)]
+    s.admit(prompts, prompt_kv)
+    # per hypothesis and layer its own keys and values
+    begin = np.concatenate([[0], np.cumsum(prompts)])
+    hist = [[torch.stack(prompt_kv[l], 1).cpu()[begin[r // W]:begin[r // W + 1]] for l in range(L)] for r in range(R)]
+    alive, parents = np.ones((B, W), np.int32), np.arange(R)
+    scores = s.scores.cpu().numpy()
+    for step in range(steps):
+        s.qkv.copy_(torch.randn(s.qkv.shape, generator=g))
+        s.logits.copy_(torch.randn(s.logits.shape, generator=g) * 2)
+        if step > 2:
+            s.logits[:, eos] += 1.5
+        new = [[torch.stack([x[r] for x in s.split(l)[1:]]).cpu() for l in range(L)] for r in range(R)]
+        grows = alive.reshape(-1).copy()
+        s.step(step % 2, eos)
+        hist = [[torch.cat([hist[parents[r]][l], new[r][l][None]]) if grows[r] else hist[parents[r]][l] for l in range(L)]
+                if parents[r] >= 0 else [torch.zeros(0, 2, Hkv, hd, dtype=s.dt)] * L for r in range(R)]
+        now = s.sets[1 - step % 2]
+        assert s.short.tolist() == [0, 0]
+        tables, lens = now["tables"].cpu().numpy(), now["lens"].tolist()
+        assert lens == [len(h[0]) for h in hist]
+        held = tables[tables >= 0]
+        assert np.array_equal(np.bincount(held, minlength=s.n_pages), now["refs"].cpu().numpy())
+        for l in range(L):
+            pages = s.pool[l].cpu()
+            for r in range(R):  # bit for bit what the hypothesis went through
+                got = [pages[tables[r, x // ps], :, :, x % ps] for x in range(lens[r])]
+                assert not lens[r] or torch.equal(torch.stack(got), hist[r][l]), (step, l, r)
+            ref, tol = attention64(s.split(l)[0], s.pool[l], tables, lens, ps, hd ** -0.5, 0)
+            assert torch.all((s.out[l].double().cpu() - ref).abs() <= tol)
+        want = select64(s.logits.cpu().numpy(), scores, alive, eos, 0)
+        scores, alive = s.scores.cpu().numpy(), s.alive.cpu().numpy()
+        assert np.array_equal(s.tokens.cpu().numpy(), want[1]) and np.array_equal(s.parents.cpu().numpy(), want[2])
+        assert np.array_equal(alive, want[3])
+        parents = s.parents.cpu().numpy().reshape(-1)
+    log("  alive at the end", alive.tolist())
+
+
+def test_recorded_step_equals_eager():
+    """Two steps (set 0 to 1 and back) as one graph, replayed with new inputs and eager
+    work in between, against the same steps run one by one; two graphs share the workspace."""
+    import torch
+
+    from paper_2503_17707_amd import binding as pb  # noqa: F401
+
+    log("recorded beam step")
+    prompts, L, eos = (40, 700), 2, 2
+    args = ("f16", 2, 4, L, 8, 2, 64, 16, 3000, 780, "heads", 3)
+    a, b = Beams(*args), Beams(*args)
+    g = torch.Generator().manual_seed(9)
+    prompt_kv = [_kv(torch, g, a.dt, sum(prompts), a.Hkv, a.hd) for _ in range(L)]
+    a.admit(prompts, prompt_kv)
+    b.admit(prompts, prompt_kv)
+    side = torch.cuda.Stream()
+
+    def fill(s, i):
+        gg = torch.Generator(device="cuda").manual_seed(100 + i)
+        s.qkv.copy_(torch.randn(s.qkv.shape, generator=gg, device="cuda"))
+        s.logits.copy_(torch.randn(s.logits.shape, generator=gg, device="cuda") * 2)
+
+    # both run one warm step pair eagerly, then b records
+    for s in (a, b):
+        fill(s, 0)
+        s.step(0, eos)
+        s.step(1, eos)
+    keep = [x.clone() for x in (b.scores, b.alive, b.parents, b.tokens)]
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    for i, gr in enumerate(graphs):
+        with torch.cuda.graph(gr):
+            b.step(i, eos)
+    for x, y in zip((b.scores, b.alive, b.parents, b.tokens), keep):
+        assert torch.equal(x, y)  # recording ran nothing
+    for i in range(1, 13):
+        fill(a, i)
+        fill(b, i)
+        a.step(0, eos)
+        a.step(1, eos)
+        if i % 3 == 0:  # on another stream
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                graphs[0].replay()
+                graphs[1].replay()
+            torch.cuda.current_stream().wait_stream(side)
+        else:
+            graphs[0].replay()
+            graphs[1].replay()
+        torch.cuda.synchronize()
+        for name in ("scores", "alive", "parents", "tokens", "short"):
+            assert torch.equal(getattr(a, name), getattr(b, name)), (i, name)
+        live = a.sets[0]["lens"].tolist()
+        assert b.sets[0]["lens"].tolist() == live
+        for n in ("tables", "refs", "start"):
+            assert torch.equal(a.sets[0][n], b.sets[0][n]), (i, n)
+        rows = [r for r in range(8) if live[r]]
+        assert torch.equal(a.out[:, rows], b.out[:, rows])
+    assert max(live) > 700
+
+
+def test_two_streams_at_once():
+    """Calls on two streams, each with its own workspace, and a stream passed by argument."""
+    import torch
+
+    from paged_common import attention64, dev, make_pool, make_tables
+    from paper_2503_17707_amd import binding as pb
+
+    log("paged attention on two streams")
+    ps, H, hd, n = 16, 8, 128, 6000
+    rs = np.random.RandomState(0)
+    tables = make_tables(rs, np.array([n, n]), ps, 2 * (n // ps), n // ps)
+    pool = make_pool(0, "bf16", (2 * (n // ps),), 2, ps, hd, "heads")
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    t, lens = [dev(tables[i:i + 1]) for i in range(2)], dev(np.array([n], np.int32))
+    qs = [torch.randn((1, H, hd), device="cuda").bfloat16() for _ in range(2)]
+    outs = [torch.empty_like(q) for q in qs]
+    ws = [torch.empty(pb.paged_attention_workspace(1, H, pool, n // ps), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i in range(2):
+            pb.op_paged_attention(0, qs[i], pool, t[i], lens, outs[i], scale=0.1, workspace=ws[i], stream=streams[i])
+    torch.cuda.synchronize()
+    for i in range(2):
+        ref, tol = attention64(qs[i], pool, tables[i:i + 1], [n], ps, 0.1, 0)
+        assert torch.all((outs[i].double().cpu() - ref).abs() <= tol)
+
+
+def test_two_runs_give_the_same_bits():
+    import torch
+
+    from paged_common import dev, make_pool, make_tables
+    from paper_2503_17707_amd import binding as pb
+
+    log("paged attention twice")
+    rs = np.random.RandomState(2)
+    lens = np.array([4000, 17, 1500, 0, 2600], np.int32)
+    n_pages = int((-(-lens // 16)).sum())
+    tables = dev(make_tables(rs, lens, 16, n_pages, 260))
+    pool = make_pool(0, "f16", (n_pages,), 4, 16, 64, "rows")
+    q = torch.randn((5, 8, 64), device="cuda").half()
+    ws = torch.empty(pb.paged_attention_workspace(5, 8, pool, 260), dtype=torch.uint8, device="cuda")
+    outs = []
+    for _ in range(3):
+        out = torch.empty_like(q)
+        ws.fill_(255)
+        pb.op_paged_attention(1, q, pool, tables, dev(lens), out, workspace=ws)
+        outs.append(out)
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
