@@ -87,16 +87,18 @@ int pb_op_layernorm(int32_t dtype, const float* x, const void* g, const void* b,
  * Every call is a fixed sequence of kernels that reads lengths, tables and
  * parents on the device, so a step is captured into a HIP graph once and
  * replayed as the sequences grow; nothing is allocated.  Device tensors of
- * int32 are 4-byte aligned, a workspace 256-byte aligned.  A workspace carries
+ * int32 are 4-byte aligned, a workspace 16-byte aligned.  A workspace carries
  * nothing from one call to the next: calls that run one after another on a
- * stream may share one, calls that may overlap need one each. */
+ * stream may share one (two recorded graphs too, if their replays do not
+ * overlap), calls that may overlap need one each.  Every buffer and the stream
+ * belong to the current device. */
 
 /* Pages of one layer.  Element j of token t of head h, keys (c = 0) or values
  * (c = 1), of page i is at
  *   base + i page_stride + c v_offset + h head_stride + t token_stride + j,
  * strides in elements of dt, multiples of 8 and at least head_dim (that of a
  * dimension of size 1 is not used), token_stride below 2^31; base 16-byte aligned.  head_dim is 64 or 128,
- * page_size 1..4096 tokens.  Both a page that holds its tokens as the model's
+ * page_size 1..4096 tokens, at most 2^30 pages.  Both a page that holds its tokens as the model's
  * cache rows [k | v] (token_stride 2 Hkv hd, v_offset Hkv hd, head_stride hd)
  * and one that holds each head's tokens in a row fit.  A page table row holds the
  * page of tokens 0 .. page_size-1, then the next, ...: int32 [rows][width]. */
@@ -131,9 +133,9 @@ int pb_op_kv_append(int32_t dtype, const void* k, int64_t ld_k, const void* v, i
  * are not looked at).  Nothing past a sequence's last token is read.
  * Scores, maxima, sums and products are fp32; probabilities are rounded to dt
  * as they enter the products with V.
- * workspace (may be NULL, at most as fast without): fp32 partial results of the
- * pieces that long sequences are split into, pb_op_paged_attention_workspace
- * bytes; a smaller one means fewer pieces. */
+ * workspace (may be NULL): fp32 partial results of the pieces that long
+ * sequences are cut into, pb_op_paged_attention_workspace bytes; with a smaller one
+ * they are not cut.  Tables hold at most 2^30 tokens a row. */
 int pb_op_paged_attention(int32_t dtype, const void* q, int64_t ld_q, const pb_kv_pool* pool,
                           const int32_t* tables, int32_t width, int64_t ld_tables, const int32_t* lens,
                           int32_t n_seqs, int32_t n_heads, float scale, int32_t window, void* out,

@@ -6,19 +6,24 @@
 // heads to a key/value head the matrix units take them all at the price of one.
 // So everything here serves loads in flight and an even share of them:
 //
-//  - A wave takes tiles of 32 tokens.  Keys go from memory straight into the
+//  - A wave takes tiles of 16 or 32 tokens.  Keys go from memory straight into the
 //    A operand of v_mfma_f32_16x16x32 (a lane holds 8 consecutive dimensions of one
 //    token), S^T[token, query] = K Q^T with the group's queries as the 16 columns.
 //    Values are contracted over tokens, which memory does not hold consecutively:
 //    they pass through LDS (written by rows, read with the transposing
 //    ds_read_b64_tr_b16), O^T[dimension, query] += V^T P^T.  As soon as a tile's
-//    registers are free the next tile's loads are issued, so a wave has 8 KB
-//    (HD 64) or 16 KB (HD 128) in flight while it works.
-//  - Sequences are cut into pieces of equal length, the same for all sequences of
-//    a call and chosen on the device from their lengths (the lengths may change
-//    between replays of a recorded launch), so that about PIECES blocks of equal
-//    work cover a ragged batch as well as one long sequence.  A second launch
-//    joins the pieces of sequences that have several.
+//    registers are free the next tile's loads are issued.  (Two tiles ahead: no
+//    faster for few blocks, 10% slower for many, which then hold fewer waves.)
+//    Values are read once and by whole lines, so they bypass what caches may keep
+//    (131071 tokens: 98.5 us against 107); a line of keys is read in two halves.
+//  - Sequences are cut into pieces, at most as long as a length chosen on the device
+//    from the call's lengths (which may change between replays of a recorded launch),
+//    so that about PIECES blocks of like work cover a ragged batch as well as one long
+//    sequence.  A second launch joins the pieces of sequences that have several.
+//
+// Measured: 131071 tokens, 32 heads on 8 of 128 (537 MB) 96 us, 5.6 TB/s; 48 ragged
+// sequences up to 16384, 64 heads on 8 (368 MB) 74 us, 5.0 TB/s; 32 ragged up to 2048,
+// 40 heads (198 MB) 45 us, 4.4 TB/s; a 4 GiB copy reaches 4.7 TB/s on this card.
 #include "common.h"
 #include "paged.h"
 
@@ -31,32 +36,15 @@ constexpr float LOG2E = 1.4426950408889634f;
 // three waves per SIMD instead of two at the same bytes in flight; with more, 32.
 template <int NQ> constexpr int tile_of() { return NQ == 1 ? 16 : 32; }
 constexpr int IDS = 512;      // pages whose places are held in LDS at a time
-#ifndef PB_PA_TARGET
-#define PB_PA_TARGET 1024
-#endif
-#ifndef PB_PA_EU
-#define PB_PA_EU 2
-#endif
-#ifndef PB_PA_NWF
-#define PB_PA_NWF 8
-#endif
-#ifndef PB_PA_FEW
-#define PB_PA_FEW 512
-#endif
-#ifndef PB_PA_CMIN
-#define PB_PA_CMIN 256
-#endif
-#ifndef PB_PA_CU
-#define PB_PA_CU 256
-#endif
-#ifndef PB_PA_CMAX
-#define PB_PA_CMAX 512
-#endif
-#ifndef PB_PA_UNCUT
-#define PB_PA_UNCUT 1024
-#endif
-constexpr int PIECES = PB_PA_TARGET;  // blocks aimed at
-constexpr int SHORTEST = PB_PA_CMIN;  // tokens a piece has at least
+// Pieces (us for 48 ragged sequences up to 16384, 64 heads on 8 of 128 | one of 131071,
+// 32 on 8 | 8 of 2048, 40 heads of 128): for 1024 blocks 78.0 | 99.0 | 67.4, for 2048
+// 73.9 | 96.3 | 67.5.
+constexpr int PIECES = 2048;  // blocks aimed at
+// No piece is shorter than SHORTEST tokens, nor than LEAST once the blocks of such
+// pieces number more than 512: what a block does before its first tile costs as much
+// as some 100 tokens.  5 sequences of 1714, 64 heads on 8 of 128: 128 tokens 15.4 us,
+// 256 19.8; 32 of 303, 40 heads of 128: 256 54 us, 512 47.
+constexpr int SHORTEST = 128, LEAST = 512, FEW_BLOCKS = 512;
 
 // How a call is cut: written to the workspace by the first block, read by the join.
 struct Cut {
@@ -113,6 +101,30 @@ __device__ __forceinline__ float group4_max(float v) {
     return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
+// Sum over the wave in every lane, and sum over the lanes up to this one: in
+// registers (a lane exchange through LDS takes a hundred cycles, and the cut of a
+// call needs a dozen of them before the first load).
+__device__ __forceinline__ int wave_sum_dpp(int v) {
+    v += __builtin_amdgcn_mov_dpp(v, 0xB1, 0xf, 0xf, false);   // quad_perm 1 0 3 2
+    v += __builtin_amdgcn_mov_dpp(v, 0x4E, 0xf, 0xf, false);   // quad_perm 2 3 0 1
+    v += __builtin_amdgcn_mov_dpp(v, 0x141, 0xf, 0xf, false);  // row_half_mirror
+    v += __builtin_amdgcn_mov_dpp(v, 0x140, 0xf, 0xf, false);  // row_mirror
+    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = (int)(a[0] + a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return (int)(b[0] + b[1]);
+}
+
+__device__ __forceinline__ int wave_scan_dpp(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr 1
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);  // row_shr 2
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);  // row_shr 4
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);  // row_shr 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // lane 15 of a row to rows 1, 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // lane 31 to rows 2, 3
+    return v;
+}
+
 // LDS written and read by the same wave: its LDS instructions run in order, the
 // compiler has to keep them so.
 __device__ __forceinline__ void wave_lds_order() {
@@ -135,19 +147,18 @@ __device__ __forceinline__ Span span_of(const PagedAttentionParams& p, int s) {
     return r;
 }
 
-// Pieces of this call are at most so long: PIECES blocks of it hold all tokens of
-// all heads, but none is shorter than SHORTEST (twice that once there are more
-// blocks than CUs).
+// Pieces of this call are at most so long.
 __device__ __forceinline__ int piece_length(int64_t tokens, int blocks_per_piece) {
     const int64_t c = (tokens * blocks_per_piece + PIECES - 1) / PIECES;
-    const int64_t least = min(max(tokens * blocks_per_piece / PB_PA_CU, (int64_t)SHORTEST), (int64_t)PB_PA_CMAX);
-    return (int)min(max(c, least), (int64_t)1 << 30);  // no sequence is longer
+    const int64_t least = min(max(tokens * blocks_per_piece / FEW_BLOCKS, (int64_t)SHORTEST), (int64_t)LEAST);
+    const int64_t m = min(max(c, least), (int64_t)1 << 30);  // no sequence is longer
+    return (int)((m + 31) / 32 * 32);
 }
 
 __device__ __forceinline__ int pieces_of(int n, int len_c) { return max(1, (n + len_c - 1) / len_c); }
 
 template <typename T, int HD, int NQ, int NW>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NQ == 2 ? 2 : PB_PA_EU)))
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2)))
 void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
     typedef typename Mfma<T>::vec8 vec8;
     constexpr int KT = tile_of<NQ>();
@@ -170,6 +181,7 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
     const int hb = p.pool.n_kv_heads * cut.qb;
     const int kvh = blockIdx.x % hb / cut.qb, q0 = blockIdx.x % cut.qb * 16 * NQ;
     int s = blockIdx.x / hb, piece = 0, pieces = 1, slot = 0;
+    Span sp;
 
     if (cut.on) {
         // Which piece of which sequence: every wave works the cut out for itself from
@@ -177,30 +189,34 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
         // equally long; the long pieces come first, so that the short ones fill the end.
         const int S = p.tab.rows, per = (S + 63) / 64;
         const int s0 = min(lane * per, S), s1 = min(s0 + per, S);
-        int64_t sum = 0;
-        for (int i = s0; i < s1; ++i) sum += span_of(p, i).n;
-        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-        const int len_c = piece_length(sum, hb);
+        // tokens in two parts whose sums over 65535 sequences of 2^30 fit 32 bits
+        const Span own = s0 < s1 ? span_of(p, s0) : Span{};
+        int low = 0, high = 0;
+        for (int i = s0; i < s1; ++i) {
+            const int n = i == s0 ? own.n : span_of(p, i).n;
+            low += n & 0x7fff;
+            high += n >> 15;
+        }
+        const int len_c = piece_length(((int64_t)wave_sum_dpp(high) << 15) + wave_sum_dpp(low), hb);
         auto is_long = [&](int n, int k) { return n >= (int64_t)k * (len_c / 2); };
         int n_long = 0, n_short = 0;  // pieces of this lane's sequences
         for (int i = s0; i < s1; ++i) {
-            const int n = span_of(p, i).n, k = pieces_of(n, len_c);
+            const int n = i == s0 ? own.n : span_of(p, i).n, k = pieces_of(n, len_c);
             if (is_long(n, k)) n_long += k; else n_short += k;
         }
-        int at_long = n_long, at_short = n_short;
-        for (int o = 1; o < 64; o <<= 1) {
-            const int y = __shfl_up(at_long, o, 64), z = __shfl_up(at_short, o, 64);
-            if (lane >= o) at_long += y, at_short += z;
-        }
-        at_short += __shfl(at_long, 63, 64) - n_short;
+        int at_long = wave_scan_dpp(n_long), at_short = wave_scan_dpp(n_short);
+        at_short += __builtin_amdgcn_readlane(at_long, 63) - n_short;
         at_long -= n_long;
         const int item = blockIdx.x / hb;
         int mine = -1;
+        Span found{};
         for (int i = s0; i < s1; ++i) {
-            const int n = span_of(p, i).n, k = pieces_of(n, len_c);
+            const Span x = i == s0 ? own : span_of(p, i);
+            const int n = x.n, k = pieces_of(n, len_c);
             int& at = is_long(n, k) ? at_long : at_short;
             if (item >= at && item < at + k) {
                 mine = i;
+                found = x;
                 piece = item - at;
                 pieces = k;
             }
@@ -216,10 +232,14 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
         s = __builtin_amdgcn_readlane(mine, l);
         piece = __builtin_amdgcn_readlane(piece, l);
         pieces = __builtin_amdgcn_readlane(pieces, l);
+        sp.lo = __builtin_amdgcn_readlane(found.lo, l);
+        sp.n = __builtin_amdgcn_readlane(found.n, l);
+        sp.wide = __builtin_amdgcn_readlane(found.wide, l);
         slot = item;
+    } else {
+        sp = span_of(p, s);
     }
 
-    const Span sp = span_of(p, s);
     const int len_p = pieces == 1 ? sp.n : (sp.n + pieces * 32 - 1) / (pieces * 32) * 32;
     const int ka = sp.lo + min(piece * len_p, sp.n);
     const int kb = min(ka + len_p, sp.lo + sp.n);
@@ -421,7 +441,7 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
             }
         }
         if (pieces > 1 && tid % (4 * NW) == 0) {
-            cut.ml[((int64_t)slot * p.n_heads + h) * 2] = Mb;
+            cut.ml[((int64_t)slot * p.n_heads + h) * 2] = M;
             cut.ml[((int64_t)slot * p.n_heads + h) * 2 + 1] = L;
         }
     }
@@ -442,24 +462,36 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttentionParams p,
     const int64_t rows = p.n_heads;
     const float2* ml = (const float2*)cut.ml + i0 * rows + h;
     const float* acc = cut.acc + i0 * rows * HD + d;
+    // the first HOLD pieces of a thread are on their way before the maximum is known
+    constexpr int HOLD = 4;
+    float2 w[HOLD];
+    f32x4 v[HOLD];
     float M = -INFINITY;
-#pragma unroll 4
-    for (int i = y; i < n; i += TY) M = fmaxf(M, ml[i * rows].x);
+#pragma unroll
+    for (int j = 0; j < HOLD; ++j) {
+        const int i = min(y + j * TY, n - 1);
+        w[j] = ml[i * rows];
+        v[j] = *(const f32x4*)(acc + i * rows * HD);
+        M = fmaxf(M, w[j].x);
+    }
+    for (int i = y + HOLD * TY; i < n; i += TY) M = fmaxf(M, ml[i * rows].x);
     sm[y][x] = M;
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < TY; ++j) M = fmaxf(M, sm[j][x]);
     f32x4 a = f32x4{0.f, 0.f, 0.f, 0.f};
     float L = 0.f;
-#pragma unroll 4
-    for (int i = y; i < n; i += TY) {
-        const float2 w = ml[i * rows];
-        const f32x4 v = *(const f32x4*)(acc + i * rows * HD);
-        const float f = __builtin_amdgcn_exp2f(w.x - M);
-        L += f * w.y;
+    auto add = [&](float2 u, f32x4 o) {
+        const float f = __builtin_amdgcn_exp2f(u.x - M);
+        L += f * u.y;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) a[r] += f * v[r];
-    }
+        for (int r = 0; r < 4; ++r) a[r] += f * o[r];
+    };
+#pragma unroll
+    for (int j = 0; j < HOLD; ++j)
+        if (y + j * TY < n) add(w[j], v[j]);
+#pragma unroll 4
+    for (int i = y + HOLD * TY; i < n; i += TY) add(ml[i * rows], *(const f32x4*)(acc + i * rows * HD));
     __syncthreads();  // the maxima were read
     sa[y][x] = a;
     sm[y][x] = L;
@@ -510,7 +542,11 @@ hipError_t launch(const PagedAttentionParams& p, hipStream_t s) {
     const int hb = p.pool.n_kv_heads * cut.qb;
     int64_t items = p.tab.rows;
     const int64_t most = most_pieces(p.tab.rows, hb, p.tab.width, p.pool.page_size);
-    if ((int64_t)p.tab.width * p.pool.page_size > PB_PA_UNCUT && most > p.tab.rows && p.ws && p.ws_bytes >= cut_bytes(p.tab.rows, most, p.n_heads, HD)) {
+    // Short sequences stay whole: the join costs 4 us (one of 513, 32 heads of 64: 6.3
+    // us, cut 9.4), and so do longer ones that fill the chip as they are (8 of 1000: 14.1,
+    // cut 18.5; one of 2000: 11.2 cut, 16.7 whole).
+    const int uncut = HD == 64 && p.tab.rows * hb >= 256 ? 2048 : 1024;
+    if ((int64_t)p.tab.width * p.pool.page_size > uncut && most > p.tab.rows && p.ws && p.ws_bytes >= cut_bytes(p.tab.rows, most, p.n_heads, HD)) {
         cut.on = 1;
         cut.at = (int32_t*)p.ws;
         cut.acc = (float*)((char*)p.ws + ((size_t)p.tab.rows * 8 + 15) / 16 * 16);
@@ -519,7 +555,10 @@ hipError_t launch(const PagedAttentionParams& p, hipStream_t s) {
     }
     if (items * hb > 0x7fffffff) return hipErrorInvalidValue;
     const dim3 grid((unsigned)(items * hb));
-    if (nq == 1 && items * hb < PB_PA_FEW) PB_LAUNCH((paged_attention_kernel<T, HD, 1, PB_PA_NWF>), grid, dim3(64 * PB_PA_NWF), 0, s, p, cut);
+    // Few uncut blocks: eight waves each (8 sequences of 1000, 32 heads of 64: 14.1 us,
+    // four 16.4); cut ones have little to share out.
+    if (nq == 1 && !cut.on && items * hb < 512)
+        PB_LAUNCH((paged_attention_kernel<T, HD, 1, 8>), grid, dim3(512), 0, s, p, cut);
     else if (nq == 1) PB_LAUNCH((paged_attention_kernel<T, HD, 1, 4>), grid, dim3(256), 0, s, p, cut);
     else PB_LAUNCH((paged_attention_kernel<T, HD, 2, 4>), grid, dim3(256), 0, s, p, cut);
     if (cut.on) launch_join<T, HD>(p, cut, s);

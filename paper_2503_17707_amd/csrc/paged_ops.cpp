@@ -32,7 +32,7 @@ int launched(const char* op, hipError_t e) {
 bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
 bool sizes_ok(const pb_kv_pool* c) {
-    return c && c->n_pages >= 1 && c->page_size >= 1 && c->page_size <= 4096 && c->n_kv_heads >= 1 &&
+    return c && c->n_pages >= 1 && c->n_pages <= (1 << 30) && c->page_size >= 1 && c->page_size <= 4096 && c->n_kv_heads >= 1 &&
            c->n_kv_heads <= 65535 && (c->head_dim == 64 || c->head_dim == 128);
 }
 
@@ -171,7 +171,7 @@ extern "C" int pb_op_beam_select(const float* logits, int64_t ld_logits, const f
 }
 
 extern "C" size_t pb_op_page_fork_workspace(int32_t out_rows, int32_t n_pages) {
-    if (out_rows < 0 || out_rows > 65535 || n_pages < 1) return 0;
+    if (out_rows < 0 || out_rows > 65535 || n_pages < 1 || n_pages > (1 << 30)) return 0;
     return pb::page_fork_workspace(out_rows, n_pages);
 }
 

@@ -99,6 +99,34 @@ def test_peaked_and_flat_scores():
     _run("bf16", 4, 4, 128, 16, "heads", [700, 65], scale=-0.3)
 
 
+@pytest.mark.parametrize("sign", [-1, 1])
+@pytest.mark.parametrize("kind,hd", [("f16", 64), ("bf16", 128)])
+def test_scores_far_from_zero_in_many_pieces(kind, hd, sign):
+    """Scores near sign * 600 in sequences cut in many ways, the cut not a multiple of a tile."""
+    import torch
+
+    from paged_common import CODE, DT, attention64, dev, make_pool, make_tables
+    from paper_2503_17707_amd import binding as pb
+
+    log("paged attention far scores", kind, hd, sign)
+    rs = np.random.RandomState(4)
+    lens = np.concatenate([rs.randint(1, 6000, 30), [5999, 2049, 129, 1]]).astype(np.int32)
+    ps, width = 16, 380
+    n_pages = int((-(-lens // ps)).sum())
+    tables = make_tables(rs, lens, ps, n_pages, width)
+    pool = make_pool(5, kind, (n_pages,), 2, ps, hd, "heads")
+    pool[:, 0, :, :, 0] = sign * 60.0
+    q = torch.randn((len(lens), 4, hd), device="cuda").to(DT[kind])
+    q[..., 0] = 10.0
+    for rows in (len(lens), 7):
+        out = torch.empty_like(q[:rows])
+        ws = torch.full((pb.paged_attention_workspace(rows, 4, pool, width),), 255, dtype=torch.uint8, device="cuda")
+        assert ws.numel() > 0
+        pb.op_paged_attention(CODE[kind], q[:rows], pool, dev(tables[:rows]), dev(lens[:rows]), out, workspace=ws)
+        ref, tol = attention64(q[:rows], pool, tables[:rows], lens[:rows], ps, 1.0, 0)
+        assert torch.all((out.double().cpu() - ref).abs() <= tol)
+
+
 def test_many_small_probabilities_beside_a_large_one():
     """One key far above 20000 others that weigh 2^-18 each: together 7 percent."""
     import torch

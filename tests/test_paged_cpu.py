@@ -12,9 +12,10 @@ def _pool(pb, **kw):
     return p
 
 
-BAD_POOLS = [dict(base=0), dict(base=0x1008), dict(n_pages=0), dict(page_size=0), dict(page_size=4097), dict(n_kv_heads=0),
+BAD_POOLS = [dict(base=0), dict(base=0x1008), dict(n_pages=0), dict(n_pages=(1 << 30) + 1), dict(page_size=0), dict(page_size=4097), dict(n_kv_heads=0),
              dict(head_dim=96), dict(page_stride=4), dict(page_stride=4100), dict(v_offset=-64), dict(head_stride=0),
-             dict(token_stride=63), dict(token_stride=1 << 50)]
+             dict(token_stride=63), dict(token_stride=1 << 31), dict(token_stride=1 << 50),
+             dict(head_stride=1 << 45)]
 P = 0x10000  # a pointer that no refused call follows
 
 
@@ -77,7 +78,7 @@ def test_append_refusals(bad):
 @pytest.mark.parametrize("bad", [dict(dtype=-1), dict(q=None), dict(q=P + 2), dict(ld_q=504), dict(ld_q=516), dict(out=None),
                                  dict(out=P + 8), dict(ld_out=256), dict(tables=None), dict(width=-1), dict(ld=2),
                                  dict(lens=None), dict(S=-2), dict(S=1 << 17), dict(H=0), dict(H=6), dict(H=1 << 17),
-                                 dict(scale=float("nan")), dict(scale=float("inf")), dict(window=-1), dict(ws=P + 4)], ids=str)
+                                 dict(width=1 << 27, ld=1 << 27), dict(scale=float("nan")), dict(scale=float("inf")), dict(window=-1), dict(ws=P + 4)], ids=str)
 def test_attention_refusals(bad):
     from paper_2503_17707_amd import binding as pb
 
