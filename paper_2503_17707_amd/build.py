@@ -13,10 +13,13 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
+# the paged cache and beam search, apart from the model's kernels: profile summaries
+# hold for the contents of csrc
+PAGED = os.path.join(HERE, "paged")
 OUT_DIR = os.path.join(HERE, "lib")
 LIB = os.path.join(OUT_DIR, "libpipeboost.so")
-SOURCES = ["gemm.hip", "attention.hip", "misc.hip", "lmhead.hip", "paged_attention.hip",
-           "paged_cache.hip", "beam.hip", "model.cpp", "paged_ops.cpp", "sched.cpp"]
+SOURCES = ["gemm.hip", "attention.hip", "misc.hip", "lmhead.hip", "model.cpp", "sched.cpp"]
+PAGED_SOURCES = ["paged_attention.hip", "paged_cache.hip", "beam.hip", "paged_ops.cpp"]
 ARCH = os.environ.get("PB_OFFLOAD_ARCH", "gfx950")
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=" + ARCH, "-Wall", "-Wno-unused-result",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -26,7 +29,8 @@ FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=" + ARCH, "-Wall", "-Wno-
 def _compile(src: str, obj_dir: str, defines=()) -> str:
     obj = os.path.join(obj_dir, os.path.splitext(src)[0] + ".o")
     lang = ["-x", "hip"] if src.endswith(".cpp") else []
-    cmd = (["hipcc", "-c"] + lang + [os.path.join(CSRC, src), "-o", obj] + FLAGS
+    path = os.path.join(PAGED if src in PAGED_SOURCES else CSRC, src)
+    cmd = (["hipcc", "-c"] + lang + [path, "-o", obj] + FLAGS
            + ["-D" + d for d in defines])
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
@@ -43,8 +47,9 @@ def build(verbose: bool = False, out: str = LIB, defines=()) -> str:
     obj_dir = os.path.join(ROOT, "_build", "pipeboost_" + tag)
     os.makedirs(obj_dir, exist_ok=True)
     os.makedirs(os.path.dirname(out), exist_ok=True)
-    with cf.ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as ex:
-        objs = list(ex.map(lambda s: _compile(s, obj_dir, defines), SOURCES))
+    sources = SOURCES + PAGED_SOURCES
+    with cf.ThreadPoolExecutor(max_workers=min(8, len(sources))) as ex:
+        objs = list(ex.map(lambda s: _compile(s, obj_dir, defines), sources))
     tmp = out + ".tmp%d" % os.getpid()
     cmd = ["hipcc", "-shared", "-fPIC", "--offload-arch=" + ARCH, "-o", tmp] + objs
     r = subprocess.run(cmd, capture_output=True, text=True)
