@@ -6,27 +6,9 @@
 #include <stddef.h>
 #include <stdint.h>
 
-namespace pb {
+#include "fastdiv.h"
 
-// Quotients by a divisor fixed at launch, exact for 0 <= n < 2^31: with
-// s = ceil(log2 d) and m = floor(2^(31 + s) / d) + 1, n / d = (2 n m) >> (32 + s)
-// (m d - 2^(31 + s) <= d <= 2^s, so the error n (m d - 2^(31+s)) / (d 2^(31+s)) is
-// below 1 / d; m < 2^32 because d > 2^(s-1)).
-struct FastDiv {
-    uint32_t m, s, d;
-    FastDiv(uint32_t div = 1) : d(div) {
-        s = 0;
-        while ((1u << s) < div) ++s;
-        m = (uint32_t)((((uint64_t)1 << (31 + s)) / div) + 1);
-    }
-    __host__ __device__ inline uint32_t quot(uint32_t n) const {
-#if defined(__HIP_DEVICE_COMPILE__)
-        return __umulhi(n << 1, m) >> s;
-#else
-        return (uint32_t)(((uint64_t)(n << 1) * m) >> 32) >> s;
-#endif
-    }
-};
+namespace pb {
 
 // One layer's pages.  Element (page, c, h, t, j) (c = 0 keys, 1 values) is at
 // base + page page_stride + c v_offset + h head_stride + t token_stride + j;

@@ -22,29 +22,30 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendParams p, int rpb,
     const int s = blockIdx.y;
     const int start = p.start[s];
     const int n = (int)min((int64_t)p.lens[s] - start, (int64_t)p.max_rows);
-    const int i0 = blockIdx.x * rpb;
-    if (start < 0 || i0 >= n) return;
-    const int i1 = min(i0 + rpb, n);
+    if (start < 0) return;
     const int64_t row0 = p.row0 ? p.row0[s] : (int64_t)s * p.max_rows;
     const int lc = p.pool.head_dim == 128 ? 4 : 3;          // log2 of a head's 16-byte chunks
     const int half = p.pool.n_kv_heads << lc;               // chunks of a row of K
     const int32_t* ids = p.tab.ids + s * p.tab.ld;
-    for (int c = threadIdx.x; c < (i1 - i0) * 2 * half; c += 256) {
-        const int r = per_row.quot(c), i = i0 + r;
-        int e = c - r * 2 * half;
-        const bool isv = e >= half;
-        e -= isv ? half : 0;
-        const int h = e >> lc, j = (e & ((1 << lc) - 1)) * 8;
-        const int64_t row = row0 + i;
-        const int col = p.pool.div.quot(start + i);
-        if (row < 0 || row >= p.n_rows || col >= p.tab.width) continue;
-        const int page = ids[col];
-        if (page < 0 || page >= p.pool.n_pages) continue;
-        const u32x4 val = *(const u32x4*)((isv ? p.v + row * p.ld_v : p.k + row * p.ld_k) + e * 8);
-        u32x4* to = (u32x4*)(p.pool.base + page * p.pool.page_stride + (isv ? p.pool.v_offset : 0) +
-                             h * p.pool.head_stride + (start + i - col * p.pool.page_size) * p.pool.token_stride + j);
-        if (PROMPTS) __builtin_nontemporal_store(val, to);
-        else *to = val;
+    for (int64_t i0 = (int64_t)blockIdx.x * rpb; i0 < n; i0 += (int64_t)gridDim.x * rpb) {
+        const int rows = min((int64_t)rpb, n - i0);
+        for (int c = threadIdx.x; c < rows * 2 * half; c += 256) {
+            const int r = per_row.quot(c), i = (int)i0 + r;
+            int e = c - r * 2 * half;
+            const bool isv = e >= half;
+            e -= isv ? half : 0;
+            const int h = e >> lc, j = (e & ((1 << lc) - 1)) * 8;
+            const int64_t row = row0 + i;
+            const int col = p.pool.div.quot(start + i);
+            if (row < 0 || row >= p.n_rows || col >= p.tab.width) continue;
+            const int page = ids[col];
+            if (page < 0 || page >= p.pool.n_pages) continue;
+            const u32x4 val = *(const u32x4*)((isv ? p.v + row * p.ld_v : p.k + row * p.ld_k) + e * 8);
+            u32x4* to = (u32x4*)(p.pool.base + page * p.pool.page_stride + (isv ? p.pool.v_offset : 0) +
+                                 h * p.pool.head_stride + (start + i - col * p.pool.page_size) * p.pool.token_stride + j);
+            if (PROMPTS) __builtin_nontemporal_store(val, to);
+            else *to = val;
+        }
     }
 }
 
@@ -373,7 +374,9 @@ hipError_t launch_kv_append(const AppendParams& p, hipStream_t s) {
     const int row_bytes = 2 * p.pool.n_kv_heads * p.pool.head_dim * 2;
     const int rpb = p.max_rows == 1 ? 1 : (16384 + row_bytes - 1) / row_bytes;
     const FastDiv per_row(2 * p.pool.n_kv_heads * p.pool.head_dim / 8);
-    const dim3 grid((p.max_rows + rpb - 1) / rpb, p.tab.rows);
+    // (max_rows may be far more than any sequence has: blocks take rows in turn then)
+    const int blocks = (p.max_rows + rpb - 1) / rpb, most = 32768 / p.tab.rows + 1;
+    const dim3 grid(blocks < most ? blocks : most, p.tab.rows);
     if (p.max_rows == 1) PB_LAUNCH(kv_append_kernel<false>, grid, dim3(256), 0, s, p, rpb, per_row);
     else PB_LAUNCH(kv_append_kernel<true>, grid, dim3(256), 0, s, p, rpb, per_row);
     return hipGetLastError();

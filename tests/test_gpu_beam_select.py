@@ -145,3 +145,15 @@ def test_large_logits_and_scores():
     _run(logits, scores, alive)
     _run(logits * 1e30, scores, alive)
     _run(logits + 1e4, scores * 1000, alive)
+
+
+def test_masks_of_the_lowest_float():
+    """Tokens masked with the type's lowest value are the last candidates, not none."""
+    rs = np.random.RandomState(10)
+    low = np.finfo(np.float32).min
+    logits, scores, alive = _random(rs, 3, 4, 700)
+    alive[:] = 1
+    logits[:, 3:] = low
+    logits[4:8] = low
+    _run(logits, scores, alive)
+    _run(np.where(rs.rand(12, 700) < 0.5, low, -INF), scores, alive)

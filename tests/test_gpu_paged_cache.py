@@ -65,6 +65,15 @@ def test_append_prompts(layout, Hkv, hd):
     _append("f16", Hkv, hd, 16, layout, [0, 2, 5], [33, 7, 5], max_rows=9)
 
 
+def test_append_with_a_bound_far_above_the_rows():
+    # max_rows left at the number of rows: many blocks' worth for each of many sequences
+    rs = np.random.RandomState(1)
+    count = rs.randint(0, 40, 700)
+    row0 = np.concatenate([[0], np.cumsum(count)[:-1]])
+    _append("f16", 1, 64, 16, "heads", np.zeros(700), count, row0=row0.tolist())
+    _append("bf16", 2, 128, 16, "rows", [0, 3], [9000, 5], max_rows=9000)
+
+
 def test_append_skips_what_has_no_place():
     tables = np.array([[0, -1, 2], [3, 9, 5], [6, 7, 8], [1, -3, 1 << 30]], np.int32)
     # holes, ids past the pool, past the width, a negative start, rows outside k and v

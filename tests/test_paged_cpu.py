@@ -128,6 +128,47 @@ def test_workspace_sizes():
     assert L.pb_op_paged_attention_workspace(2, 8, None, 10) == 0
 
 
+def test_page_division(tmp_path):
+    """The quotients of page numbers against the machine's: divisors and numerators at
+    the edges and between."""
+    import os
+    import shutil
+    import subprocess
+
+    if not shutil.which("g++"):
+        pytest.skip("no C++ compiler")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    src = tmp_path / "div.cpp"
+    src.write_text("""
+#include <cstdio>
+#include "fastdiv.h"
+int main() {
+    const uint32_t top = 0x7fffffffu;
+    unsigned long long seed = 1;
+    for (uint32_t k = 0; k < 20000; ++k) {
+        seed = seed * 6364136223846793005ull + 1442695040888963407ull;
+        const uint32_t d = k < 5000 ? k + 1 : k < 5031 ? 1u << (k - 5000) : k < 5062 ? (1u << (k - 5031)) + 1
+                           : k < 5093 ? top >> (k - 5062) : (uint32_t)(seed >> 33) >> (k % 31);
+        if (!d || d > top) continue;
+        const pb::FastDiv f(d);
+        for (int j = 0; j < 200; ++j) {
+            seed = seed * 6364136223846793005ull + 1442695040888963407ull;
+            const uint32_t q = (uint32_t)(seed >> 33) / d;
+            const uint32_t ns[] = {(uint32_t)(seed >> 33), q * d, q * d + d - 1, q ? q * d - 1 : 0, top, (uint32_t)j};
+            for (uint32_t n : ns)
+                if (n <= top && f.quot(n) != n / d) return printf("%u / %u\\n", n, d), 1;
+        }
+    }
+    return 0;
+}
+""")
+    exe = str(tmp_path / "div")
+    inc = os.path.join(root, "paper_2503_17707_amd", "paged")
+    subprocess.run(["g++", "-O2", "-std=c++17", "-I" + inc, str(src), "-o", exe], check=True)
+    r = subprocess.run([exe], capture_output=True, text=True)
+    assert r.returncode == 0, r.stdout
+
+
 def test_wrappers_refuse_what_the_library_cannot_see():
     import torch
 
