@@ -131,6 +131,8 @@ int pb_op_kv_append(int32_t dtype, const void* k, int64_t ld_k, const void* v, i
  * aligned.  lens[s] <= 0: zeros.  A row with a page id outside the pool, or past
  * the table's width, among the tokens it attends to: NaN (pages before the window
  * are not looked at).  Nothing past a sequence's last token is read.
+ * shared != 0 says that rows next to each other share pages (beams of one prompt):
+ * caches are used then for what otherwise streams past them; results are the same.
  * Scores, maxima, sums and products are fp32; probabilities are rounded to dt
  * as they enter the products with V.
  * workspace (may be NULL): fp32 partial results of the pieces that long
@@ -138,8 +140,8 @@ int pb_op_kv_append(int32_t dtype, const void* k, int64_t ld_k, const void* v, i
  * they are not cut.  Tables hold at most 2^30 tokens a row. */
 int pb_op_paged_attention(int32_t dtype, const void* q, int64_t ld_q, const pb_kv_pool* pool,
                           const int32_t* tables, int32_t width, int64_t ld_tables, const int32_t* lens,
-                          int32_t n_seqs, int32_t n_heads, float scale, int32_t window, void* out,
-                          int64_t ld_out, void* workspace, size_t workspace_bytes, void* stream);
+                          int32_t n_seqs, int32_t n_heads, float scale, int32_t window, int32_t shared,
+                          void* out, int64_t ld_out, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Workspace bytes for n_seqs sequences of tables of `width` pages (0 for
  * arguments pb_op_paged_attention refuses). */

@@ -153,7 +153,7 @@ _SIGS = {
     "pb_op_paged_attention": (ctypes.c_int, [ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
                                              ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p,
                                              ctypes.c_int32, ctypes.c_int32, ctypes.c_float, ctypes.c_int32,
-                                             ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t,
+                                             ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t,
                                              ctypes.c_void_p]),
     "pb_op_paged_attention_workspace": (ctypes.c_size_t, [ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p,
                                                           ctypes.c_int32]),
@@ -824,9 +824,9 @@ def paged_attention_workspace(n_seqs: int, n_heads: int, pool, width: int) -> in
 
 
 def op_paged_attention(dtype: int, q, pool, tables, lens, out, scale: float = 1.0, window: int = 0, workspace=None,
-                       stream=None):
+                       shared: bool = False, stream=None):
     """pb_op_paged_attention: q and out [sequences, heads, head_dim] (rows may be strided); scale 1 for a q that is
-    divided by sqrt(head_dim) already."""
+    divided by sqrt(head_dim) already; shared: rows next to each other share pages (beams)."""
     op = "op_paged_attention"
     c = kv_pool(pool)
     S, width, ld = _tables(op, tables)
@@ -835,7 +835,7 @@ def op_paged_attention(dtype: int, q, pool, tables, lens, out, scale: float = 1.
         raise PbError(PB_EINVAL, "%s: q and out must be [%d, heads, %d]" % (op, S, c.head_dim))
     _checked(op, stream, dtype, (pool, q, out), (("lens", lens, (S,)),), (tables, workspace))
     rc = lib().pb_op_paged_attention(dtype, q.data_ptr(), _heads(op, "q", q), ctypes.byref(c), tables.data_ptr(), width,
-                                     ld, lens.data_ptr(), S, shape[1], scale, window, out.data_ptr(),
+                                     ld, lens.data_ptr(), S, shape[1], scale, window, shared, out.data_ptr(),
                                      _heads(op, "out", out), _ptr(workspace), _nbytes(workspace), _stream(stream))
     if rc:
         check(rc)

@@ -48,6 +48,7 @@ struct PagedAttentionParams {
     int n_heads;
     float scale;
     int window;
+    bool shared;  // rows next to each other share pages
     void* ws; size_t ws_bytes;
 };
 size_t paged_attention_workspace(int n_seqs, int n_heads, int n_kv_heads, int hd, int width, int page_size);

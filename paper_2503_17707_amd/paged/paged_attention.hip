@@ -16,6 +16,9 @@
 //    faster for few blocks, 10% slower for many, which then hold fewer waves.)
 //    Values are read once and by whole lines, so they bypass what caches may keep
 //    (131071 tokens: 98.5 us against 107); a line of keys is read in two halves.
+//    Where rows share pages, as beams do, caches serve most reads and are used (4
+//    prompts of 1000 with 8 beams each, 32 heads of 64: 27.7 us against 32.4; the same
+//    rows on pages of their own: 61.4 against 54.5).
 //  - Sequences are cut into pieces, at most as long as a length chosen on the device
 //    from the call's lengths (which may change between replays of a recorded launch),
 //    so that about PIECES blocks of like work cover a ragged batch as well as one long
@@ -157,7 +160,7 @@ __device__ __forceinline__ int piece_length(int64_t tokens, int blocks_per_piece
 
 __device__ __forceinline__ int pieces_of(int n, int len_c) { return max(1, (n + len_c - 1) / len_c); }
 
-template <typename T, int HD, int NQ, int NW>
+template <typename T, int HD, int NQ, int NW, bool SHARED>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2)))
 void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
     typedef typename Mfma<T>::vec8 vec8;
@@ -180,7 +183,7 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
     const int group = p.n_heads / p.pool.n_kv_heads;
     const int hb = p.pool.n_kv_heads * cut.qb;
     // blocks that share keys and values run on one XCD, and its L2 holds them: every
-    // eighth block does (4 sequences of 30000, 71 heads on one: 39.5 us, side by side 44.3)
+    // eighth block does (4 sequences of 30000, 71 heads on one: 39.5 us; neighbouring blocks: 44.3)
     const int unit = blockIdx.x / (8 * cut.qb) * 8 + blockIdx.x % 8;  // (piece, key/value head)
     const int kvh = unit % p.pool.n_kv_heads, q0 = (int)(blockIdx.x / 8 % cut.qb) * 16 * NQ;
     const int item = unit / p.pool.n_kv_heads;
@@ -303,9 +306,11 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
                 for (int c = 0; c < CS; ++c) kr[i][c] = *(const u32x4*)(a + c * 32);
             }
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                vr[i] = __builtin_nontemporal_load(
-                    (const u32x4*)(token(min(k0 + i * RPI + lane / CPR, seg_end - 1)) + p.pool.v_offset + lane % CPR * 8));
+            for (int i = 0; i < NV; ++i) {
+                const u32x4* a = (const u32x4*)(token(min(k0 + i * RPI + lane / CPR, seg_end - 1)) + p.pool.v_offset +
+                                                lane % CPR * 8);
+                vr[i] = SHARED ? *a : __builtin_nontemporal_load(a);
+            }
         };
         int k0 = seg + wave * KT;
         if (k0 < seg_end) load(k0);
@@ -537,7 +542,7 @@ size_t cut_bytes(int rows, int64_t pieces, int n_heads, int hd) {
     return ((size_t)rows * 8 + 15) / 16 * 16 + (size_t)pieces * n_heads * (hd + 2) * 4;
 }
 
-template <typename T, int HD>
+template <typename T, int HD, bool SHARED>
 hipError_t launch(const PagedAttentionParams& p, hipStream_t s) {
     const int group = p.n_heads / p.pool.n_kv_heads;
     const int nq = group <= 16 ? 1 : 2;
@@ -563,11 +568,19 @@ hipError_t launch(const PagedAttentionParams& p, hipStream_t s) {
     // Few uncut blocks: eight waves each (8 sequences of 1000, 32 heads of 64: 14.1 us,
     // four 16.4); cut ones have little to share out.
     if (nq == 1 && !cut.on && items * hb < 512)
-        PB_LAUNCH((paged_attention_kernel<T, HD, 1, 8>), grid, dim3(512), 0, s, p, cut);
-    else if (nq == 1) PB_LAUNCH((paged_attention_kernel<T, HD, 1, 4>), grid, dim3(256), 0, s, p, cut);
-    else PB_LAUNCH((paged_attention_kernel<T, HD, 2, 4>), grid, dim3(256), 0, s, p, cut);
+        PB_LAUNCH((paged_attention_kernel<T, HD, 1, 8, SHARED>), grid, dim3(512), 0, s, p, cut);
+    else if (nq == 1) PB_LAUNCH((paged_attention_kernel<T, HD, 1, 4, SHARED>), grid, dim3(256), 0, s, p, cut);
+    else PB_LAUNCH((paged_attention_kernel<T, HD, 2, 4, SHARED>), grid, dim3(256), 0, s, p, cut);
     if (cut.on) launch_join<T, HD>(p, cut, s);
     return hipGetLastError();
+}
+
+template <typename T, int HD>
+hipError_t launch_shared(const PagedAttentionParams& p, hipStream_t s) {
+    // more than 32 heads to a key/value head: several blocks read the same values too
+    // (4 sequences of 30000, 71 heads on one: 35.4 us against 38.7)
+    const bool shared = p.shared || p.n_heads / p.pool.n_kv_heads > 32;
+    return shared ? launch<T, HD, true>(p, s) : launch<T, HD, false>(p, s);
 }
 
 }  // namespace
@@ -580,8 +593,8 @@ size_t paged_attention_workspace(int n_seqs, int n_heads, int n_kv_heads, int hd
 
 hipError_t launch_paged_attention(int dtype, const PagedAttentionParams& p, hipStream_t s) {
     if (p.tab.rows <= 0) return hipSuccess;
-    if (p.pool.head_dim == 64) return dtype == 1 ? launch<_Float16, 64>(p, s) : launch<__bf16, 64>(p, s);
-    return dtype == 1 ? launch<_Float16, 128>(p, s) : launch<__bf16, 128>(p, s);
+    if (p.pool.head_dim == 64) return dtype == 1 ? launch_shared<_Float16, 64>(p, s) : launch_shared<__bf16, 64>(p, s);
+    return dtype == 1 ? launch_shared<_Float16, 128>(p, s) : launch_shared<__bf16, 128>(p, s);
 }
 
 }  // namespace pb

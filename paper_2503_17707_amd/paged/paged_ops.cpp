@@ -116,8 +116,8 @@ extern "C" size_t pb_op_paged_attention_workspace(int32_t n_seqs, int32_t n_head
 
 extern "C" int pb_op_paged_attention(int32_t dtype, const void* q, int64_t ld_q, const pb_kv_pool* pool,
                                      const int32_t* tables, int32_t width, int64_t ld_tables, const int32_t* lens,
-                                     int32_t n_seqs, int32_t n_heads, float scale, int32_t window, void* out,
-                                     int64_t ld_out, void* workspace, size_t workspace_bytes, void* stream) {
+                                     int32_t n_seqs, int32_t n_heads, float scale, int32_t window, int32_t shared,
+                                     void* out, int64_t ld_out, void* workspace, size_t workspace_bytes, void* stream) {
     const char* op = "pb_op_paged_attention";
     pb::PagedAttentionParams p{};
     if (int rc = make_pool(op, dtype, pool, &p.pool)) return rc;
@@ -135,7 +135,7 @@ extern "C" int pb_op_paged_attention(int32_t dtype, const void* q, int64_t ld_q,
     if (workspace && !aligned(workspace, 16)) return refuse("%s: workspace must be 16-byte aligned", op);
     p.q = (const uint16_t*)q; p.ld_q = ld_q; p.out = (uint16_t*)out; p.ld_out = ld_out;
     p.tab = {tables, ld_tables, width, n_seqs};
-    p.lens = lens; p.n_heads = n_heads; p.scale = scale; p.window = window;
+    p.lens = lens; p.n_heads = n_heads; p.scale = scale; p.window = window; p.shared = shared != 0;
     p.ws = workspace; p.ws_bytes = workspace ? workspace_bytes : 0;
     return launched(op, pb::launch_paged_attention(dtype, p, (hipStream_t)stream));
 }

@@ -52,7 +52,7 @@ class Beams:
             q, k, v = self.split(l)
             pb.op_kv_append(self.code, k, v, self.pool[l], b["tables"], b["start"], b["lens"])
             pb.op_paged_attention(self.code, q, self.pool[l], b["tables"], b["lens"], self.out[l], scale=self.hd ** -0.5,
-                                  workspace=self.ws)
+                                  workspace=self.ws, shared=True)
         pb.op_beam_select(self.logits, self.scores, self.alive, self.scores, self.tokens, self.parents, self.alive, eos=eos,
                           pad=0, workspace=self.ws)
 
@@ -241,6 +241,6 @@ def test_two_runs_give_the_same_bits():
     for _ in range(3):
         out = torch.empty_like(q)
         ws.fill_(255)
-        pb.op_paged_attention(1, q, pool, tables, dev(lens), out, workspace=ws)
+        pb.op_paged_attention(1, q, pool, tables, dev(lens), out, workspace=ws, shared=len(outs) == 2)
         outs.append(out)
     assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])

@@ -28,7 +28,7 @@ def _append(pb, pool, dtype=1, k=P, ld_k=256, v=P, ld_v=256, n=8, tables=P, widt
 def _attend(pb, pool, dtype=0, q=P, ld_q=512, tables=P, width=4, ld=4, lens=P, S=2, H=8, scale=1.0, window=0, out=P,
             ld_out=512, ws=P, ws_bytes=64):
     return pb.lib().pb_op_paged_attention(dtype, q, ld_q, ctypes.byref(pool) if pool else None, tables, width, ld, lens, S,
-                                          H, scale, window, out, ld_out, ws, ws_bytes, None)
+                                          H, scale, window, 0, out, ld_out, ws, ws_bytes, None)
 
 
 def _select(pb, logits=P, ld=100, scores=P, alive=P, B=2, W=3, V=100, eos=2, pad=1, o=(P, P, P, P), ws=P, ws_bytes=1 << 20):
