@@ -5,7 +5,8 @@
  * launcher splits) on caller-provided device buffers, on the given stream,
  * asynchronously.  They exist to test every kernel against the CPU oracle's
  * component functions and to time kernels in isolation; the model API in
- * pipeboost.h is the product path.  All pointers are device pointers, all
+ * pipeboost.h is the product path.  The last section is for programs that run
+ * decode steps of their own over a cache of pages.  All pointers are device pointers, all
  * matrices row-major with the reduction dimension contiguous; "dt" is
  * bfloat16 (dtype 0) or IEEE binary16 (dtype 1).  Every call returns a
  * pb_status (PB_EINVAL for unsupported shapes, PB_EHIP for launch failures,
