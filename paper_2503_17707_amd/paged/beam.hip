@@ -3,15 +3,21 @@
 //
 // log softmax(l)[v] = l[v] - m - log sum exp(l - m): a row's order is its logits'
 // order, so a row offers its W largest logits and its log sum, and only those are
-// compared across rows.  What bounds it is reading the logits once; the two
-// launches then cost their latency:
+// compared across rows.  What bounds it is reading the logits once, if the
+// arithmetic on them (four instructions a logit, one of them exp2 at a quarter of
+// the rate) hides behind it; the two launches then cost their latency:
 //
 //  chunks  One block per (row, chunk of 256 R logits), the chunk in registers.  The
 //          W-th largest of the 256 threads' maxima is a value that at least W
 //          logits reach and that only W threads (and ties) hold any above: found by
 //          bisection on the bits, with ballots, it leaves a handful of candidates,
 //          each placed by counting those before it.  The chunk's maximum and sum of
-//          exponentials come from the same registers.
+//          exponentials come from the same registers, as the logits arrive:
+//          2^(x log2 e - c) with c the rounded maximum in the base of two, one
+//          multiply-add and exact in c.  (256 rows of 50272 logits take 11.6 us, 128 of
+//          128256 15.1; loading alone takes 8.4 and 10.3, and with the sum after the
+//          selection and every logit cleaned first it was 14.2 and 18.5: the vector
+//          units were the bound.)
 //  join    One block per prompt over the sorted lists of its rows' chunks: the same
 //          idea, the W-th largest list head keeps all but W lists (and ties) out.
 //
@@ -27,6 +33,7 @@ namespace pb {
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
+constexpr float HUGE_LOGIT = 4194304.f;  // 2^22: below it a rounded maximum is exact, in base two also
 constexpr int NT = 256;       // threads of a chunk's block
 constexpr int MOST = 1024;    // candidates of a chunk: 32 threads' 32 logits
 constexpr int LISTS = 4096;   // lists of a prompt: 32 rows of 2^20 logits in 128 chunks
@@ -47,14 +54,13 @@ __device__ inline float float_of(uint32_t key) { return __uint_as_float(key & 0x
 // A logit and its token as one key: of equal logits the lower token is the larger key.
 __device__ inline uint64_t entry_of(float x, int v) { return (uint64_t)key_of(x) << 32 | (uint32_t)~v; }
 
-// How many of n keys in LDS are larger, counted by the G lanes that share `mine`.
-template <int G>
+// How many of n keys in LDS are larger, counted by the four lanes that share `mine`.
 __device__ inline int rank_of(const uint64_t* keys, int n, uint64_t mine) {
     int rank = 0;
 #pragma unroll 4
-    for (int j = threadIdx.x % G; j < n; j += G) rank += keys[j] > mine;
-    for (int o = 1; o < G; o <<= 1) rank += __shfl_xor(rank, o, 64);
-    return rank;
+    for (int j = threadIdx.x % 4; j < n; j += 4) rank += keys[j] > mine;
+    rank += __builtin_amdgcn_mov_dpp(rank, 0xB1, 0xf, 0xf, false);         // quad_perm 1 0 3 2
+    return rank + __builtin_amdgcn_mov_dpp(rank, 0x4E, 0xf, 0xf, false);  // quad_perm 2 3 0 1
 }
 
 struct ChunkBest {
@@ -85,6 +91,37 @@ __device__ inline float wave_max_dpp(float v) {
     v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
     const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// Sum over the wave, in every lane, the same way.
+__device__ inline float wave_sum_dpp(float v) {
+    auto step = [&](int x) { v += __int_as_float(x); };
+    step(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0xB1, 0xf, 0xf, false));
+    step(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x4E, 0xf, 0xf, false));
+    step(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x141, 0xf, 0xf, false));
+    step(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x140, 0xf, 0xf, false));
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// Maximum of G values.
+template <int G>
+__device__ inline float max_of(const float* x) {
+    // v_max3 itself: fmaxf would first quiet each operand.  With a NaN among them the
+    // result is any of them.
+    float v = x[0];
+#pragma unroll
+    for (int i = 1; i < G; i += 2) asm("v_max3_f32 %0, %0, %1, %2" : "+v"(v) : "v"(x[i]), "v"(x[i + 1 < G ? i + 1 : i]));
+    return v;
+}
+
+// Zero, which the compiler cannot know to be the same in all lanes.
+__device__ inline int zero_of_lane() {
+    int z = 0;
+    asm volatile("" : "+v"(z));
+    return z;
 }
 
 // A value t that at least `want` of `keys` keys reach, and at most `most` of them
@@ -125,51 +162,88 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(5))) void be
     __shared__ float ssum[NT / 64];
     __shared__ uint64_t cand[MOST];
     __shared__ int cn, eq[NT / 64];
+    __shared__ uint32_t reached;
+    constexpr int G = R < 8 ? R : 8;
     const int row = blockIdx.x / chunks, chunk = blockIdx.x % chunks;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int W = p.W, v0 = chunk * NT * R + tid;
     const ChunkBest out = chunk_best(p.ws, (size_t)p.B * W * chunks, W);
     const size_t list = (size_t)row * chunks + chunk;
-    const float* l = p.logits + row * p.ld;
-    float x[R], mx = -INFINITY;
+    const float* l = p.logits + row * p.ld + chunk * NT * R;
+    const int left = p.V - chunk * NT * R;
+    float x[R], top[R / G];  // the logits, the largest of every G
+    if (left >= NT * R) {
 #pragma unroll
-    for (int i = 0; i < R; ++i) x[i] = l[min(v0 + i * NT, p.V - 1)];
+        for (int i = 0; i < R; ++i) x[i] = l[i * NT + (unsigned)tid];
+    } else {
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-        x[i] = clean(x[i]);
-        if ((chunk + 1) * NT * R > p.V && v0 + i * NT >= p.V) x[i] = -INFINITY;
-        mx = fmaxf(mx, x[i]);
+        for (int i = 0; i < R; ++i) x[i] = l[min(i * NT + tid, left - 1)];
+#pragma unroll
+        for (int i = 0; i < R; ++i) x[i] = i * NT + tid < left ? x[i] : -INFINITY;
     }
+    // Sum of 2^(x log2 e - ref), ref a whole number near the largest so far.  NaN or
+    // +inf make it NaN.
+    float ref = -2 * HUGE_LOGIT, sum = 0.f;
+#pragma unroll
+    for (int g = 0; g < R / G; ++g) {
+        top[g] = max_of<G>(x + g * G);
+        const float next = fmaxf(ref, __builtin_rintf(top[g] * LOG2E));
+        sum *= __builtin_amdgcn_exp2f(ref - next);
+#pragma unroll
+        for (int i = 0; i < G; ++i) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(x[g * G + i], LOG2E, -next));
+        ref = next;
+    }
+    // (the sum is used before the barrier, so it is formed while loads are under way)
+    const bool odd = __any(!(sum < INFINITY));
+    if (odd) {
+        asm volatile("");  // a branch: rarely taken
+#pragma unroll
+        for (int i = 0; i < R; ++i) x[i] = clean(x[i]);
+#pragma unroll
+        for (int g = 0; g < R / G; ++g) top[g] = max_of<G>(x + g * G);
+    }
+    float mx = top[0];
+#pragma unroll
+    for (int g = 1; g < R / G; ++g) mx = fmaxf(mx, top[g]);
     smax[tid] = mx;
     if (tid == 0) cn = 0;
     __syncthreads();
     // the W-th largest of the maxima of every four threads is a little lower than
-    // that of all, and found with one ballot a step
+    // that of all, and found with one ballot a step, by one wave
     const f32x4 four = *(const f32x4*)&smax[4 * lane];
     const float of4 = fmaxf(fmaxf(four[0], four[1]), fmaxf(four[2], four[3]));
     const float m = wave_max_dpp(of4);
-    const uint32_t key4 = key_of(of4);
-    uint32_t t = reach([&](uint32_t least) { return __popcll(__ballot(key4 >= least)); }, 64, key_of(m), W, W);
-    t = max(t, KEY_NONE + 1);
-    float sum = 0.f;
-    if (m > -INFINITY) {
-#pragma unroll
-        for (int i = 0; i < R; ++i) sum += __builtin_amdgcn_exp2f((x[i] - m) * LOG2E);
-        const float least = float_of(t);
-        if (mx >= least) {
-            int mine = 0;
-#pragma unroll
-            for (int i = 0; i < R; ++i) mine += x[i] >= least;
-            int at = atomicAdd(&cn, mine);
-#pragma unroll
-            for (int i = 0; i < R; ++i)
-                if (x[i] >= least) {
-                    if (at < MOST) cand[at] = entry_of(x[i], v0 + i * NT);
-                    ++at;
-                }
-        }
+    if (wave == (blockIdx.x & 3)) {
+        const uint32_t key4 = key_of(of4);
+        const uint32_t r = reach([&](uint32_t least) { return __popcll(__ballot(key4 >= least)); }, 64, key_of(m), W, W);
+        if (lane == 0) reached = r;
     }
-    sum = wave_sum(sum);
+    __syncthreads();
+    uint32_t t = max(reached, KEY_NONE + 1);
+    if (m > -INFINITY) {
+        if (odd || !(fabsf(m) < HUGE_LOGIT)) {
+            sum = 0.f;  // logits cleaned since, or too large for a whole number between them
+#pragma unroll
+            for (int i = 0; i < R; ++i) sum += __builtin_amdgcn_exp2f((x[i] - m) * LOG2E);
+        } else {
+            sum *= __builtin_amdgcn_exp2f(__builtin_fmaf(-m, LOG2E, ref));
+        }
+        const float least = float_of(t);
+        // one counter, at an address that may differ between lanes: a single LDS add
+        int* const count = &cn + zero_of_lane();
+#pragma unroll
+        for (int g = 0; g < R / G; ++g)
+            if (top[g] >= least)
+#pragma unroll
+                for (int i = g * G; i < g * G + G; ++i)
+                    if (x[i] >= least) {
+                        const int at = atomicAdd(count, 1);
+                        if (at < MOST) cand[at] = entry_of(x[i], v0 + i * NT);
+                    }
+    } else {
+        sum = 0.f;
+    }
+    sum = wave_sum_dpp(sum);
     if (lane == 0) ssum[wave] = sum;
     __syncthreads();
     int n = cn;
@@ -218,10 +292,10 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(5))) void be
         n += min(taken, W);
     }
     __syncthreads();
-    for (int c0 = 0; c0 < n; c0 += NT / 4) {
-        const int c = c0 + tid / 4;
+    for (int c0 = wave * 16; c0 < n; c0 += NT / 4) {
+        const int c = c0 + lane / 4;
         const uint64_t e = cand[min(c, n - 1)];
-        const int rank = rank_of<4>(cand, n, e);
+        const int rank = rank_of(cand, n, e);
         if (c < n && tid % 4 == 0 && rank < W) {
             out.val[list * W + rank] = float_of((uint32_t)(e >> 32));
             out.idx[list * W + rank] = ~(uint32_t)e;
@@ -382,14 +456,12 @@ __global__ __launch_bounds__(JT) void beam_join_kernel(BeamParams p, int chunks)
     }
 }
 
-#ifndef PB_BEAM_BLOCKS
-#define PB_BEAM_BLOCKS 512
-#endif
-// Logits per thread: the most (fewest lists to join) that leave PB_BEAM_BLOCKS blocks,
+constexpr int BLOCKS = 512;
+// Logits per thread: the most (fewest lists to join) that leave BLOCKS blocks,
 // and enough that a row has at most 64 lists (128 of 2^20 logits).
 int logits_per_thread(int64_t rows, int V) {
     int r = 32;
-    while (r > 4 && rows * ((V + NT * r - 1) / (NT * r)) < PB_BEAM_BLOCKS) r /= 2;
+    while (r > 4 && rows * ((V + NT * r - 1) / (NT * r)) < BLOCKS) r /= 2;
     while (r < 32 && (V + NT * r - 1) / (NT * r) > 64) r *= 2;
     return r;
 }

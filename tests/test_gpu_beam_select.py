@@ -147,6 +147,27 @@ def test_large_logits_and_scores():
     _run(logits + 1e4, scores * 1000, alive)
 
 
+@pytest.mark.parametrize("far", [2.0 ** 21, 3.5e6, 2.0 ** 22, 5e6, 2.0 ** 23, 3e7])
+@pytest.mark.parametrize("V", [37, 1024, 40000])
+def test_logits_of_millions(far, V):
+    """The whole number that exponents are taken relative to: at the end of its range, on
+    both sides, in every logit or beside masked and ordinary ones."""
+    rs = np.random.RandomState(11)
+    for sign in (-1, 1):
+        logits, scores, alive = _random(rs, 2, 4, V)
+        alive[:] = 1
+        near = np.isfinite(logits)
+        logits[near] = sign * far
+        logits[near] += np.float32(0.5) * rs.randint(-8, 9, near.sum()).astype(np.float32)
+        logits[1, rs.rand(V) < 0.9] = np.finfo(np.float32).min
+        logits[2, rs.rand(V) < 0.5] = -8e6
+        logits[3, : V // 2] = rs.randn(V // 2)
+        logits[4, V // 2:] = np.nan
+        logits[5, V // 3] = INF
+        logits[6, V // 3:] = -INF
+        _run(logits, scores, alive)
+
+
 def test_masks_of_the_lowest_float():
     """Tokens masked with the type's lowest value are the last candidates, not none."""
     rs = np.random.RandomState(10)
