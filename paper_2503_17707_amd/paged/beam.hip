@@ -20,8 +20,10 @@
 //          units were the bound.)
 //  join    One block per prompt over the sorted lists of its rows' chunks: the same
 //          idea, the W-th largest list head keeps all but W lists (and ties) out.
+//          One block's chain of dependent steps: 5.0 us for 8 x 7 lists, 6.1 for 32 x 16.
 //
-// Sums of exponentials run in fp32 within a chunk and are joined in 64 bits; a
+// Sums of exponentials run in fp32 within a chunk and are joined in 64 bits, their
+// weights and the logarithm's fraction to fp32, as near as the sums are; a
 // candidate's score, score + ((l - m) - log sum), is formed and compared in 64 bits,
 // because candidates of different rows can lie closer than fp32 tells apart at
 // scores of tens.
@@ -54,13 +56,47 @@ __device__ inline float float_of(uint32_t key) { return __uint_as_float(key & 0x
 // A logit and its token as one key: of equal logits the lower token is the larger key.
 __device__ inline uint64_t entry_of(float x, int v) { return (uint64_t)key_of(x) << 32 | (uint32_t)~v; }
 
+template <int N> struct Words { uint32_t w[N]; };
+
+// The value of the lane that the DPP control names.
+template <int CONTROL, typename T>
+__device__ inline T moved(T v) {
+    auto b = __builtin_bit_cast(Words<sizeof(T) / 4>, v);
+    for (uint32_t& w : b.w) w = (uint32_t)__builtin_amdgcn_mov_dpp((int)w, CONTROL, 0xf, 0xf, false);
+    return __builtin_bit_cast(T, b);
+}
+
+// op over groups of g lanes (4 to 64), in every lane, without LDS: quads, rows of 16,
+// then the rows.
+template <typename T, typename Op>
+__device__ inline T over_lanes(T v, int g, Op op) {
+    using B = Words<sizeof(T) / 4>;
+    v = op(v, moved<0xB1>(v));                // quad_perm 1 0 3 2
+    v = op(v, moved<0x4E>(v));                // quad_perm 2 3 0 1
+    if (g >= 8) v = op(v, moved<0x141>(v));   // row_half_mirror
+    if (g >= 16) v = op(v, moved<0x140>(v));  // row_mirror
+    auto halves = [&](auto swap) {
+        B a = __builtin_bit_cast(B, v), b = a;
+        for (int i = 0; i < (int)(sizeof(T) / 4); ++i) {
+            const auto s = swap(a.w[i]);
+            a.w[i] = s[0];
+            b.w[i] = s[1];
+        }
+        v = op(__builtin_bit_cast(T, a), __builtin_bit_cast(T, b));
+    };
+    if (g >= 32) halves([](uint32_t w) { return __builtin_amdgcn_permlane16_swap(w, w, false, false); });
+    if (g >= 64) halves([](uint32_t w) { return __builtin_amdgcn_permlane32_swap(w, w, false, false); });
+    return v;
+}
+constexpr auto add = [](auto a, auto b) { return a + b; };
+constexpr auto larger = [](float a, float b) { return fmaxf(a, b); };
+
 // How many of n keys in LDS are larger, counted by the four lanes that share `mine`.
 __device__ inline int rank_of(const uint64_t* keys, int n, uint64_t mine) {
     int rank = 0;
 #pragma unroll 4
     for (int j = threadIdx.x % 4; j < n; j += 4) rank += keys[j] > mine;
-    rank += __builtin_amdgcn_mov_dpp(rank, 0xB1, 0xf, 0xf, false);         // quad_perm 1 0 3 2
-    return rank + __builtin_amdgcn_mov_dpp(rank, 0x4E, 0xf, 0xf, false);  // quad_perm 2 3 0 1
+    return over_lanes(rank, 4, add);
 }
 
 struct ChunkBest {
@@ -79,32 +115,6 @@ __host__ __device__ inline ChunkBest chunk_best(void* ws, size_t lists, int W) {
 
 // (a, i) comes before (b, j)
 template <typename K> __device__ inline bool before(K a, int i, K b, int j) { return a > b || (a == b && i < j); }
-
-// Maximum over the wave, in every lane, without LDS: quads, rows of 16, then the rows.
-__device__ inline float wave_max_dpp(float v) {
-    auto step = [&](int x) { v = fmaxf(v, __int_as_float(x)); };
-    step(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0xB1, 0xf, 0xf, false));   // quad_perm 1 0 3 2
-    step(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x4E, 0xf, 0xf, false));   // quad_perm 2 3 0 1
-    step(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x141, 0xf, 0xf, false));  // row_half_mirror
-    step(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x140, 0xf, 0xf, false));  // row_mirror
-    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-
-// Sum over the wave, in every lane, the same way.
-__device__ inline float wave_sum_dpp(float v) {
-    auto step = [&](int x) { v += __int_as_float(x); };
-    step(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0xB1, 0xf, 0xf, false));
-    step(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x4E, 0xf, 0xf, false));
-    step(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x141, 0xf, 0xf, false));
-    step(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x140, 0xf, 0xf, false));
-    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
-}
 
 // Maximum of G values.
 template <int G>
@@ -127,11 +137,12 @@ __device__ inline int zero_of_lane() {
 // A value t that at least `want` of `keys` keys reach, and at most `most` of them
 // unless more are equal (then t is the want-th largest itself; 0 if there are no
 // `want` keys).  hi: the largest key; count(t): how many reach t, the same in every
-// lane.  The want-th largest of a few hundred
-// shares the largest one's leading bits: the common part is found first, upwards
-// from 14 of them, then bits are added until few enough keys are left.
+// lane.  The want-th largest of a few hundred shares the largest one's leading bits:
+// the common part is found first, upwards from 14 of them, then bits are added until
+// few enough keys are left.  (Two bits a step, with three counts, take 5% longer.)
 template <typename Count>
 __device__ inline uint32_t reach(Count count, int keys, uint32_t hi, int want, int most) {
+    hi = __builtin_amdgcn_readfirstlane(hi);  // (all steps on the scalar unit)
     int b = 18, n = 0;
     uint32_t t = 0;
     for (; b < 32; b += 2) {
@@ -212,7 +223,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(5))) void be
     // that of all, and found with one ballot a step, by one wave
     const f32x4 four = *(const f32x4*)&smax[4 * lane];
     const float of4 = fmaxf(fmaxf(four[0], four[1]), fmaxf(four[2], four[3]));
-    const float m = wave_max_dpp(of4);
+    const float m = over_lanes(of4, 64, larger);
     if (wave == (blockIdx.x & 3)) {
         const uint32_t key4 = key_of(of4);
         const uint32_t r = reach([&](uint32_t least) { return __popcll(__ballot(key4 >= least)); }, 64, key_of(m), W, W);
@@ -243,7 +254,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(5))) void be
     } else {
         sum = 0.f;
     }
-    sum = wave_sum_dpp(sum);
+    sum = over_lanes(sum, 64, add);
     if (lane == 0) ssum[wave] = sum;
     __syncthreads();
     int n = cn;
@@ -308,10 +319,21 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(5))) void be
     if (tid == 0) out.ms[list] = make_float2(m, (ssum[0] + ssum[1]) + (ssum[2] + ssum[3]));
 }
 
+static_assert(BEAM_MAX_VOCAB <= 1 << 20 && BEAM_MAX_WIDTH <= 1 << 11, "a place's 20 and 11 bits");
+constexpr int HELD = 8;  // heads that a lane holds in registers: 512 lists, more are read again
 constexpr int TIED = 64; // lists whose heads may pass the bisection: the W and ties
 
+// log of 1 <= x < 2^21: the exponent's part in 64 bits, the rest within 2^-23.
+__device__ inline double log_of(double x) {
+    const float v = (float)x;
+    const uint32_t b = __float_as_uint(v);
+    const int e = (int)((b + 0x00400000u) >> 23) - 127;  // v / 2^e in [3/4, 3/2)
+    const float f = __uint_as_float(b - ((uint32_t)e << 23));
+    return e * 0.6931471805599453 + (double)(__builtin_amdgcn_logf(f) * 0.6931471805599453f);
+}
+
 template <int JT>
-__global__ __launch_bounds__(JT) void beam_join_kernel(BeamParams p, int chunks) {
+__global__ __launch_bounds__(JT) void beam_join_kernel(BeamParams p, int chunks, FastDiv by_chunks, FastDiv by_width) {
     __shared__ double lse[BEAM_MAX_WIDTH];
     __shared__ float row_max[BEAM_MAX_WIDTH], own[BEAM_MAX_WIDTH];
     __shared__ uint32_t key[LISTS], threshold;
@@ -338,26 +360,26 @@ __global__ __launch_bounds__(JT) void beam_join_kernel(BeamParams p, int chunks)
         const float2 mine = tid % g < chunks ? ms[tid % g] : make_float2(-INFINITY, 0.f);
         float m = mine.x;
         for (int c = tid % g + g; c < chunks; c += g) m = fmaxf(m, ms[c].x);
-        for (int o = g / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-        auto term = [&](float2 v) { return v.x == -INFINITY ? 0.0 : (double)v.y * exp((double)v.x - (double)m); };
+        m = over_lanes(m, g, larger);
+        auto term = [&](float2 v) { return v.x == -INFINITY ? 0.0 : (double)v.y * __builtin_amdgcn_exp2f((v.x - m) * LOG2E); };
         double sum = term(mine);
         for (int c = tid % g + g; c < chunks; c += g) sum += term(ms[c]);
-        for (int o = g / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+        sum = over_lanes(sum, g, add);
         if (tid % g == 0 && w < W) {
             row_max[w] = m;
-            lse[w] = log(sum);
+            lse[w] = log_of(sum);
         }
     }
     __syncthreads();
-    // score of a list's k-th entry and its place w V + v; an ended hypothesis stands
+    // score of a list's k-th entry and its place (w, v); an ended hypothesis stands
     // at the head of its first list, as token pad
     auto score_as = [&](int i, int k, int& place, float v, int v_idx) -> double {
-        const int w = i / chunks;
-        place = w * p.V + p.pad;
+        const int w = by_chunks.quot(i);
+        place = w << 20 | p.pad;
         if (!(own[w] - own[w] == 0.f)) return -INFINITY;
-        if (live[w] == 0) return i % chunks == 0 && k == 0 ? (double)own[w] : -INFINITY;
+        if (live[w] == 0) return i == w * chunks && k == 0 ? (double)own[w] : -INFINITY;
         if (v == -INFINITY) return -INFINITY;
-        place = w * p.V + v_idx;
+        place = w << 20 | v_idx;
         return (double)own[w] + (((double)v - (double)row_max[w]) - lse[w]);
     };
     auto score_of = [&](int i, int k, int& place) {
@@ -371,13 +393,20 @@ __global__ __launch_bounds__(JT) void beam_join_kernel(BeamParams p, int chunks)
     // the W-th largest head, about, to fp32 (rounding keeps the order)
     if (wave == 0) {
         // from the lanes' maxima of every 64th head: at least W heads reach it
-        uint32_t top = 0;
-        for (int i = lane; i < lists; i += 64) top = max(top, key[i]);
-        const uint32_t hi = key_of(wave_max_dpp(top ? float_of(top) : -INFINITY));
+        uint32_t held[HELD], top = 0;
+#pragma unroll
+        for (int j = 0; j < HELD; ++j) {
+            held[j] = j * 64 + lane < lists ? key[j * 64 + lane] : 0;
+            top = max(top, held[j]);
+        }
+        for (int i = HELD * 64 + lane; i < lists; i += 64) top = max(top, key[i]);
+        const uint32_t hi = key_of(over_lanes(top ? float_of(top) : -INFINITY, 64, larger));
         uint32_t v = reach([&](uint32_t least) { return __popcll(__ballot(top >= least)); }, 64, hi, W, W);
         auto count = [&](uint32_t least) {
             int n = 0;
-            for (int i = 0; i < lists; i += 64) n += __popcll(__ballot(i + lane < lists && key[i + lane] >= least));
+#pragma unroll
+            for (int j = 0; j < HELD; ++j) n += __popcll(__ballot(held[j] >= least));
+            for (int i = HELD * 64; i < lists; i += 64) n += __popcll(__ballot(i + lane < lists && key[i + lane] >= least));
             return n;
         };
         if (lists > 64 && count(v) > TIED) v = reach(count, lists, hi, W, TIED);
@@ -414,7 +443,8 @@ __global__ __launch_bounds__(JT) void beam_join_kernel(BeamParams p, int chunks)
     // their entries that reach the W-th head too
     for (int i = tid; i < n * W; i += JT) {
         int place;
-        const double s = score_of(pick[i / W], i % W, place);
+        const int nth = by_width.quot(i);
+        const double s = score_of(pick[nth], i - nth * W, place);
         if (s > -INFINITY && key_of((float)s) >= t) {
             const int at = atomicAdd(&cn, 1);
             sc[at] = s;
@@ -434,14 +464,13 @@ __global__ __launch_bounds__(JT) void beam_join_kernel(BeamParams p, int chunks)
             rank += sc[j] > s;
             same += sc[j] == s;
         }
-        for (int o = 1; o < G; o <<= 1) {
-            rank += __shfl_xor(rank, o, 64);
-            same += __shfl_xor(same, o, 64);
-        }
+        const int both = over_lanes(rank | same << 16, G, add);  // (at most 2048 each)
+        rank = both & 0xffff;
+        same = both >> 16;
         if (same > 1)  // the lowest place first
             for (int j = 0; j < n; ++j) rank += sc[j] == s && id[j] < id[c];
         if (rank >= W || c0 + tid / G >= n || tid % G) continue;
-        const int o = b * W + rank, w = id[c] / p.V, token = id[c] - w * p.V;
+        const int o = b * W + rank, w = id[c] >> 20, token = id[c] & 0xfffff;
         p.out_scores[o] = (float)sc[c];
         p.out_tokens[o] = token;
         p.out_parents[o] = b * W + w;
@@ -482,8 +511,9 @@ hipError_t launch_beam_select(const BeamParams& p, hipStream_t s) {
     else if (r == 16) PB_LAUNCH(beam_chunks_kernel<16>, grid, dim3(NT), 0, s, p, chunks);
     else if (r == 8) PB_LAUNCH(beam_chunks_kernel<8>, grid, dim3(NT), 0, s, p, chunks);
     else PB_LAUNCH(beam_chunks_kernel<4>, grid, dim3(NT), 0, s, p, chunks);
-    if (p.W * chunks <= 256) PB_LAUNCH(beam_join_kernel<256>, dim3(p.B), dim3(256), 0, s, p, chunks);
-    else PB_LAUNCH(beam_join_kernel<1024>, dim3(p.B), dim3(1024), 0, s, p, chunks);
+    const FastDiv by_chunks(chunks), by_width(p.W);
+    if (p.W * chunks <= 256) PB_LAUNCH(beam_join_kernel<256>, dim3(p.B), dim3(256), 0, s, p, chunks, by_chunks, by_width);
+    else PB_LAUNCH(beam_join_kernel<1024>, dim3(p.B), dim3(1024), 0, s, p, chunks, by_chunks, by_width);
     return hipGetLastError();
 }
 
