@@ -32,9 +32,10 @@ def _run(logits, scores, alive, eos=2, pad=1, pitch=0, in_place=False):
     for name, got, ref in zip(("tokens", "parents", "alive"), out[1:], want[1:]):
         assert np.array_equal(got.cpu().numpy(), ref), (name, got.cpu().numpy(), ref)
     got = out[0].double().cpu().numpy()
-    # fp32 sums of positive terms, each within (|l - m| log2 e + 2) 2^-24 of its
-    # exponential where l - m and its product are rounded; terms of l - m < -40 weigh
-    # under 2^-57 each: the log sum is off by less than 64 2^-24 + V 2^-57, and the
+    # fp32 sums of positive terms, each within (|l - m| log2 e + 4) 2^-24 of its
+    # exponential where exponents, their products and the chunks' weights are rounded;
+    # terms of l - m < -40 weigh under 2^-57 each; the logarithm's fraction is off by
+    # up to 2 2^-24: the log sum is off by less than 64 2^-24 + V 2^-57, and the
     # sums of up to V / 64 terms per thread by at most another V / 64 2^-24 (V 2^-24 for
     # the shortest blocks); then one rounding of the score
     tol = (64 + min(V, 4096)) * 2.0 ** -24 + np.abs(want[0]) * 2.0 ** -24
