@@ -321,7 +321,11 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(5))) void be
 
 static_assert(BEAM_MAX_VOCAB <= 1 << 20 && BEAM_MAX_WIDTH <= 1 << 11, "a place's 20 and 11 bits");
 constexpr int HELD = 8;  // heads that a lane holds in registers: 512 lists, more are read again
-constexpr int TIED = 64; // lists whose heads may pass the bisection: the W and ties
+constexpr int TIED = 64;  // lists whose heads may pass the bisection: the W and ties
+// More entries than MANY go through a bisection of their own before they are placed, down
+// to FEW (20 prompts of 32 beams and 6245 logits, 32 lists each: the call 23 us, 112 without
+// it; 10 of 12 beams and 954 logits, some 140 entries: 11.4, with it 14.7).
+constexpr int FEW = 128, MANY = 256;
 
 // log of 1 <= x < 2^21: the exponent's part in 64 bits, the rest within 2^-23.
 __device__ inline double log_of(double x) {
@@ -340,6 +344,8 @@ __global__ __launch_bounds__(JT) void beam_join_kernel(BeamParams p, int chunks,
     __shared__ int live[BEAM_MAX_WIDTH], pick[TIED], picks;
     __shared__ double sc[TIED * BEAM_MAX_WIDTH];
     __shared__ int id[TIED * BEAM_MAX_WIDTH], cn;
+    __shared__ double few_sc[FEW];
+    __shared__ int few_id[FEW];
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, W = p.W;
     const int lists = W * chunks;
     const ChunkBest in = chunk_best(p.ws, (size_t)p.B * lists, W);
@@ -453,25 +459,68 @@ __global__ __launch_bounds__(JT) void beam_join_kernel(BeamParams p, int chunks,
     }
     __syncthreads();
     n = cn;
+    const double* score = sc;
+    const int* place = id;
+    if (n > MANY) {
+        // Few lists, so most of their entries reach the W-th head: the same once more over
+        // all entries (unless it leaves more, which are equal then).
+        if (wave == 0) {
+            constexpr int E = TIED * BEAM_MAX_WIDTH / 64;
+            uint32_t held[E], top = 0;
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                held[j] = 0;
+                if (j * 64 < n) held[j] = j * 64 + lane < n ? key_of((float)sc[min(j * 64 + lane, n - 1)]) : 0;
+                top = max(top, held[j]);
+            }
+            const uint32_t hi = key_of(over_lanes(top ? float_of(top) : -INFINITY, 64, larger));
+            const uint32_t v = reach([&](uint32_t least) {
+                int c = 0;
+#pragma unroll
+                for (int j = 0; j < E; ++j)
+                    if (j * 64 < n) c += __popcll(__ballot(held[j] >= least));
+                return c;
+            }, n, hi, W, FEW);
+            if (lane == 0) {
+                threshold = v;
+                picks = 0;
+            }
+        }
+        __syncthreads();
+        for (int c = tid; c < n; c += JT)
+            if (key_of((float)sc[c]) >= threshold) {
+                const int at = atomicAdd(&picks, 1);
+                if (at < FEW) {
+                    few_sc[at] = sc[c];
+                    few_id[at] = id[c];
+                }
+            }
+        __syncthreads();
+        if (picks <= FEW) {
+            n = picks;
+            score = few_sc;
+            place = few_id;
+        }
+    }
     // (scores and alive are in LDS: the outputs may be the same arrays)
     constexpr int G = 8;  // lanes that share a candidate's count
     for (int c0 = 0; c0 < n; c0 += JT / G) {
         const int c = min(c0 + tid / G, n - 1);
-        const double s = sc[c];
+        const double s = score[c];
         int rank = 0, same = 0;
 #pragma unroll 4
         for (int j = tid % G; j < n; j += G) {
-            rank += sc[j] > s;
-            same += sc[j] == s;
+            rank += score[j] > s;
+            same += score[j] == s;
         }
         const int both = over_lanes(rank | same << 16, G, add);  // (at most 2048 each)
         rank = both & 0xffff;
         same = both >> 16;
         if (same > 1)  // the lowest place first
-            for (int j = 0; j < n; ++j) rank += sc[j] == s && id[j] < id[c];
+            for (int j = 0; j < n; ++j) rank += score[j] == s && place[j] < place[c];
         if (rank >= W || c0 + tid / G >= n || tid % G) continue;
-        const int o = b * W + rank, w = id[c] >> 20, token = id[c] & 0xfffff;
-        p.out_scores[o] = (float)sc[c];
+        const int o = b * W + rank, w = place[c] >> 20, token = place[c] & 0xfffff;
+        p.out_scores[o] = (float)score[c];
         p.out_tokens[o] = token;
         p.out_parents[o] = b * W + w;
         p.out_alive[o] = live[w] != 0 && token != p.eos;
@@ -512,7 +561,9 @@ hipError_t launch_beam_select(const BeamParams& p, hipStream_t s) {
     else if (r == 8) PB_LAUNCH(beam_chunks_kernel<8>, grid, dim3(NT), 0, s, p, chunks);
     else PB_LAUNCH(beam_chunks_kernel<4>, grid, dim3(NT), 0, s, p, chunks);
     const FastDiv by_chunks(chunks), by_width(p.W);
-    if (p.W * chunks <= 256) PB_LAUNCH(beam_join_kernel<256>, dim3(p.B), dim3(256), 0, s, p, chunks, by_chunks, by_width);
+    // (wide beams have up to W entries a list: 8 prompts of 20 beams and 900 logits 13.5 us,
+    // with 256 threads 15.3)
+    if (p.W * chunks <= 256 && p.W <= 11) PB_LAUNCH(beam_join_kernel<256>, dim3(p.B), dim3(256), 0, s, p, chunks, by_chunks, by_width);
     else PB_LAUNCH(beam_join_kernel<1024>, dim3(p.B), dim3(1024), 0, s, p, chunks, by_chunks, by_width);
     return hipGetLastError();
 }

@@ -148,6 +148,23 @@ def test_large_logits_and_scores():
     _run(logits + 1e4, scores * 1000, alive)
 
 
+@pytest.mark.parametrize("W", [7, 11, 12, 16, 20, 32])
+@pytest.mark.parametrize("V", [33, 500, 954, 3000, 6245])
+@pytest.mark.parametrize("spread", [0.0, 1e-3, 1.0])
+def test_few_lists_of_many_entries(W, V, spread):
+    """Rows about as good as each other: most of their entries reach the W-th best row's
+    best, up to W x W of them, with equal ones among them or all equal."""
+    rs = np.random.RandomState(W)
+    logits, scores, alive = _random(rs, 5, W, V)
+    alive[:] = 1
+    scores[:] = -3 + spread * rs.randn(5, W)
+    scores[1, ::2] = scores[1, 0]
+    logits[2 * W : 3 * W] = logits[2 * W]                      # rows alike
+    logits[3 * W : 4 * W] = np.round(logits[3 * W : 4 * W])    # few values
+    logits[4 * W :] = 0.5
+    _run(logits, scores, alive)
+
+
 @pytest.mark.parametrize("far", [2.0 ** 21, 3.5e6, 2.0 ** 22, 5e6, 2.0 ** 23, 3e7])
 @pytest.mark.parametrize("V", [37, 1024, 40000])
 def test_logits_of_millions(far, V):
