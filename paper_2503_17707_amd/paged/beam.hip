@@ -38,6 +38,9 @@ constexpr float LOG2E = 1.4426950408889634f;
 constexpr float HUGE_LOGIT = 4194304.f;  // 2^22: below it a rounded maximum is exact, in base two also
 constexpr int NT = 256;       // threads of a chunk's block
 constexpr int MOST = 1024;    // candidates of a chunk: 32 threads' 32 logits
+// More candidates than CROWD are looked at again before they are placed: equal ones, as a
+// rule (4 beams that all offer 50272 equal logits: 19 us, placed as they are 238).
+constexpr int CROWD = 192;
 constexpr int LISTS = 4096;   // lists of a prompt: 32 rows of 2^20 logits in 128 chunks
 
 // What a logit counts as: NaN is no candidate, +inf the largest float.
@@ -239,7 +242,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(5))) void be
         } else {
             sum *= __builtin_amdgcn_exp2f(__builtin_fmaf(-m, LOG2E, ref));
         }
-        const float least = float_of(t);
+        float least = float_of(t);
         // one counter, at an address that may differ between lanes: a single LDS add
         int* const count = &cn + zero_of_lane();
 #pragma unroll
@@ -249,7 +252,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(5))) void be
                 for (int i = g * G; i < g * G + G; ++i)
                     if (x[i] >= least) {
                         const int at = atomicAdd(count, 1);
-                        if (at < MOST) cand[at] = entry_of(x[i], v0 + i * NT);
+                        if (at < CROWD) cand[at] = entry_of(x[i], v0 + i * NT);
+                        else least = INFINITY;  // looked at again anyway
                     }
     } else {
         sum = 0.f;
@@ -258,10 +262,11 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(5))) void be
     if (lane == 0) ssum[wave] = sum;
     __syncthreads();
     int n = cn;
-    if (n > MOST) {
+    if (n > CROWD) {
         // Many equal ones, or the best side by side in few groups of four threads.  By
-        // all the threads' maxima those above t are at most MOST; of those at t the W
-        // lowest are enough, taken in ascending order.
+        // all the threads' maxima those above t are at most MOST - W (those from t on are
+        // all in W threads, but for equal maxima); of those at t the W lowest are
+        // enough, taken in ascending order.
         auto count = [&](uint32_t least) {
             int c = 0;
 #pragma unroll
@@ -272,14 +277,10 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(5))) void be
         __syncthreads();
         if (tid == 0) cn = 0;
         __syncthreads();
-        for (int i = 0; i < R; ++i) {
-            float v = 0.f;
+        const float best = float_of(t);
 #pragma unroll
-            for (int j = 0; j < R; ++j) v = j == i ? x[j] : v;
-            if (key_of(v) > t) {
-                cand[atomicAdd(&cn, 1)] = entry_of(v, v0 + i * NT);
-            }
-        }
+        for (int i = 0; i < R; ++i)
+            if (x[i] > best) cand[atomicAdd(&cn + zero_of_lane(), 1)] = entry_of(x[i], v0 + i * NT);
         __syncthreads();
         n = cn;
         int taken = 0;
@@ -287,7 +288,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(5))) void be
             float v = 0.f;
 #pragma unroll
             for (int j = 0; j < R; ++j) v = j == i ? x[j] : v;
-            const bool mine = key_of(v) == t;
+            const bool mine = v == best;
             const uint64_t b = __ballot(mine);
             if (lane == 0) eq[wave] = __popcll(b);
             __syncthreads();
@@ -326,6 +327,52 @@ constexpr int TIED = 64;  // lists whose heads may pass the bisection: the W and
 // to FEW (20 prompts of 32 beams and 6245 logits, 32 lists each: the call 23 us, 112 without
 // it; 10 of 12 beams and 954 logits, some 140 entries: 11.4, with it 14.7).
 constexpr int FEW = 128, MANY = 256;
+
+// Which of n candidates, K to a thread, are the `want` that come first, by score and then
+// place: a bit for each of this thread's.  None is -inf.  By all threads, bit by bit: 8 us
+// with 256 of them and 45 with 1024, for candidates too much alike for anything else.
+constexpr int K = 4;
+template <int JT>
+__device__ __forceinline__ uint32_t first_of(const double (&score)[K], const int (&place)[K], int n, int want) {
+    uint64_t key[K];  // in the order of the doubles (-0 and +0 alike), 0: none
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const uint64_t b = __builtin_bit_cast(uint64_t, score[k] + 0.0);
+        key[k] = score[k] == -INFINITY ? 0 : b >> 63 ? ~b : b | (uint64_t)1 << 63;
+    }
+    // (three counters in turn, one barrier a count)
+    __shared__ int counter[3];
+    int turn = 0;
+    if (threadIdx.x == 0) counter[0] = 0;
+    __syncthreads();
+    auto count = [&](auto passed) {
+        int c = 0;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (k * JT < n) c += __popcll(__ballot(passed(k)));
+        const int next = turn == 2 ? 0 : turn + 1;
+        if (threadIdx.x == 0) counter[next] = 0;
+        if (threadIdx.x % 64 == 0) atomicAdd(&counter[turn], c);
+        __syncthreads();
+        c = counter[turn];
+        turn = next;
+        return c;
+    };
+    uint64_t t = 0;  // the want-th largest
+#pragma unroll 1
+    for (uint64_t bit = (uint64_t)1 << 63; bit; bit >>= 1)
+        if (count([&](int k) { return key[k] >= (t | bit); }) >= want) t |= bit;
+    want -= count([&](int k) { return key[k] > t; });
+    uint32_t low = 0;  // and the want-th lowest place of those equal to it, inverted
+#pragma unroll 1
+    for (uint32_t bit = 1u << 31; bit && t; bit >>= 1)
+        if (count([&](int k) { return key[k] == t && ~(uint32_t)place[k] >= (low | bit); }) >= want) low |= bit;
+    uint32_t kept = 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (key[k] > t || (t && key[k] == t && ~(uint32_t)place[k] >= low)) kept |= 1u << k;
+    return kept;
+}
 
 // log of 1 <= x < 2^21: the exponent's part in 64 bits, the rest within 2^-23.
 __device__ inline double log_of(double x) {
@@ -429,20 +476,19 @@ __global__ __launch_bounds__(JT) void beam_join_kernel(BeamParams p, int chunks,
     int n = picks;
     if (n > TIED) {
         // Many heads alike to fp32: the W that come first in 64 bits.
-        __syncthreads();
+        double s[K];
+        int at[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int i = k * JT + tid;
+            s[k] = i < lists && key[min(i, lists - 1)] >= t ? score_of(i, 0, at[k]) : -INFINITY;
+        }
+        const uint32_t kept = first_of<JT>(s, at, lists, W);
         if (tid == 0) picks = 0;
         __syncthreads();
-        for (int i = tid; i < lists; i += JT) {
-            if (key[i] < t) continue;
-            int pi, pj, rank = 0;
-            const double si = score_of(i, 0, pi);
-            for (int j = 0; j < lists && rank < W; ++j)
-                if (key[j] >= t) {
-                    const double sj = score_of(j, 0, pj);
-                    rank += before(sj, pj, si, pi);
-                }
-            if (rank < W) pick[atomicAdd(&picks, 1)] = i;
-        }
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (kept >> k & 1) pick[atomicAdd(&picks, 1)] = k * JT + tid;
         __syncthreads();
         n = picks;
     }
@@ -463,7 +509,7 @@ __global__ __launch_bounds__(JT) void beam_join_kernel(BeamParams p, int chunks,
     const int* place = id;
     if (n > MANY) {
         // Few lists, so most of their entries reach the W-th head: the same once more over
-        // all entries (unless it leaves more, which are equal then).
+        // all entries.
         if (wave == 0) {
             constexpr int E = TIED * BEAM_MAX_WIDTH / 64;
             uint32_t held[E], top = 0;
@@ -496,30 +542,46 @@ __global__ __launch_bounds__(JT) void beam_join_kernel(BeamParams p, int chunks,
                 }
             }
         __syncthreads();
-        if (picks <= FEW) {
-            n = picks;
-            score = few_sc;
-            place = few_id;
+        if (picks > FEW) {  // equal ones
+            double s[K];
+            int at[K];
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int c = k * JT + tid;
+                s[k] = c < n ? sc[min(c, n - 1)] : -INFINITY;
+                at[k] = id[min(c, n - 1)];
+            }
+            const uint32_t kept = first_of<JT>(s, at, n, W);
+            if (tid == 0) picks = 0;
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (kept >> k & 1) {
+                    const int to = atomicAdd(&picks, 1);
+                    few_sc[to] = s[k];
+                    few_id[to] = at[k];
+                }
+            __syncthreads();
         }
+        n = picks;
+        score = few_sc;
+        place = few_id;
     }
     // (scores and alive are in LDS: the outputs may be the same arrays)
     constexpr int G = 8;  // lanes that share a candidate's count
     for (int c0 = 0; c0 < n; c0 += JT / G) {
         const int c = min(c0 + tid / G, n - 1);
         const double s = score[c];
-        int rank = 0, same = 0;
+        const int own_place = place[c];
+        int rank = 0;
 #pragma unroll 4
         for (int j = tid % G; j < n; j += G) {
-            rank += score[j] > s;
-            same += score[j] == s;
+            const bool lower = place[j] < own_place;
+            rank += (score[j] > s) | ((score[j] == s) & lower);
         }
-        const int both = over_lanes(rank | same << 16, G, add);  // (at most 2048 each)
-        rank = both & 0xffff;
-        same = both >> 16;
-        if (same > 1)  // the lowest place first
-            for (int j = 0; j < n; ++j) rank += score[j] == s && place[j] < place[c];
+        rank = over_lanes(rank, G, add);
         if (rank >= W || c0 + tid / G >= n || tid % G) continue;
-        const int o = b * W + rank, w = place[c] >> 20, token = place[c] & 0xfffff;
+        const int o = b * W + rank, w = own_place >> 20, token = own_place & 0xfffff;
         p.out_scores[o] = (float)score[c];
         p.out_tokens[o] = token;
         p.out_parents[o] = b * W + w;

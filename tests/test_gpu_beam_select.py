@@ -10,7 +10,7 @@ pytestmark = pytest.mark.gpu
 INF = float("inf")
 
 
-def _run(logits, scores, alive, eos=2, pad=1, pitch=0, in_place=False):
+def _run(logits, scores, alive, eos=2, pad=1, pitch=0, in_place=False, rows_apart=True):
     import torch
 
     from paged_common import select64
@@ -30,6 +30,8 @@ def _run(logits, scores, alive, eos=2, pad=1, pitch=0, in_place=False):
     ws = torch.full((pb.beam_select_workspace(B, W, V),), 255, dtype=torch.uint8, device="cuda")
     pb.op_beam_select(lg[:, :V], sc, al, *out, eos=eos, pad=pad, workspace=ws)
     for name, got, ref in zip(("tokens", "parents", "alive"), out[1:], want[1:]):
+        if not rows_apart:
+            break
         assert np.array_equal(got.cpu().numpy(), ref), (name, got.cpu().numpy(), ref)
     got = out[0].double().cpu().numpy()
     # fp32 sums of positive terms, each within (|l - m| log2 e + 4) 2^-24 of its
@@ -41,6 +43,20 @@ def _run(logits, scores, alive, eos=2, pad=1, pitch=0, in_place=False):
     tol = (64 + min(V, 4096)) * 2.0 ** -24 + np.abs(want[0]) * 2.0 ** -24
     with np.errstate(invalid="ignore"):
         assert np.all((got == want[0]) | (np.abs(got - want[0]) <= tol))
+    if not rows_apart:
+        # Rows whose scores differ by less than the bound may come in either order: each choice
+        # is as good as the one at its place, and the best tokens of its row, lowest first.
+        tokens, parents = out[1].cpu().numpy(), out[2].cpu().numpy()
+        x = logits.astype(np.float64)
+        lse = x.max(1) + np.log(np.exp(x - x.max(1, keepdims=True)).sum(1))
+        for b in range(B):
+            taken = {}
+            for j in range(W):
+                r, t = parents[b, j], tokens[b, j]
+                assert abs(scores[b, r - b * W] + x[r, t] - lse[r] - want[0][b, j]) <= tol[b, j]
+                taken.setdefault(int(r), []).append(int(t))
+            for r, ts in taken.items():
+                assert ts == np.argsort(-x[r], kind="stable")[: len(ts)].tolist()
     return want
 
 
@@ -163,6 +179,30 @@ def test_few_lists_of_many_entries(W, V, spread):
     logits[3 * W : 4 * W] = np.round(logits[3 * W : 4 * W])    # few values
     logits[4 * W :] = 0.5
     _run(logits, scores, alive)
+
+
+@pytest.mark.parametrize("W,V", [(1, 70000), (4, 60000), (8, 30000), (11, 20000), (12, 20000), (32, 60000), (16, 300000)])
+@pytest.mark.parametrize("kind", ["equal", "low", "plateau", "steps"])
+def test_crowds_of_equal_logits(W, V, kind):
+    """Equal logits in every chunk of every row, of hypotheses with equal scores and not."""
+    rs = np.random.RandomState(W)
+    logits, scores, alive = _random(rs, 2, W, V)
+    alive[:] = 1
+    scores[0] = -4.0
+    if kind == "equal":
+        logits[:] = 0.25
+    elif kind == "low":  # less is allowed than is asked for
+        logits[:, rs.permutation(V)[3:]] = np.finfo(np.float32).min
+    elif kind == "plateau":  # a few hundred equal best ones among others
+        logits[:, rs.permutation(V)[: min(V, 400)]] = 20.0
+        logits[0, V // 2 : V // 2 + 1000] = 20.0
+    else:
+        logits[:] = np.floor(np.arange(V) / 700.0) % 5
+    # On the plateau rows of one score are not apart: their log sums are 20 + log(400 + s), where s
+    # = sum e^(x - 20) over the others is some V e^(4.5 - 20) = V 1.9e-7, so they differ by parts
+    # of s / 400 = V 4.6e-10 (3e-5 of 60000 logits) while the bound is over 64 2^-24 + 4096 2^-24
+    # = 2.5e-4.
+    _run(logits, scores, alive, rows_apart=kind != "plateau")
 
 
 @pytest.mark.parametrize("far", [2.0 ** 21, 3.5e6, 2.0 ** 22, 5e6, 2.0 ** 23, 3e7])
