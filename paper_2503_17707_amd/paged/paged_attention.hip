@@ -531,9 +531,9 @@ void launch_join(const PagedAttentionParams& p, const Cut& cut, hipStream_t s) {
 }
 
 // Most pieces a call can have: PIECES blocks' worth and the remainder of each
-// sequence, or every sequence at the table's width cut into shortest pieces.
-int64_t most_pieces(int rows, int hb, int width, int page_size) {
-    const int64_t each = ((int64_t)width * page_size + SHORTEST - 1) / SHORTEST;
+// sequence, or every sequence at its `longest` cut into shortest pieces.
+int64_t most_pieces(int rows, int hb, int64_t longest) {
+    const int64_t each = (longest + SHORTEST - 1) / SHORTEST;
     const int64_t a = PIECES / hb + rows, b = rows * each;
     return a < b ? a : b;
 }
@@ -550,12 +550,16 @@ hipError_t launch(const PagedAttentionParams& p, hipStream_t s) {
     cut.qb = (group + 16 * nq - 1) / (16 * nq);
     int hb = p.pool.n_kv_heads * cut.qb;
     int64_t items = p.tab.rows;
-    const int64_t most = most_pieces(p.tab.rows, hb, p.tab.width, p.pool.page_size);
+    const int64_t held = (int64_t)p.tab.width * p.pool.page_size;
+    const int64_t longest = p.window > 0 && p.window < held ? p.window : held;  // that is attended to
+    const int64_t most = most_pieces(p.tab.rows, hb, longest);
     // Short sequences stay whole: the join costs 4 us (one of 513, 32 heads of 64: 6.3
     // us, cut 9.4), and so do longer ones that fill the chip as they are (8 of 1000: 14.1,
-    // cut 18.5; one of 2000: 11.2 cut, 16.7 whole).
-    const int uncut = HD == 64 && p.tab.rows * hb >= 256 ? 2048 : 1024;
-    if ((int64_t)p.tab.width * p.pool.page_size > uncut && most > p.tab.rows && p.ws && p.ws_bytes >= cut_bytes(p.tab.rows, most, p.n_heads, HD)) {
+    // cut 18.5; one of 2000: 11.2 cut, 16.7 whole).  With heads of 128 a few blocks take longer
+    // (32 blocks of 600: 9.9, of 1000 13.9; cut 10.1 and 11.5; 128 of 1000: 17.3, cut 19.8).
+    const int64_t whole = (int64_t)p.tab.rows * hb;
+    const int uncut = HD == 64 ? (whole >= 256 ? 2048 : 1024) : (whole >= 64 ? 1024 : 640);
+    if (longest > uncut && most > p.tab.rows && p.ws && p.ws_bytes >= cut_bytes(p.tab.rows, most, p.n_heads, HD)) {
         cut.on = 1;
         cut.at = (int32_t*)p.ws;
         cut.acc = (float*)((char*)p.ws + ((size_t)p.tab.rows * 8 + 15) / 16 * 16);
@@ -596,7 +600,7 @@ hipError_t launch_shared(const PagedAttentionParams& p, hipStream_t s) {
 
 size_t paged_attention_workspace(int n_seqs, int n_heads, int n_kv_heads, int hd, int width, int page_size) {
     const int group = n_heads / n_kv_heads, nq = group <= 16 ? 1 : 2;
-    const int64_t most = most_pieces(n_seqs, n_kv_heads * ((group + 16 * nq - 1) / (16 * nq)), width, page_size);
+    const int64_t most = most_pieces(n_seqs, n_kv_heads * ((group + 16 * nq - 1) / (16 * nq)), (int64_t)width * page_size);
     return most > n_seqs ? cut_bytes(n_seqs, most, n_heads, hd) : 0;
 }
 

@@ -150,6 +150,13 @@ def test_many_small_probabilities_beside_a_large_one():
     assert torch.all((out.double().cpu() - ref).abs() <= tol)
 
 
+@pytest.mark.parametrize("window", [500, 641, 1024, 1500, 4000])
+@pytest.mark.parametrize("H,Hkv,hd", [(8, 2, 64), (8, 2, 128), (24, 1, 128), (40, 1, 64)])
+def test_windows_of_long_sequences(window, H, Hkv, hd):
+    """Whole and cut by what the window leaves, whatever the tables hold."""
+    _run("bf16", H, Hkv, hd, 16, "rows", [0, 1, 499, 1500, 3001, 5000], window=window, width=400)
+
+
 @pytest.mark.parametrize("window", [0, 40])
 def test_bad_pages_give_nan_only_where_they_are_attended_to(window):
     import torch
