@@ -159,8 +159,9 @@ size_t pb_op_paged_attention_workspace(int32_t n_seqs, int32_t n_heads, const pb
  * (within 2^-18: of two rows' continuations that are nearer than that either may
  * come first).  Logits of -inf or NaN are no candidates and have no part in the
  * softmax, one of +inf counts as the largest float; a hypothesis whose score is not
- * finite offers nothing (a prompt's first step: scores 0, -inf, -inf, ...).  Places
- * that no candidate takes: score -inf, token pad, parent -1, alive 0.  out_scores and
+ * finite offers nothing (a prompt's first step: scores 0, -inf, -inf, ...), and a
+ * continuation whose score is below the lowest float is none.  Places that no
+ * candidate takes: score -inf, token pad, parent -1, alive 0.  out_scores and
  * out_alive may be scores and alive.  1 <= W <= 32, 1 <= V <= 2^20, 0 <= pad < V;
  * workspace: pb_op_beam_select_workspace bytes (0 for refused sizes). */
 int pb_op_beam_select(const float* logits, int64_t ld_logits, const float* scores, const int32_t* alive,

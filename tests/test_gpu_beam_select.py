@@ -226,6 +226,23 @@ def test_logits_of_millions(far, V):
         _run(logits, scores, alive)
 
 
+def test_scores_below_the_lowest_float_are_none():
+    import torch
+
+    from paper_2503_17707_amd import binding as pb
+
+    logits = torch.full((4, 9), -3e38, device="cuda")
+    logits[:, 5] = 3e38  # the others' scores are -6e38
+    scores = torch.tensor([[-1.0, -2.0], [-3.0, float("-inf")]], device="cuda")
+    i32 = dict(dtype=torch.int32, device="cuda")
+    alive = torch.ones((2, 2), **i32)
+    out = [torch.empty((2, 2), device="cuda"), *(torch.empty((2, 2), **i32) for _ in range(3))]
+    ws = torch.empty(pb.beam_select_workspace(2, 2, 9), dtype=torch.uint8, device="cuda")
+    pb.op_beam_select(logits, scores, alive, *out, eos=2, pad=1, workspace=ws)
+    assert out[0].tolist() == [[-1.0, -2.0], [-3.0, -INF]]
+    assert [o.tolist() for o in out[1:]] == [[[5, 5], [5, 1]], [[0, 1], [2, -1]], [[1, 1], [1, 0]]]
+
+
 def test_masks_of_the_lowest_float():
     """Tokens masked with the type's lowest value are the last candidates, not none."""
     rs = np.random.RandomState(10)
