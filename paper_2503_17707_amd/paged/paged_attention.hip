@@ -358,7 +358,9 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
                 for (int i = 0; i < RT; ++i) {
                     float w[4];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) w[r] = __builtin_amdgcn_exp2f(sc[t][i][r] - (mb - shift_of<T>()));
+                    // (the shift is added last: far from zero mb - 12 would be rounded, and a
+                    // weight of 2^16 is fp16's infinity)
+                    for (int r = 0; r < 4; ++r) w[r] = __builtin_amdgcn_exp2f((sc[t][i][r] - mb) + shift_of<T>());
                     pf[t][i] = pack4<T>(w[0], w[1], w[2], w[3]);
                 }
                 if (__any(alpha != 1.f)) {

@@ -127,6 +127,35 @@ def test_scores_far_from_zero_in_many_pieces(kind, hd, sign):
         assert torch.all((out.double().cpu() - ref).abs() <= tol)
 
 
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("n", [40, 5000])
+def test_scores_of_millions(kind, n):
+    """Two keys tie far above the others, at scores where fp32 steps are whole numbers: the
+    output is the mean of their values, exactly."""
+    import torch
+
+    from paged_common import CODE, DT, dev
+    from paper_2503_17707_amd import binding as pb
+
+    hd, ps = 64, 16
+    pages = -(-n // ps)
+    pool = torch.zeros((pages, 2, 1, ps, hd), dtype=DT[kind], device="cuda")
+    pool[:, 1] = 100.0
+    for x, v in ((3, 1.0), (n - 2, 2.0)):
+        pool[x // ps, 0, 0, x % ps, 0] = 2.0 ** 13
+        pool[x // ps, 1, 0, x % ps] = v
+    q = torch.zeros((1, 1, hd), dtype=DT[kind], device="cuda")
+    tables, lens = dev(np.arange(pages, dtype=np.int32)[None]), dev(np.array([n], np.int32))
+    ws = torch.full((pb.paged_attention_workspace(1, 1, pool, pages) + 16,), 255, dtype=torch.uint8, device="cuda")
+    for e in (8, 10, 11, 12, 13, 14, 15):
+        for scale in (1.0, 0.8, 8.0):
+            log("paged attention scores of millions", kind, n, e, scale)
+            q[..., 0] = 2.0 ** e
+            out = torch.full_like(q, float("nan"))
+            pb.op_paged_attention(CODE[kind], q, pool, tables, lens, out, scale=scale, workspace=ws)
+            assert torch.all(out == 1.5), (e, scale, out[0, 0, :4].tolist())
+
+
 def test_many_small_probabilities_beside_a_large_one():
     """One key far above 20000 others that weigh 2^-18 each: together 7 percent."""
     import torch
