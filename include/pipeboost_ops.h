@@ -134,8 +134,8 @@ int pb_op_kv_append(int32_t dtype, const void* k, int64_t ld_k, const void* v, i
  * are not looked at).  Nothing past a sequence's last token is read.
  * shared != 0 says that rows next to each other share pages (beams of one prompt):
  * caches are used then for what otherwise streams past them; results are the same.
- * Scores, maxima, sums and products are fp32; probabilities are rounded to dt
- * as they enter the products with V.
+ * Scores, maxima, sums and products are fp32; probabilities enter the products with
+ * V and their sum within 2^-21 (f16) or 2^-15 (bf16) of themselves.
  * workspace (may be NULL): fp32 partial results of the pieces that long
  * sequences are cut into, pb_op_paged_attention_workspace bytes; with a smaller one
  * they are not cut.  Tables hold at most 2^30 tokens a row. */

@@ -156,6 +156,64 @@ def test_scores_of_millions(kind, n):
             assert torch.all(out == 1.5), (e, scale, out[0, 0, :4].tolist())
 
 
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("H,hd", [(1, 64), (3, 128), (20, 128)])
+def test_probabilities_are_not_rounded_to_the_type(kind, H, hd):
+    """Half the keys weigh 1, half e^a, and their values cancel but for their own rounding: a
+    probability that is rounded to the storage type shows, by up to half a step."""
+    import torch
+
+    from paged_common import CODE, DT, HALF_STEP, attention64, dev
+    from paper_2503_17707_amd import binding as pb
+
+    log("paged attention probabilities", kind, H, hd)
+    S, n, ps = 40, 64, 16
+    a = -torch.linspace(0.02, 1.0, S).to(DT[kind])
+    pool = torch.zeros((S, n // ps, 2, 1, ps, hd), dtype=DT[kind])
+    pool[:, :, 0, :, 1::2, 0] = a[:, None, None, None]
+    pool[:, :, 1, :, 0::2] = 1.0
+    pool[:, :, 1, :, 1::2] = -torch.exp(-a.double()).to(DT[kind])[:, None, None, None, None]
+    pool = pool.flatten(0, 1).cuda()
+    q = torch.zeros((S, H, hd), dtype=DT[kind], device="cuda")
+    q[..., 0] = 1.0
+    tables, lens = np.arange(S * n // ps, dtype=np.int32).reshape(S, -1), np.full(S, n, np.int32)
+    out = torch.empty_like(q)
+    pb.op_paged_attention(CODE[kind], q, pool, dev(tables), dev(lens), out)
+    ref, _ = attention64(q, pool, tables, lens, ps, 1.0, 0)
+    # |a| <= 1: the factor to base two, its product and the exponential are off by 5 2^-24 of a
+    # probability, its parts by 2 u^2; both in numerator and sum; fp32 sums over n tokens
+    u = HALF_STEP[kind]
+    tol = 2.75 * (4 * u * u + (20 + 2 * n) * 2.0 ** -24) + u * ref.abs() + 2.0 ** -25
+    err = (out.double().cpu() - ref).abs()
+    log("  worst error / tolerance %.3f" % float((err / tol).max()))
+    assert torch.all(err <= tol)
+
+
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("H,n", [(2, 500), (2, 5000), (20, 5000)])
+def test_other_dimensions_beside_an_infinite_value(kind, H, n):
+    import torch
+
+    from paged_common import CODE, DT, attention64, dev, make_pool
+    from paper_2503_17707_amd import binding as pb
+
+    log("paged attention beside infinities", kind, H, n)
+    ps, hd = 16, 64
+    pages = -(-n // ps)
+    pool = make_pool(3, kind, (pages,), 1, ps, hd, "heads")
+    for x, j, v in ((n // 2, 5, float("inf")), (n - 1, 20, -float("inf"))):
+        pool[x // ps, 1, 0, x % ps, j] = v
+    q = torch.randn((1, H, hd), generator=torch.Generator().manual_seed(4)).to(DT[kind]).cuda()
+    out, tables = torch.empty_like(q), np.arange(pages, dtype=np.int32)[None]
+    ws = torch.full((pb.paged_attention_workspace(1, H, pool, pages) + 16,), 255, dtype=torch.uint8, device="cuda")
+    pb.op_paged_attention(CODE[kind], q, pool, dev(tables), dev(np.array([n], np.int32)), out, scale=0.1, workspace=ws)
+    assert torch.all(out[..., 5] == float("inf")) and torch.all(out[..., 20] == -float("inf"))
+    pool[pool.isinf()] = 0
+    ref, tol = attention64(q, pool, tables, [n], ps, 0.1, 0)
+    keep = [j for j in range(hd) if j not in (5, 20)]
+    assert torch.all(((out.double().cpu() - ref).abs() <= tol)[..., keep])
+
+
 def test_many_small_probabilities_beside_a_large_one():
     """One key far above 20000 others that weigh 2^-18 each: together 7 percent."""
     import torch
