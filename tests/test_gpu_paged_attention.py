@@ -92,6 +92,64 @@ def test_many_sequences(S):
     _run("f16", 2, 1, 64, 16, "heads", lens.tolist())
 
 
+@pytest.mark.parametrize("kind,H,hd,ps,n,window,layout,ws", [
+    ("f16", 16, 128, 16, 5000, 0, "rows", True),     # pieces
+    ("f16", 16, 128, 1, 5000, 0, "heads", True),     # pieces of more pages than are held at a time
+    ("bf16", 16, 64, 1, 1500, 0, "rows", False),     # whole, eight waves
+    ("f16", 1, 64, 1, 700, 0, "gaps", False),        # whole, four waves
+    ("bf16", 32, 128, 20, 3001, 0, "heads", True),   # two operands of queries, pieces
+    ("f16", 32, 64, 1, 1300, 0, "rows", False),      # two operands, whole
+    ("bf16", 16, 128, 16, 4000, 1111, "rows", True),
+    ("f16", 40, 64, 7, 2100, 900, "heads", False),
+])
+def test_every_token_counts_once(kind, H, hd, ps, n, window, layout, ws):
+    """A query per token whose key it shares with one other token alone: the output is the mean
+    of their two values, and would show either of them left out or taken twice."""
+    import torch
+
+    from paged_common import CODE, DT, HALF_STEP, dev, make_pool, make_tables
+    from paper_2503_17707_amd import binding as pb
+
+    log("paged attention token by token", kind, H, hd, ps, n, window)
+    g = torch.Generator().manual_seed(n)
+    lo = n - window if window else 0
+    half = (n - lo) // 2
+    keys = (torch.randint(0, 2, (n, hd), generator=g) * 2 - 1).double()
+    keys[lo + half:lo + 2 * half] = keys[lo:lo + half]
+    values = torch.randn((n, hd), generator=g).to(DT[kind])
+    pages = -(-n // ps)
+    tables = make_tables(np.random.RandomState(n), [n], ps, pages, pages)
+    pool = make_pool(1, kind, (pages,), 1, ps, hd, layout)
+    pool.fill_(float("nan"))
+    x = torch.arange(n)
+    at = torch.from_numpy(tables[0]).long()[x // ps].cuda(), (x % ps).cuda()
+    pool[at[0], 0, 0, at[1]] = keys.to(DT[kind]).cuda()
+    pool[at[0], 1, 0, at[1]] = values.cuda()
+    S = -(-2 * half // H)
+    who = lo + torch.arange(S * H) % (2 * half)  # the token that a query asks for
+    q = keys[who].to(DT[kind]).view(S, H, hd).cuda()
+    out = torch.empty_like(q)
+    work = None
+    if ws:
+        work = torch.full((pb.paged_attention_workspace(S, H, pool, pages),), 255, dtype=torch.uint8, device="cuda")
+        assert work.numel() > 0
+    pb.op_paged_attention(CODE[kind], q, pool, dev(np.repeat(tables, S, 0)), dev(np.full(S, n, np.int32)), out, window=window,
+                          workspace=work)
+    k, v = keys[lo:].cuda(), values[lo:].double().cuda()
+    p = torch.softmax(keys[who].cuda() @ k.t().contiguous(), 1)
+    ref = p @ v
+    # scores are whole numbers up to hd: their factor to base two and its product round, equal
+    # ones alike; parts of probabilities, sums and the output as elsewhere
+    u, V = HALF_STEP[kind], float(v.abs().max())
+    tol = V * (4 * u * u + 4 * 5 * hd * 2.0 ** -24 + 2 * len(v) * 2.0 ** -24) + u * ref.abs() + 2.0 ** -25
+    mine = p.gather(1, (who - lo).cuda()[:, None])
+    gap = mine * (v[who - lo] - ref)  # over 1 -+ mine: what a token left out or taken twice changes
+    assert torch.all((gap.abs() / (1 + mine) > 4 * tol).any(1))
+    err = (out.view(-1, hd).double() - ref).abs()
+    log("  worst error / tolerance %.3f" % float((err / tol).max()))
+    assert torch.all(err <= tol)
+
+
 def test_peaked_and_flat_scores():
     # large scores: one key takes all; scale 0: the mean of the values
     _run("f16", 4, 4, 64, 16, "heads", [700, 65], scale=3.0)
