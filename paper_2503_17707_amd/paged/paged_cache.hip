@@ -375,7 +375,7 @@ hipError_t launch_kv_append(const AppendParams& p, hipStream_t s) {
     const int rpb = p.max_rows == 1 ? 1 : (16384 + row_bytes - 1) / row_bytes;
     const FastDiv per_row(2 * p.pool.n_kv_heads * p.pool.head_dim / 8);
     // (max_rows may be far more than any sequence has: blocks take rows in turn then)
-    const int blocks = (p.max_rows + rpb - 1) / rpb, most = 32768 / p.tab.rows + 1;
+    const int blocks = (p.max_rows - 1) / rpb + 1, most = 32768 / p.tab.rows + 1;
     const dim3 grid(blocks < most ? blocks : most, p.tab.rows);
     if (p.max_rows == 1) PB_LAUNCH(kv_append_kernel<false>, grid, dim3(256), 0, s, p, rpb, per_row);
     else PB_LAUNCH(kv_append_kernel<true>, grid, dim3(256), 0, s, p, rpb, per_row);

@@ -74,6 +74,12 @@ def test_append_with_a_bound_far_above_the_rows():
     _append("bf16", 2, 128, 16, "rows", [0, 3], [9000, 5], max_rows=9000)
 
 
+@pytest.mark.parametrize("Hkv,hd", [(1, 64), (32, 64), (40, 128)])
+def test_append_without_a_bound(Hkv, hd):
+    # the largest max_rows there is: as many rows as lens and start say
+    _append("f16", Hkv, hd, 16, "rows", [0, 3, 7], [70, 3, 47], row0=[0, 70, 70], max_rows=2 ** 31 - 1)
+
+
 def test_append_skips_what_has_no_place():
     tables = np.array([[0, -1, 2], [3, 9, 5], [6, 7, 8], [1, -3, 1 << 30]], np.int32)
     # holes, ids past the pool, past the width, a negative start, rows outside k and v
