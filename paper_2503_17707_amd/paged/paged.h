@@ -78,6 +78,8 @@ struct ForkParams {
     void* ws;
 };
 size_t page_fork_workspace(int out_rows, int n_pages);
+// Pieces of pages that the rows' copies can be, at most; launches need them below 2^31.
+int64_t page_fork_copies(const ForkParams& p);
 hipError_t launch_page_fork(const ForkParams& p, hipStream_t s);
 
 }  // namespace pb

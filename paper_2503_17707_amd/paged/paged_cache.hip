@@ -384,6 +384,13 @@ hipError_t launch_kv_append(const AppendParams& p, hipStream_t s) {
 
 size_t page_fork_workspace(int out_rows, int n_pages) { return ((size_t)2 * n_pages + 5 * (size_t)out_rows + 1) * 4; }
 
+static int64_t copy_pieces(const PagePool& c) {
+    const int64_t chunks = (int64_t)c.page_size * 2 * c.n_kv_heads * c.head_dim / 8;
+    return (chunks + PIECE - 1) / PIECE;
+}
+
+int64_t page_fork_copies(const ForkParams& p) { return p.out_rows * (int64_t)p.n_layers * copy_pieces(p.pool); }
+
 hipError_t launch_page_fork(const ForkParams& p, hipStream_t s) {
     const int P = p.pool.n_pages;
     const int rows = p.in_rows > p.out_rows ? p.in_rows : p.out_rows;
@@ -400,9 +407,7 @@ hipError_t launch_page_fork(const ForkParams& p, hipStream_t s) {
         if (rows > 0) PB_LAUNCH(fork_tables_kernel, dim3((p.width + 1023) / 1024, rows), dim3(256), 0, s, p);
         if (p.out_rows > 0) PB_LAUNCH(fork_places_kernel<false>, dim3(1), dim3(1024), 0, s, p, FastDiv(p.width));
     }
-    const int64_t chunks = (int64_t)p.pool.page_size * 2 * p.pool.n_kv_heads * p.pool.head_dim / 8;
-    const int64_t pieces = (chunks + PIECE - 1) / PIECE, most = p.out_rows * (int64_t)p.n_layers * pieces;
-    if (most > 0x7fffffff) return hipErrorInvalidValue;
+    const int64_t most = page_fork_copies(p), pieces = copy_pieces(p.pool);
     if (most > 0)
         PB_LAUNCH(fork_copy_kernel, dim3((unsigned)(most < COPY_BLOCKS ? most : COPY_BLOCKS)), dim3(256), 0, s, p,
                   FastDiv(p.pool.n_kv_heads), FastDiv(p.n_layers), FastDiv((uint32_t)pieces),

@@ -205,5 +205,8 @@ extern "C" int pb_op_page_fork(int32_t dtype, const pb_kv_pool* pool, int32_t n_
     p.tables = tables; p.width = width; p.lens = lens; p.in_rows = in_rows; p.refs = refs; p.grow = grow;
     p.out_tables = out_tables; p.out_start = out_start; p.out_lens = out_lens; p.out_refs = out_refs;
     p.short_of = short_of; p.ws = workspace;
+    if (pb::page_fork_copies(p) > 0x7fffffff)
+        return refuse("%s: %d rows in %d layers of pages of %lld bytes: 2^31 pieces of 32 KB to copy or more", op, out_rows, n_layers,
+                      (long long)pool->page_size * 4 * pool->n_kv_heads * pool->head_dim);
     return launched(op, pb::launch_page_fork(p, (hipStream_t)stream));
 }

@@ -107,6 +107,18 @@ def test_fork_refusals(bad):
     _refused(pb, _fork(pb, _pool(pb), **bad), bad)
 
 
+def test_fork_of_more_copies_than_a_launch_takes():
+    from paper_2503_17707_amd import binding as pb
+
+    # pages of 64 KB are two pieces; a page of a piece and a little, two
+    far = dict(parents=0x10 << 32, tables=0x20 << 32, lens=0x30 << 32, grow=0x50 << 32, ot=0x60 << 32, os=0x70 << 32,
+               ol=0x80 << 32, ws_bytes=1 << 22)
+    _refused(pb, _fork(pb, _pool(pb, page_size=64), L=32768, R=32768, **far), "2^31")
+    assert "2^31" in pb.lib().pb_last_error().decode()
+    _refused(pb, _fork(pb, _pool(pb, page_size=33), L=32768, R=32768, **far), "2^31")
+    assert "2^31" in pb.lib().pb_last_error().decode()
+
+
 def test_nothing_to_do_is_no_error():
     from paper_2503_17707_amd import binding as pb
 
