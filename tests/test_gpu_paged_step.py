@@ -196,6 +196,42 @@ def test_recorded_step_equals_eager():
     assert max(live) > 700
 
 
+def test_the_readme_s_step_runs():
+    """The step as the README shows it: scores, parents and alive [prompts, beams], q scaled."""
+    import os
+
+    import torch
+
+    from paged_common import attention64, select64
+    from paper_2503_17707_amd import binding as pb
+
+    log("the README's step")
+    readme = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
+    code = [b.split("```")[0] for b in readme.split("```python\n")[1:] if "op_page_fork" in b.split("```")[0]]
+    assert len(code) == 1
+    B, W, L, prompts = 2, 3, 2, (5, 40)
+    s = Beams("f16", B, W, L, 4, 2, 64, 16, 50, 60, "rows", 3)
+    g = torch.Generator().manual_seed(3)
+    s.admit(prompts, [_kv(torch, g, s.dt, sum(prompts), 2, 64) for _ in range(L)])
+    s.qkv.copy_(torch.randn(s.qkv.shape, generator=g))
+    s.qkv[1] = s.qkv[0]
+    s.logits.copy_(torch.randn(s.logits.shape, generator=g))
+    s.scores.copy_(-torch.rand(s.scores.shape, generator=g))
+    s.alive[1, 2] = 0
+    q, k, v = s.split(0)
+    want = select64(s.logits.cpu().numpy(), s.scores.cpu().numpy(), s.alive.cpu().numpy(), 2, 1)
+    a, b = s.sets
+    exec(code[0], dict(pb=pb, dt=s.code, pools=s.pool, parents=s.parents, tables=a["tables"], lens=a["lens"], refs=a["refs"],
+                       alive=s.alive, new_tables=b["tables"], start=b["start"], new_lens=b["lens"], new_refs=b["refs"],
+                       short=s.short, ws=s.ws, n_layers=L, q=q, k=k, v=v, out=s.out[0], logits=s.logits, scores=s.scores,
+                       tokens=s.tokens))
+    assert b["lens"].tolist() == [6, 6, 6, 41, 41, 40] and s.short.tolist() == [0, 0]
+    ref, tol = attention64(q, s.pool[1], b["tables"].cpu().numpy(), b["lens"].tolist(), 16, 1.0, 0)
+    assert torch.all((s.out[0].double().cpu() - ref).abs() <= tol)
+    for got, ref in zip((s.tokens, s.parents, s.alive), want[1:]):
+        assert np.array_equal(got.cpu().numpy(), ref)
+
+
 def test_two_streams_at_once():
     """Calls on two streams, each with its own workspace, and a stream passed by argument."""
     import torch
