@@ -22,7 +22,8 @@
 //  - Sequences are cut into pieces, at most as long as a length chosen on the device
 //    from the call's lengths (which may change between replays of a recorded launch),
 //    so that about PIECES blocks of like work cover a ragged batch as well as one long
-//    sequence.  A second launch joins the pieces of sequences that have several.
+//    sequence.  A second launch joins the pieces of sequences that have several; of many
+//    sequences one ahead lists the pieces.
 //
 // Measured: 131071 tokens, 32 heads on 8 of 128 (537 MB) 96 us, 5.6 TB/s; 48 ragged
 // sequences up to 16384, 64 heads on 8 (368 MB) 74 us, 5.0 TB/s; 32 ragged up to 2048,
@@ -49,11 +50,15 @@ constexpr int PIECES = 2048;  // blocks aimed at
 // 256 19.8; 32 of 303, 40 heads of 128: 256 54 us, 512 47.
 constexpr int SHORTEST = 128, LEAST = 512, FEW_BLOCKS = 512;
 
-// How a call is cut: written to the workspace by the first block, read by the join.
+// How a call is cut: written to the workspace by the first block, or by a launch before
+// (LISTED), and read by the join.
 struct Cut {
     int on;        // 0: one piece per sequence, no join
     int qb;        // blocks of 16 NQ query heads per key/value head
     int32_t* at;   // [rows][2] first piece of each sequence, how many
+    int most;      // pieces there can be
+    int4* list;    // [most] each piece's sequence (-1: none), first token, end and how many
+                   // pieces the sequence has (-1: one that is past its table); NULL: not listed
     float* ml;     // [pieces][n_heads][2] maximum (log2 units) and sum
     float* acc;    // [pieces][n_heads][HD] unnormalised output
 };
@@ -185,6 +190,88 @@ __device__ __forceinline__ int piece_length(int64_t tokens, int blocks_per_piece
 
 __device__ __forceinline__ int pieces_of(int n, int len_c) { return max(1, (n + len_c - 1) / len_c); }
 
+// A sequence's pieces are equally long, whole tiles but for the last.
+__device__ __forceinline__ int piece_tokens(int n, int pieces) {
+    return pieces == 1 ? n : (n + pieces * 32 - 1) / (pieces * 32) * 32;
+}
+
+// Long pieces come first, so that the short ones fill the end.
+__device__ __forceinline__ bool is_long(int n, int k, int len_c) { return n >= (int64_t)k * (len_c / 2); }
+
+// The cut of more sequences than LISTED, by one block.  Up to there every wave of the
+// attention works it out for itself, which spares 3 us of a launch, but takes lengths
+// times blocks, and blocks grow with the lengths (32 heads on 8 of 128 in tables of 16384
+// tokens, listed and each wave for itself: 96 sequences up to 2000 80 us and 76, 192 163 and
+// 162, 1024 up to 600 241 and 402, 4096 up to 200 416 and 3146; 192 up to 200, 32 heads of
+// 64: 39 and 53).
+constexpr int LISTED = 128;
+__global__ __launch_bounds__(1024) void paged_cut_kernel(PagedAttentionParams p, Cut cut, int hb) {
+    __shared__ int64_t tokens_of[16];
+    __shared__ int longs_of[16], shorts_of[16];
+    const int S = p.tab.rows, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const Span own = tid < S ? span_of(p, tid) : Span{};
+    auto span = [&](int i) { return i == tid ? own : span_of(p, i); };
+    int low = 0, high = 0;  // (a wave's sums fit: 4096 lengths of up to 2^30)
+    for (int i = tid; i < S; i += 1024) {
+        const int n = span(i).n;
+        low += n & 0x7fff;
+        high += n >> 15;
+    }
+    low = wave_sum_dpp(low);
+    high = wave_sum_dpp(high);
+    if (lane == 0) tokens_of[wave] = ((int64_t)high << 15) + low;
+    __syncthreads();
+    int64_t tokens = 0;
+    for (int w = 0; w < 16; ++w) tokens += tokens_of[w];
+    const int len_c = piece_length(tokens, hb);
+    int longs = 0;
+    for (int i = tid; i < S; i += 1024) {
+        const int n = span(i).n, k = pieces_of(n, len_c);
+        longs += is_long(n, k, len_c) ? k : 0;
+    }
+    longs = wave_sum_dpp(longs);
+    if (lane == 0) longs_of[wave] = longs;
+    __syncthreads();
+    int at_long = 0, at_short = 0;  // of the next 1024 sequences
+    for (int w = 0; w < 16; ++w) at_short += longs_of[w];
+    for (int i0 = 0; i0 < S; i0 += 1024) {
+        const int i = i0 + tid;
+        const Span x = i < S ? span(i) : Span{};
+        const int k = i < S ? pieces_of(x.n, len_c) : 0;
+        const bool lng = is_long(x.n, k, len_c);
+        const int l = wave_scan_dpp(lng ? k : 0), s = wave_scan_dpp(lng ? 0 : k);
+        __syncthreads();  // what was there was read
+        if (lane == 63) {
+            longs_of[wave] = l;
+            shorts_of[wave] = s;
+        }
+        __syncthreads();
+        int at = (lng ? at_long + l : at_short + s) - k;
+        for (int w = 0; w < 16; ++w) {
+            if (w < wave) at += lng ? longs_of[w] : shorts_of[w];
+            at_long += longs_of[w];
+            at_short += shorts_of[w];
+        }
+        if (i < S) {
+            cut.at[2 * i] = at;
+            cut.at[2 * i + 1] = k;
+        }
+        const int len = k > 0 ? piece_tokens(x.n, k) : 0;
+        constexpr int OWN = 8;  // pieces that a lane lists by itself, more by the whole wave
+        for (int j = 0; j < OWN && j < k; ++j)
+            cut.list[at + j] = make_int4(i, x.lo + min(j * len, x.n), x.lo + min(j * len + len, x.n), x.wide ? -1 : k);
+        for (uint64_t many = __ballot(k > OWN); many; many &= many - 1) {
+            const int who = __ffsll((unsigned long long)many) - 1;
+            const int first = __builtin_amdgcn_readlane(at, who), pieces = __builtin_amdgcn_readlane(k, who);
+            const int lo = __builtin_amdgcn_readlane(x.lo, who), n = __builtin_amdgcn_readlane(x.n, who);
+            const int l = __builtin_amdgcn_readlane(len, who);
+            for (int j = OWN + lane; j < pieces; j += 64)
+                cut.list[first + j] = make_int4(i - lane + who, lo + min(j * l, n), lo + min(j * l + l, n), pieces);
+        }
+    }
+    for (int j = at_short + tid; j < cut.most; j += 1024) cut.list[j] = make_int4(-1, 0, 0, 0);
+}
+
 template <typename T, int HD, int NQ, int NW, bool SHARED>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2)))
 void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
@@ -212,14 +299,24 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
     const int unit = blockIdx.x / (8 * cut.qb) * 8 + blockIdx.x % 8;  // (piece, key/value head)
     const int kvh = unit % p.pool.n_kv_heads, q0 = (int)(blockIdx.x / 8 % cut.qb) * 16 * NQ;
     const int item = unit / p.pool.n_kv_heads;
-    int s = item, piece = 0, pieces = 1, slot = 0;
-    Span sp;
+    int s = item, pieces = 1, slot = 0;
+    int ka, kb;         // tokens of this block
+    bool wide = false;  // the sequence is past its table
     if (!cut.on && s >= p.tab.rows) return;
 
-    if (cut.on) {
+    if (cut.list) {
+        if (item >= cut.most) return;
+        const int4 mine = cut.list[item];
+        s = __builtin_amdgcn_readfirstlane(mine.x);
+        if (s < 0) return;  // the grid is sized for the most pieces there can be
+        ka = __builtin_amdgcn_readfirstlane(mine.y);
+        kb = __builtin_amdgcn_readfirstlane(mine.z);
+        pieces = __builtin_amdgcn_readfirstlane(mine.w);
+        wide = pieces < 0;
+        slot = item;
+    } else if (cut.on) {
         // Which piece of which sequence: every wave works the cut out for itself from
-        // the lengths (a scan over them, without a barrier).  A sequence's pieces are
-        // equally long; the long pieces come first, so that the short ones fill the end.
+        // the lengths (a scan over them, without a barrier).
         const int S = p.tab.rows, per = (S + 63) / 64;
         const int s0 = min(lane * per, S), s1 = min(s0 + per, S);
         // tokens in two parts whose sums over 65535 sequences of 2^30 fit 32 bits
@@ -231,21 +328,20 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
             high += n >> 15;
         }
         const int len_c = piece_length(((int64_t)wave_sum_dpp(high) << 15) + wave_sum_dpp(low), hb);
-        auto is_long = [&](int n, int k) { return n >= (int64_t)k * (len_c / 2); };
         int n_long = 0, n_short = 0;  // pieces of this lane's sequences
         for (int i = s0; i < s1; ++i) {
             const int n = i == s0 ? own.n : span_of(p, i).n, k = pieces_of(n, len_c);
-            if (is_long(n, k)) n_long += k; else n_short += k;
+            if (is_long(n, k, len_c)) n_long += k; else n_short += k;
         }
         int at_long = wave_scan_dpp(n_long), at_short = wave_scan_dpp(n_short);
         at_short += __builtin_amdgcn_readlane(at_long, 63) - n_short;
         at_long -= n_long;
-        int mine = -1;
+        int mine = -1, piece = 0;
         Span found{};
         for (int i = s0; i < s1; ++i) {
             const Span x = i == s0 ? own : span_of(p, i);
             const int n = x.n, k = pieces_of(n, len_c);
-            int& at = is_long(n, k) ? at_long : at_short;
+            int& at = is_long(n, k, len_c) ? at_long : at_short;
             if (item >= at && item < at + k) {
                 mine = i;
                 found = x;
@@ -259,22 +355,24 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
             at += k;
         }
         const uint64_t who = __ballot(mine >= 0);
-        if (!who) return;  // the grid is sized for the most pieces there can be
+        if (!who) return;
         const int l = __ffsll((unsigned long long)who) - 1;
         s = __builtin_amdgcn_readlane(mine, l);
         piece = __builtin_amdgcn_readlane(piece, l);
         pieces = __builtin_amdgcn_readlane(pieces, l);
-        sp.lo = __builtin_amdgcn_readlane(found.lo, l);
-        sp.n = __builtin_amdgcn_readlane(found.n, l);
-        sp.wide = __builtin_amdgcn_readlane(found.wide, l);
+        found.lo = __builtin_amdgcn_readlane(found.lo, l);
+        found.n = __builtin_amdgcn_readlane(found.n, l);
+        wide = __builtin_amdgcn_readlane(found.wide, l);
+        const int len = piece_tokens(found.n, pieces);
+        ka = found.lo + min(piece * len, found.n);
+        kb = found.lo + min(piece * len + len, found.n);
         slot = item;
     } else {
-        sp = span_of(p, s);
+        const Span sp = span_of(p, s);
+        wide = sp.wide;
+        ka = sp.lo;
+        kb = sp.lo + sp.n;
     }
-
-    const int len_p = pieces == 1 ? sp.n : (sp.n + pieces * 32 - 1) / (pieces * 32) * 32;
-    const int ka = sp.lo + min(piece * len_p, sp.n);
-    const int kb = min(ka + len_p, sp.lo + sp.n);
     const int nq = min(group - q0, 16 * NQ);  // query heads of this block
     const int h0 = kvh * group + q0;
 
@@ -297,7 +395,7 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
     const float fold = p.scale * LOG2E;
     const uint16_t* base = p.pool.base + kvh * p.pool.head_stride;
     uint8_t* myv = sv + wave * WB;
-    bool bad = sp.wide;
+    bool bad = wide;
 
     // IDS pages at a time
     for (int seg = ka; seg < kb && !bad;) {
@@ -459,7 +557,7 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
         }
         if (bad) L = NAN;
         const int h = h0 + 16 * t + q;
-        const bool empty = sp.n == 0 && !bad;
+        const bool empty = ka == kb && !bad;  // (of a sequence in one piece)
 #pragma unroll
         for (int j = 0; j < (HD + 16 * NW - 1) / (16 * NW); ++j) {
             const int ch = j * 4 * NW + tid % (4 * NW);  // 4 dimensions
@@ -568,8 +666,11 @@ int64_t most_pieces(int rows, int hb, int64_t longest) {
     return a < b ? a : b;
 }
 
+// The cut and the list of pieces (multiples of 16 bytes), their partial results.
+size_t at_bytes(int rows) { return ((size_t)rows * 8 + 15) / 16 * 16; }
+size_t list_bytes(int rows, int64_t pieces) { return rows > LISTED ? (size_t)pieces * 16 : 0; }
 size_t cut_bytes(int rows, int64_t pieces, int n_heads, int hd) {
-    return ((size_t)rows * 8 + 15) / 16 * 16 + (size_t)pieces * n_heads * (hd + 2) * 4;
+    return at_bytes(rows) + list_bytes(rows, pieces) + (size_t)pieces * n_heads * (hd + 2) * 4;
 }
 
 template <typename T, int HD, bool SHARED>
@@ -591,8 +692,11 @@ hipError_t launch(const PagedAttentionParams& p, hipStream_t s) {
     const int uncut = HD == 64 ? (whole >= 256 ? 2048 : 1024) : (whole >= 64 ? 1024 : 640);
     if (longest > uncut && most > p.tab.rows && p.ws && p.ws_bytes >= cut_bytes(p.tab.rows, most, p.n_heads, HD)) {
         cut.on = 1;
+        cut.most = (int)most;
         cut.at = (int32_t*)p.ws;
-        cut.acc = (float*)((char*)p.ws + ((size_t)p.tab.rows * 8 + 15) / 16 * 16);
+        const size_t list = list_bytes(p.tab.rows, most);
+        if (list) cut.list = (int4*)((char*)p.ws + at_bytes(p.tab.rows));
+        cut.acc = (float*)((char*)p.ws + at_bytes(p.tab.rows) + list);
         cut.ml = cut.acc + (size_t)most * p.n_heads * HD;
         items = most;
     }
@@ -608,6 +712,7 @@ hipError_t launch(const PagedAttentionParams& p, hipStream_t s) {
     const int64_t blocks = (items * p.pool.n_kv_heads + 7) / 8 * 8 * cut.qb;
     if (blocks > 0x7fffffff) return hipErrorInvalidValue;
     const dim3 grid((unsigned)blocks);
+    if (cut.list) PB_LAUNCH(paged_cut_kernel, dim3(1), dim3(1024), 0, s, p, cut, hb);
     // Few uncut blocks: eight waves each (8 sequences of 1000, 32 heads of 64: 14.1 us,
     // four 16.4); cut ones have little to share out.
     if (nq == 1 && !cut.on && items * hb < 512)

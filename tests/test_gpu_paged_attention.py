@@ -150,6 +150,46 @@ def test_every_token_counts_once(kind, H, hd, ps, n, window, layout, ws):
     assert torch.all(err <= tol)
 
 
+@pytest.mark.parametrize("S,H,Hkv,hd,window", [(128, 4, 2, 128, 0), (129, 4, 2, 128, 0), (200, 2, 2, 64, 0), (1500, 1, 1, 64, 0), (1024, 2, 1, 128, 0),
+                                               (300, 2, 1, 64, 2100)])
+def test_many_sequences_in_pieces(S, H, Hkv, hd, window):
+    """Sequences of none to thousands of tokens in wide tables, where the cut is listed first and not."""
+    rs = np.random.RandomState(S)
+    lens = rs.randint(0, 24, S)
+    lens[[3, S // 2, S - 2]] = [4999, 2500, 129]
+    lens[[5, S - 1]] = [-7, 1600]
+    _run("f16", H, Hkv, hd, 16, "heads", lens.tolist(), window=window, width=400)
+
+
+def test_many_long_sequences_and_one_past_its_table():
+    import torch
+
+    from paged_common import attention64, dev, make_pool
+    from paper_2503_17707_amd import binding as pb
+
+    log("paged attention many long")
+    S, ps, hd, pages = 140, 16, 64, 256
+    rs = np.random.RandomState(0)
+    lens = rs.randint(1, 4097, S).astype(np.int32)
+    lens[7] = 4097
+    pool = make_pool(0, "f16", (pages,), 1, ps, hd, "heads")
+    tables = np.stack([rs.permutation(pages) for _ in range(S)]).astype(np.int32)  # pages in common
+    tables[9, :] = -1
+    q = torch.randn((S, 2, hd), generator=torch.Generator().manual_seed(1)).half().cuda()
+    ws = torch.full((pb.paged_attention_workspace(S, 2, pool, pages),), 255, dtype=torch.uint8, device="cuda")
+    out = torch.empty_like(q)
+    pb.op_paged_attention(1, q, pool, dev(tables), dev(lens), out, scale=0.125, workspace=ws)
+    bad = torch.isnan(out).flatten(1)
+    assert bad[[7, 9]].all() and not bad[[i for i in range(S) if i not in (7, 9)]].any()
+    some = [0, 1, 8, 10, 63, 64, 65, 100, 139]
+    ref, tol = attention64(q[some], pool, tables[some], lens[some], ps, 0.125, 0)
+    assert torch.all((out[some].double().cpu() - ref).abs() <= tol)
+    plain = torch.empty_like(q)  # no sequence in pieces
+    pb.op_paged_attention(1, q, pool, dev(tables), dev(lens), plain, scale=0.125)
+    rest = [i for i in range(S) if i not in (7, 9)]
+    assert (out[rest].float() - plain[rest].float()).abs().max() < 2e-3
+
+
 def test_peaked_and_flat_scores():
     # large scores: one key takes all; scale 0: the mean of the values
     _run("f16", 4, 4, 64, 16, "heads", [700, 65], scale=3.0)
