@@ -90,8 +90,9 @@ def kind_of(name):
         return {0: "gemv_qkv", 1: "gemv_fc1", 2: "gemv_o_fc2", 3: "gemv_shrink"}[int(m.group(1))]
     if "decode_attention" in name:
         return "decode_attention"
-    for k, kind in (("paged_attention", "paged_attention"), ("paged_join", "paged_attention"), ("paged_cut", "paged_attention"), ("kv_append", "kv_append"),
-                    ("fork_", "page_fork"), ("beam_", "beam_select")):
+    for k, kind in (("paged_attention", "paged_attention"), ("paged_join", "paged_attention"),
+                    ("paged_cut", "paged_attention"), ("kv_append", "kv_append"), ("fork_", "page_fork"),
+                    ("beam_", "beam_select")):
         if k in name:
             return kind
     if "row_shrink" in name:

@@ -217,6 +217,27 @@ def test_fork_of_nothing():
     _fork("f16", 1, 1, 64, 4, "heads", [], [[0, -1]], [3], [1, 0], [])
 
 
+@pytest.mark.parametrize("n_pages", [2730, 2731, 8191, 8192, 8193])
+@pytest.mark.parametrize("R", [6, 511])
+def test_fork_where_pools_no_longer_fit_one_block(n_pages, R):
+    """Pools around the sizes where one block counts their pages in more LDS, and no longer does:
+    references and free pages to the last one, rows near the most that block takes too."""
+    rs = np.random.RandomState(n_pages + R)
+    width, ps = 16384 // 512, 8
+    lens = rs.randint(1, 20, R) if R > 100 else rs.randint(1, width * ps - 9, R)
+    need = -(-lens // ps)
+    pages = n_pages - 1 - rs.permutation(min(n_pages, 2000))  # of the far end, the last one among them
+    rs.shuffle(pages)
+    tables = np.full((R, width), -1)
+    free = list(pages)
+    for r in range(R):
+        tables[r, :need[r]] = [free.pop() for _ in range(need[r])]
+    refs = np.bincount(tables[tables >= 0], minlength=n_pages)
+    refs[: n_pages // 2] = 1  # held by others
+    parents = np.sort(rs.randint(0, R, R))
+    _fork("f16", 1, 1, 64, ps, "heads", parents, tables, lens, refs, rs.randint(0, 3, R), seed=R)
+
+
 def test_fork_over_many_pages():
     """Free pages far into a large pool, most of it in use."""
     rs = np.random.RandomState(3)
