@@ -264,9 +264,10 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(5))) void be
     int n = cn;
     if (n > CROWD) {
         // Many equal ones, or the best side by side in few groups of four threads.  By
-        // all the threads' maxima those above t are at most MOST - W (those from t on are
-        // all in W threads, but for equal maxima); of those at t the W lowest are
-        // enough, taken in ascending order.
+        // all the threads' maxima: W threads reach t, and hold those above it and those at
+        // it, MOST at most; or more do, then t is the W-th largest maximum, those above it
+        // are in W - 1 threads, and of those at t the W lowest are enough, taken in
+        // ascending order: MOST at most again.
         auto count = [&](uint32_t least) {
             int c = 0;
 #pragma unroll

@@ -226,6 +226,33 @@ def test_logits_of_millions(far, V):
         _run(logits, scores, alive)
 
 
+@pytest.mark.parametrize("R,V", [(1, 255), (1, 257), (1, 1023), (1, 1024), (1, 1025), (3, 4097), (600, 8191), (600, 8192),
+                                 (600, 8193), (300, 16385), (70, 50271), (70, 50273), (1, 131071)])
+def test_every_logit_is_in_the_log_sum(R, V):
+    """Log sums to the 2^-18 that are promised, where a logit left out or taken twice weighs more."""
+    import torch
+
+    from paper_2503_17707_amd import binding as pb
+
+    log("beam select log sums", R, V)
+    assert 1 / V > 1.5 * 2.0 ** -18  # of equal logits
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x = torch.randn((R, V), generator=g, device="cuda")
+    x[0::3] = x[0::3, :1] * 3  # equal ones
+    x[1::3] = 5 + 1e-3 * x[1::3]  # and nearly
+    x[2::3] *= 3
+    best, ref = x.double().max(1).values, torch.logsumexp(x.double(), 1)
+    own = (ref - best).float().view(R, 1)  # leaves what the log sum is off by
+    i32 = dict(dtype=torch.int32, device="cuda")
+    out = [torch.empty((R, 1), device="cuda"), *(torch.empty((R, 1), **i32) for _ in range(3))]
+    ws = torch.full((pb.beam_select_workspace(R, 1, V),), 255, dtype=torch.uint8, device="cuda")
+    pb.op_beam_select(x, own, torch.ones((R, 1), **i32), *out, eos=-1, pad=0, workspace=ws)
+    want = own[:, 0].double() + (best - ref)
+    err = (out[0][:, 0].double() - want).abs()
+    log("  worst error %.2e" % float(err.max()))
+    assert torch.all(err <= 2.0 ** -18 + want.abs() * 2.0 ** -24)
+
+
 def test_scores_below_the_lowest_float_are_none():
     import torch
 
