@@ -188,8 +188,8 @@ size_t pb_op_beam_select_workspace(int32_t B, int32_t W, int32_t V);
  * short_of[0]: how many pages are missing; if any is, no row grows or copies
  * (out_lens = out_start).  short_of[1]: rows that would pass the table's width;
  * they do not grow.  Table entries past a row's pages are -1.
- * tables, out_tables: [rows][width], contiguous.  Outputs must not overlap the
- * inputs.  grow = 0 keeps, parents = -1 frees, an empty row with grow = T is a new
+ * tables, out_tables: [rows][width], contiguous.  Outputs and workspace must not
+ * overlap the inputs or each other.  grow = 0 keeps, parents = -1 frees, an empty row with grow = T is a new
  * prompt's.  At most 65535 rows, and rows x layers x pieces of 32 KB of a page below
  * 2^31; workspace: pb_op_page_fork_workspace bytes.  A refused call writes nothing. */
 int pb_op_page_fork(int32_t dtype, const pb_kv_pool* pool, int32_t n_layers, int64_t layer_stride,

@@ -201,6 +201,9 @@ extern "C" int pb_op_page_fork(int32_t dtype, const pb_kv_pool* pool, int32_t n_
     for (const auto& i : ins)
         for (const auto& o : outs)
             if (overlap(i.p, i.n, o.p, o.n)) return refuse("%s: an output overlaps an input", op);
+    for (const auto& o : outs)  // (some are read again: places in the tables come from out_start)
+        for (const auto* other = &o + 1; other < outs + sizeof(outs) / sizeof(outs[0]); ++other)
+            if (overlap(o.p, o.n, other->p, other->n)) return refuse("%s: two outputs overlap, or one the workspace", op);
     p.n_layers = n_layers; p.layer_stride = layer_stride; p.parents = parents; p.out_rows = out_rows;
     p.tables = tables; p.width = width; p.lens = lens; p.in_rows = in_rows; p.refs = refs; p.grow = grow;
     p.out_tables = out_tables; p.out_start = out_start; p.out_lens = out_lens; p.out_refs = out_refs;

@@ -107,6 +107,15 @@ def test_fork_refusals(bad):
     _refused(pb, _fork(pb, _pool(pb), **bad), bad)
 
 
+@pytest.mark.parametrize("bad", [dict(ol=0x700000), dict(os=0x60007c), dict(orf=0x600000), dict(short=0x80000c),
+                                 dict(short=0x6ffffc), dict(ws=0x900020)], ids=str)
+def test_fork_outputs_that_overlap(bad):
+    from paper_2503_17707_amd import binding as pb
+
+    _refused(pb, _fork(pb, _pool(pb), **bad), bad)
+    assert "overlap" in pb.lib().pb_last_error().decode()
+
+
 def test_fork_of_more_copies_than_a_launch_takes():
     from paper_2503_17707_amd import binding as pb
 
