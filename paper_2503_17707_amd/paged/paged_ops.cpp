@@ -133,6 +133,12 @@ extern "C" int pb_op_paged_attention(int32_t dtype, const void* q, int64_t ld_q,
                       op, (long long)ld_q, (long long)ld_out, (long long)cols);
     if (!lens) return refuse("%s: lens is NULL", op);
     if (workspace && !aligned(workspace, 16)) return refuse("%s: workspace must be 16-byte aligned", op);
+    const size_t rows = (size_t)n_seqs - 1;
+    if (overlap(workspace, workspace_bytes, q, (rows * ld_q + cols) * 2) ||
+        overlap(workspace, workspace_bytes, out, (rows * ld_out + cols) * 2) ||
+        overlap(workspace, workspace_bytes, lens, (size_t)n_seqs * 4) ||
+        overlap(workspace, workspace_bytes, tables, (rows * ld_tables + width) * 4))
+        return refuse("%s: the workspace overlaps an operand", op);
     p.q = (const uint16_t*)q; p.ld_q = ld_q; p.out = (uint16_t*)out; p.ld_out = ld_out;
     p.tab = {tables, ld_tables, width, n_seqs};
     p.lens = lens; p.n_heads = n_heads; p.scale = scale; p.window = window; p.shared = shared != 0;

@@ -85,6 +85,16 @@ def test_attention_refusals(bad):
     _refused(pb, _attend(pb, _pool(pb), **bad), bad)
 
 
+@pytest.mark.parametrize("bad", [dict(ws=P), dict(q=0x20000, ws=0x207f0), dict(out=0x20000, ws=0x1fff0),
+                                 dict(out=0x20000, ld_out=1024, ws=0x20800), dict(lens=0x20004, ws=0x20000),
+                                 dict(tables=0x20000, ld=400, ws=0x20640)], ids=str)
+def test_attention_workspace_over_an_operand(bad):
+    from paper_2503_17707_amd import binding as pb
+
+    _refused(pb, _attend(pb, _pool(pb), **bad), bad)
+    assert "overlap" in pb.lib().pb_last_error().decode()
+
+
 @pytest.mark.parametrize("bad", [dict(logits=None), dict(logits=P + 2), dict(ld=99), dict(scores=None), dict(alive=None),
                                  dict(B=-1), dict(B=65536), dict(W=0), dict(W=33), dict(V=0), dict(V=(1 << 20) + 1, ld=1 << 21), dict(eos=-2),
                                  dict(eos=100), dict(pad=-1), dict(pad=100), dict(o=(None, P, P, P)), dict(o=(P, P, P, None)),
