@@ -52,6 +52,7 @@ struct PagedAttentionParams {
     void* ws; size_t ws_bytes;
 };
 size_t paged_attention_workspace(int n_seqs, int n_heads, int n_kv_heads, int hd, int width, int page_size);
+bool paged_attention_fits(int n_seqs, int n_heads, int n_kv_heads);  // a launch holds its blocks
 hipError_t launch_paged_attention(int dtype, const PagedAttentionParams& p, hipStream_t s);
 
 struct BeamParams {

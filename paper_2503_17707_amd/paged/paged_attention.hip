@@ -709,8 +709,7 @@ hipError_t launch(const PagedAttentionParams& p, hipStream_t s) {
         cut.qb = qb1;
         hb = p.pool.n_kv_heads * qb1;
     }
-    const int64_t blocks = (items * p.pool.n_kv_heads + 7) / 8 * 8 * cut.qb;
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+    const int64_t blocks = (items * p.pool.n_kv_heads + 7) / 8 * 8 * cut.qb;  // (paged_attention_fits)
     const dim3 grid((unsigned)blocks);
     if (cut.list) PB_LAUNCH(paged_cut_kernel, dim3(1), dim3(1024), 0, s, p, cut, hb);
     // Few uncut blocks: eight waves each (8 sequences of 1000, 32 heads of 64: 14.1 us,
@@ -737,6 +736,13 @@ size_t paged_attention_workspace(int n_seqs, int n_heads, int n_kv_heads, int hd
     const int group = n_heads / n_kv_heads, nq = group <= 16 ? 1 : 2;
     const int64_t most = most_pieces(n_seqs, n_kv_heads * ((group + 16 * nq - 1) / (16 * nq)), (int64_t)width * page_size);
     return most > n_seqs ? cut_bytes(n_seqs, most, n_heads, hd) : 0;
+}
+
+// Threads of a launch are counted in 32 bits: 2^24 blocks of 256.  Pieces add PIECES
+// blocks at most, and blocks of 16 heads are the most there are.
+bool paged_attention_fits(int n_seqs, int n_heads, int n_kv_heads) {
+    const int64_t qb = (n_heads / n_kv_heads + 15) / 16;
+    return ((int64_t)n_seqs * n_kv_heads + 8) * qb + PIECES < 1 << 24;
 }
 
 hipError_t launch_paged_attention(int dtype, const PagedAttentionParams& p, hipStream_t s) {

@@ -127,6 +127,8 @@ extern "C" int pb_op_paged_attention(int32_t dtype, const void* q, int64_t ld_q,
     if (window < 0 || !(scale - scale == 0.f)) return refuse("%s: window=%d scale=%g", op, window, (double)scale);
     if ((int64_t)width * pool->page_size > (1 << 30)) return refuse("%s: tables of more than 2^30 tokens a row", op);
     if (n_seqs == 0) return PB_OK;
+    if (!pb::paged_attention_fits(n_seqs, n_heads, pool->n_kv_heads))
+        return refuse("%s: %d sequences of %d heads on %d: more blocks than a launch takes", op, n_seqs, n_heads, pool->n_kv_heads);
     const int64_t cols = (int64_t)n_heads * pool->head_dim;
     if (!rows_ok(q, ld_q, n_seqs, cols) || !rows_ok(out, ld_out, n_seqs, cols))
         return refuse("%s: q and out must be 16-byte aligned, row strides (%lld, %lld) multiples of 8 and at least %lld",
