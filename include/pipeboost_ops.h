@@ -139,8 +139,8 @@ int pb_op_kv_append(int32_t dtype, const void* k, int64_t ld_k, const void* v, i
  * workspace (may be NULL): fp32 partial results of the pieces that long
  * sequences are cut into, pb_op_paged_attention_workspace bytes; with a smaller one
  * they are not cut.  It must not overlap the other operands.  Tables hold at most 2^30
- * tokens a row; sequences x blocks of up to 16 heads of one key/value head stay below
- * 2^24 - 4096 (65535 sequences of 255 heads do). */
+ * tokens a row; sequences x key/value heads (of more than 32 heads each: x
+ * blocks of 32) stay below 2^24 - 8. */
 int pb_op_paged_attention(int32_t dtype, const void* q, int64_t ld_q, const pb_kv_pool* pool,
                           const int32_t* tables, int32_t width, int64_t ld_tables, const int32_t* lens,
                           int32_t n_seqs, int32_t n_heads, float scale, int32_t window, int32_t shared,

@@ -666,6 +666,10 @@ int64_t most_pieces(int rows, int hb, int64_t longest) {
     return a < b ? a : b;
 }
 
+// Blocks of a launch; its threads are counted in 32 bits, 256 to a block.
+constexpr int64_t MOST_BLOCKS = 1 << 24;
+int64_t grid_blocks(int64_t items, int n_kv_heads, int qb) { return (items * n_kv_heads + 7) / 8 * 8 * qb; }
+
 // The cut and the list of pieces (multiples of 16 bytes), their partial results.
 size_t at_bytes(int rows) { return ((size_t)rows * 8 + 15) / 16 * 16; }
 size_t list_bytes(int rows, int64_t pieces) { return rows > LISTED ? (size_t)pieces * 16 : 0; }
@@ -690,7 +694,8 @@ hipError_t launch(const PagedAttentionParams& p, hipStream_t s) {
     // (32 blocks of 600: 9.9, of 1000 13.9; cut 10.1 and 11.5; 128 of 1000: 17.3, cut 19.8).
     const int64_t whole = (int64_t)p.tab.rows * hb;
     const int uncut = HD == 64 ? (whole >= 256 ? 2048 : 1024) : (whole >= 64 ? 1024 : 640);
-    if (longest > uncut && most > p.tab.rows && p.ws && p.ws_bytes >= cut_bytes(p.tab.rows, most, p.n_heads, HD)) {
+    if (longest > uncut && most > p.tab.rows && grid_blocks(most, p.pool.n_kv_heads, cut.qb) < MOST_BLOCKS && p.ws &&
+        p.ws_bytes >= cut_bytes(p.tab.rows, most, p.n_heads, HD)) {
         cut.on = 1;
         cut.most = (int)most;
         cut.at = (int32_t*)p.ws;
@@ -709,8 +714,7 @@ hipError_t launch(const PagedAttentionParams& p, hipStream_t s) {
         cut.qb = qb1;
         hb = p.pool.n_kv_heads * qb1;
     }
-    const int64_t blocks = (items * p.pool.n_kv_heads + 7) / 8 * 8 * cut.qb;  // (paged_attention_fits)
-    const dim3 grid((unsigned)blocks);
+    const dim3 grid((unsigned)grid_blocks(items, p.pool.n_kv_heads, cut.qb));
     if (cut.list) PB_LAUNCH(paged_cut_kernel, dim3(1), dim3(1024), 0, s, p, cut, hb);
     // Few uncut blocks: eight waves each (8 sequences of 1000, 32 heads of 64: 14.1 us,
     // four 16.4); cut ones have little to share out.
@@ -738,11 +742,9 @@ size_t paged_attention_workspace(int n_seqs, int n_heads, int n_kv_heads, int hd
     return most > n_seqs ? cut_bytes(n_seqs, most, n_heads, hd) : 0;
 }
 
-// Threads of a launch are counted in 32 bits: 2^24 blocks of 256.  Pieces add PIECES
-// blocks at most, and blocks of 16 heads are the most there are.
 bool paged_attention_fits(int n_seqs, int n_heads, int n_kv_heads) {
-    const int64_t qb = (n_heads / n_kv_heads + 15) / 16;
-    return ((int64_t)n_seqs * n_kv_heads + 8) * qb + PIECES < 1 << 24;
+    const int group = n_heads / n_kv_heads, nq = group <= 16 ? 1 : 2;
+    return grid_blocks(n_seqs, n_kv_heads, (group + 16 * nq - 1) / (16 * nq)) < MOST_BLOCKS;
 }
 
 hipError_t launch_paged_attention(int dtype, const PagedAttentionParams& p, hipStream_t s) {

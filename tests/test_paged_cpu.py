@@ -89,9 +89,9 @@ def test_attention_of_more_blocks_than_a_launch_takes():
     from paper_2503_17707_amd import binding as pb
 
     far = dict(q=1 << 50, out=1 << 51, ld_q=1 << 16, ld_out=1 << 16, tables=1 << 44, lens=1 << 43, ws=None)
-    for H, Hkv in ((256, 256), (4080, 255), (65520, 4), (1024, 128)):
+    for H, Hkv in ((256, 256), (257, 257), (4096, 256), (8192, 256), (8448, 256), (65520, 4), (1024, 128)):
         pool = _pool(pb, n_kv_heads=Hkv)
-        fits = 65535 * Hkv * -(-(H // Hkv) // 16) < (1 << 24) - 4096
+        fits = 65535 * Hkv * -(-(H // Hkv) // 32) < (1 << 24) - 8
         rc = _attend(pb, pool, S=65535, H=H, **dict(far, ld_q=H * 64, ld_out=H * 64, lens=None if fits else far["lens"]))
         _refused(pb, rc, (H, Hkv))
         assert ("lens" if fits else "blocks") in pb.lib().pb_last_error().decode(), (H, Hkv)
