@@ -15,19 +15,19 @@
 //    registers are free the next tile's loads are issued.  (Two tiles ahead: no
 //    faster for few blocks, 10% slower for many, which then hold fewer waves.)
 //    Values are read once and by whole lines, so they bypass what caches may keep
-//    (131071 tokens: 98.5 us against 107); a line of keys is read in two halves.
+//    (131071 tokens: 97 us against 104); a line of keys is read in two halves.
 //    Where rows share pages, as beams do, caches serve most reads and are used (4
-//    prompts of 1000 with 8 beams each, 32 heads of 64: 27.7 us against 32.4; the same
-//    rows on pages of their own: 61.4 against 54.5).
+//    prompts of 1000 with 8 beams each, 32 heads of 64: 28.1 us against 32.7; the same
+//    rows on pages of their own: 62.6 against 57.6).
 //  - Sequences are cut into pieces, at most as long as a length chosen on the device
 //    from the call's lengths (which may change between replays of a recorded launch),
 //    so that about PIECES blocks of like work cover a ragged batch as well as one long
 //    sequence.  A second launch joins the pieces of sequences that have several; of many
 //    sequences one ahead lists the pieces.
 //
-// Measured: 131071 tokens, 32 heads on 8 of 128 (537 MB) 96 us, 5.6 TB/s; 48 ragged
-// sequences up to 16384, 64 heads on 8 (368 MB) 74 us, 5.0 TB/s; 32 ragged up to 2048,
-// 40 heads (198 MB) 45 us, 4.4 TB/s; a 4 GiB copy reaches 4.7 TB/s on this card.
+// Measured, the join with it: 131071 tokens, 32 heads on 8 of 128 (537 MB) 97 us, 5.5
+// TB/s; 48 ragged sequences up to 16384, 64 heads on 8 (368 MB) 74 us, 5.0 TB/s; 32 ragged
+// up to 2048, 40 heads (198 MB) 45.7 us, 4.3 TB/s; a 4 GiB copy reaches 4.7 TB/s on this card.
 #include "common.h"
 #include "paged.h"
 
@@ -41,13 +41,13 @@ constexpr float LOG2E = 1.4426950408889634f;
 template <int NQ> constexpr int tile_of() { return NQ == 1 ? 16 : 32; }
 constexpr int IDS = 512;      // pages whose places are held in LDS at a time
 // Pieces (us for 48 ragged sequences up to 16384, 64 heads on 8 of 128 | one of 131071,
-// 32 on 8 | 8 of 2048, 40 heads of 128): for 1024 blocks 78.0 | 99.0 | 67.4, for 2048
-// 73.9 | 96.3 | 67.5.
+// 32 on 8 | 8 of 2048, 40 heads of 128): for 1024 blocks 77.0 | 99.5 | 67.9, for 2048
+// 73.8 | 96.9 | 68.0.
 constexpr int PIECES = 2048;  // blocks aimed at
 // No piece is shorter than SHORTEST tokens, nor than LEAST once the blocks of such
 // pieces number more than 512: what a block does before its first tile costs as much
-// as some 100 tokens.  5 sequences of 1714, 64 heads on 8 of 128: 128 tokens 15.4 us,
-// 256 19.8; 32 of 303, 40 heads of 128: 256 54 us, 512 47.
+// as some 100 tokens.  5 sequences of 1714, 64 heads on 8 of 128: 128 tokens 15.7 us,
+// 256 16.2; 32 of 303, 40 heads of 128 in tables of 2080: 256 49.9 us, 512 42.4.
 constexpr int SHORTEST = 128, LEAST = 512, FEW_BLOCKS = 512;
 
 // How a call is cut: written to the workspace by the first block, or by a launch before
@@ -295,7 +295,7 @@ void paged_attention_kernel(PagedAttentionParams p, Cut cut) {
     const int group = p.n_heads / p.pool.n_kv_heads;
     const int hb = p.pool.n_kv_heads * cut.qb;
     // blocks that share keys and values run on one XCD, and its L2 holds them: every
-    // eighth block does (4 sequences of 30000, 71 heads on one: 39.5 us; neighbouring blocks: 44.3)
+    // eighth block does (4 sequences of 30000, 71 heads on one: 36.4 us; neighbouring blocks: 43.6)
     const int unit = blockIdx.x / (8 * cut.qb) * 8 + blockIdx.x % 8;  // (piece, key/value head)
     const int kvh = unit % p.pool.n_kv_heads, q0 = (int)(blockIdx.x / 8 % cut.qb) * 16 * NQ;
     const int item = unit / p.pool.n_kv_heads;
@@ -688,10 +688,10 @@ hipError_t launch(const PagedAttentionParams& p, hipStream_t s) {
     const int64_t held = (int64_t)p.tab.width * p.pool.page_size;
     const int64_t longest = p.window > 0 && p.window < held ? p.window : held;  // that is attended to
     const int64_t most = most_pieces(p.tab.rows, hb, longest);
-    // Short sequences stay whole: the join costs 4 us (one of 513, 32 heads of 64: 6.3
-    // us, cut 9.4), and so do longer ones that fill the chip as they are (8 of 1000: 14.1,
-    // cut 18.5; one of 2000: 11.2 cut, 16.7 whole).  With heads of 128 a few blocks take longer
-    // (32 blocks of 600: 9.9, of 1000 13.9; cut 10.1 and 11.5; 128 of 1000: 17.3, cut 19.8).
+    // Short sequences stay whole: the join costs 4 us (one of 513, 32 heads of 64: 6.8
+    // us, cut 9.3), and so do longer ones that fill the chip as they are (8 of 1000: 14.2,
+    // cut 18.6; one of 2000: 11.7 cut, 18.1 whole).  With heads of 128 a few blocks take longer
+    // (32 blocks of 600: 10.5, of 1000 16.5; cut 10.6 and 12.2; 128 of 1000: 18.4, cut 19.8).
     const int64_t whole = (int64_t)p.tab.rows * hb;
     const int uncut = HD == 64 ? (whole >= 256 ? 2048 : 1024) : (whole >= 64 ? 1024 : 640);
     if (longest > uncut && most > p.tab.rows && grid_blocks(most, p.pool.n_kv_heads, cut.qb) < MOST_BLOCKS && p.ws &&
@@ -707,7 +707,7 @@ hipError_t launch(const PagedAttentionParams& p, hipStream_t s) {
     }
     // Whole sequences of more than 16 heads to a key/value head that leave the chip mostly
     // idle: more blocks of 16 heads, on the caches (12 ragged of 662, 71 heads on one of
-    // 128: 11.0 us, 14.6 with 32; 100 of 500 would be 500 blocks: 14.3 us against 11.7).
+    // 128: 11.1 us, 15.7 with 32; 100 of 500 would be 500 blocks: 26.7 us against 20.8).
     const int qb1 = (group + 15) / 16;
     if (nq == 2 && !cut.on && items * p.pool.n_kv_heads * qb1 <= 256) {
         nq = 1;
@@ -716,8 +716,8 @@ hipError_t launch(const PagedAttentionParams& p, hipStream_t s) {
     }
     const dim3 grid((unsigned)grid_blocks(items, p.pool.n_kv_heads, cut.qb));
     if (cut.list) PB_LAUNCH(paged_cut_kernel, dim3(1), dim3(1024), 0, s, p, cut, hb);
-    // Few uncut blocks: eight waves each (8 sequences of 1000, 32 heads of 64: 14.1 us,
-    // four 16.4); cut ones have little to share out.
+    // Few uncut blocks: eight waves each (8 sequences of 1000, 32 heads of 64: 14.2 us,
+    // four 17.0); cut ones have little to share out.
     if (nq == 1 && !cut.on && items * hb < 512)
         PB_LAUNCH((paged_attention_kernel<T, HD, 1, 8, SHARED>), grid, dim3(512), 0, s, p, cut);
     else if (nq == 1) PB_LAUNCH((paged_attention_kernel<T, HD, 1, 4, SHARED>), grid, dim3(256), 0, s, p, cut);
@@ -729,7 +729,7 @@ hipError_t launch(const PagedAttentionParams& p, hipStream_t s) {
 template <typename T, int HD>
 hipError_t launch_shared(const PagedAttentionParams& p, hipStream_t s) {
     // more than 32 heads to a key/value head: several blocks read the same values too
-    // (4 sequences of 30000, 71 heads on one: 35.4 us against 38.7)
+    // (4 sequences of 30000, 71 heads on one: 36.4 us against 39.9)
     const bool shared = p.shared || p.n_heads / p.pool.n_kv_heads > 32;
     return shared ? launch<T, HD, true>(p, s) : launch<T, HD, false>(p, s);
 }

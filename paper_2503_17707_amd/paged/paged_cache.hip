@@ -59,8 +59,8 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendParams p, int rpb,
 //  4 copies: the tokens of every page copied, in every layer
 // Copying bounds large calls, the chain of launches and dependent reads small ones:
 // up to SMALL_PAGES pages and SMALL_ENTRIES table entries one block takes steps 1
-// to 3 with the counts in LDS (256 rows of 22 pages in 1300: 53.5 us with the copies,
-// 57.9 the other way; 256 rows of 96: 17.5 against 16.2).
+// to 3 with the counts in LDS (256 rows of 22 pages in 1300: 53 us with the copies,
+// 57 the other way; 256 rows of 96: 17.4 against 16.1).
 
 constexpr int SMALL_PAGES = 8192, SMALL_ROWS = 512, SMALL_ENTRIES = 16384;
 
@@ -328,8 +328,9 @@ __global__ __launch_bounds__(1024) void fork_places_kernel(ForkParams p, FastDiv
 // The copies' tokens (not their pages), PIECE 16-byte chunks of one in one layer to
 // a block at a time, eight steps of a thread in flight; as many blocks as the chip
 // holds take the pieces in turn, since how many copies there are is not known here.
-// 80 copies of 6 tokens in 24 layers of 32 heads of 64 (200 MB read and written): 41
-// us, 4.8 TB/s; with ordinary stores 52, a block to a row and layer 61.
+// Some 80 copies of 6 tokens in 24 layers of 32 heads of 64 (rows of one parent copy the
+// same page, which is read from memory once: 75 MB in, 100 out): 45 to 46 us, 3.8 TB/s;
+// the call 53, with ordinary stores 62.
 constexpr int PIECE = 8 * 256, COPY_BLOCKS = 1024;
 __global__ __launch_bounds__(256) void fork_copy_kernel(ForkParams p, FastDiv heads, FastDiv layers, FastDiv pieces,
                                                         bool by_token) {
