@@ -196,6 +196,114 @@ def test_recorded_step_equals_eager():
     assert max(live) > 700
 
 
+@pytest.mark.parametrize("dtype,hd", [("f16", 64), ("bf16", 128)])
+def test_a_decoder_over_pages_matches_the_oracle(dtype, hd):
+    """Prompts of two lengths and three tokens more, layer by layer through the single-kernel entry
+    points, the cache in pages: each step's logits and tokens are the oracle's of the prompt so far."""
+    import torch
+
+    import oracle
+    import synth
+    from gpu_common import compare
+    from paper_2503_17707_amd import binding as pb
+
+    log("decoder over pages", dtype, hd)
+    w = synth.Workload(name="paged", seed=51, n_layers=2, d_model=256, n_heads=256 // hd, d_ffn=512, vocab=900, max_pos=64,
+                       dtype=dtype, batch=2, seq_len=29, n_adapters=0)
+    code, dt = (pb.PB_F16, torch.float16) if dtype == "f16" else (pb.PB_BF16, torch.bfloat16)
+    d, H, L = 256, 256 // hd, 2
+    get = lambda l, n: torch.from_numpy(synth.base_tensor(w, l, n, dtype).view(np.int16)).view(dt).cuda()  # noqa: E731
+    G = {n: get(-1, n) for n in synth.GLOBAL_TENSORS}
+    layers = [{n: get(l, n) for n in synth.LAYER_TENSORS} for l in range(L)]
+    for x in layers:
+        x["wqkv"], x["bqkv"] = torch.cat([x["wq"], x["wk"], x["wv"]]), torch.cat([x["bq"], x["bk"], x["bv"]])
+    lens, ps, n_pages, B = [12, 29], 16, 7, 2
+    i32 = dict(dtype=torch.int32, device="cuda")
+    pools = torch.full((L, n_pages, ps, 2, H, hd), float("nan"), dtype=dt, device="cuda").permute(0, 1, 3, 4, 2, 5)
+    ws = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+    state = [torch.full((B, 4), -1, **i32), torch.zeros(B, **i32), torch.zeros(n_pages, **i32)]  # tables, lens, refs
+
+    def forward(rows, grow, attend):
+        """Appends rows [n, d] of new tokens (fp32), sequence after sequence; their last hidden states."""
+        new = [torch.empty((B, 4), **i32), torch.empty(B, **i32), torch.empty(n_pages, **i32)]
+        start, short = torch.empty(B, **i32), torch.empty(2, **i32)
+        pb.op_page_fork(code, pools, torch.arange(B, **i32), *state, torch.tensor(grow, **i32), new[0], start, new[1], new[2],
+                        short, ws)
+        assert short.tolist() == [0, 0]
+        state[:] = new
+        n, row0 = len(rows), torch.tensor([0, grow[0]], **i32)
+        h, a = torch.empty((n, d), dtype=dt, device="cuda"), torch.empty((n, d), dtype=dt, device="cuda")
+        qkv, f = torch.empty((n, 3 * d), dtype=dt, device="cuda"), torch.empty((n, 512), dtype=dt, device="cuda")
+        for l, x in enumerate(layers):
+            pb.op_layernorm(code, rows, x["ln1_g"], x["ln1_b"], h)
+            pb.op_gemm(code, 0, h, x["wqkv"], x["bqkv"], C=qkv, qscale=hd ** -0.5, qcols=d)
+            q, k, v = (qkv[:, i * d:(i + 1) * d].unflatten(1, (H, hd)) for i in range(3))
+            pb.op_kv_append(code, k, v, pools[l], state[0], start, state[1], row0=row0)
+            attend(l, qkv, q, a)
+            pb.op_gemm(code, 2, a, x["wo"], x["bo"], R=rows)
+            pb.op_layernorm(code, rows, x["ln2_g"], x["ln2_b"], h)
+            pb.op_gemm(code, 1, h, x["w1"], x["b1"], C=f)
+            pb.op_gemm(code, 2, f, x["w2"], x["b2"], R=rows)
+        last = rows[torch.tensor([grow[0] - 1, n - 1], device="cuda")].contiguous()
+        out = torch.empty((B, d), device="cuda")
+        pb.op_layernorm(code, last, G["lnf_g"], G["lnf_b"], out)
+        return torch.matmul(out, G["embed"].float().t().contiguous())
+
+    def prompt(l, qkv, q, a):
+        for i, (lo, hi) in enumerate(((0, lens[0]), (lens[0], sum(lens)))):
+            pb.op_attention(code, qkv[lo:hi], a[lo:hi], 1, hi - lo, H, hd)
+
+    def step(l, qkv, q, a):
+        pb.op_paged_attention(code, q, pools[l], state[0], state[1], a.unflatten(1, (H, hd)), workspace=ws)
+
+    seqs = [t[:n].tolist() for t, n in zip(synth.tokens(w), lens)]
+    embed = lambda ids, pos: G["embed"].float()[torch.tensor(ids)] + G["pos"].float()[torch.tensor(pos)]  # noqa: E731
+    logits = forward(embed(sum(seqs, []), [*range(lens[0]), *range(lens[1])]), lens, prompt)
+    alive, scores = torch.ones((B, 1), **i32), torch.zeros((B, 1), device="cuda")
+    for k in range(4):
+        tokens, parents = torch.empty((B, 1), **i32), torch.empty((B, 1), **i32)
+        pb.op_beam_select(logits, scores, alive, scores, tokens, parents, alive, eos=-1, pad=0, workspace=ws)
+        for b in range(B):
+            one = w.with_(batch=1, seq_len=len(seqs[b]))
+            ref, ref_token = oracle.prefill_first_token(one, np.array([seqs[b]], np.int32))
+            compare("step %d sequence %d" % (k, b), logits[b:b + 1].cpu().numpy(), [int(tokens[b])], ref, ref_token)
+            seqs[b].append(int(tokens[b]))
+        if k < 3:
+            logits = forward(embed([s[-1] for s in seqs], [len(s) - 1 for s in seqs]), [1, 1], step)
+    assert state[1].tolist() == [n + 3 for n in lens]
+
+
+def test_a_recorded_call_of_many_sequences():
+    """One recorded launch of 200 sequences whose lengths change between replays: more pieces and
+    fewer, none, and rows past their table."""
+    import torch
+
+    from paged_common import dev, make_pool
+    from paper_2503_17707_amd import binding as pb
+
+    log("recorded paged attention of many sequences")
+    S, ps, pages = 200, 16, 256
+    rs = np.random.RandomState(1)
+    pool = make_pool(0, "f16", (pages,), 1, ps, 64, "heads")
+    tables = dev(np.stack([rs.permutation(pages) for _ in range(S)]).astype(np.int32))
+    q = torch.randn((S, 2, 64), generator=torch.Generator().manual_seed(1)).half().cuda()
+    lens, out, eager = torch.zeros(S, dtype=torch.int32, device="cuda"), torch.empty_like(q), torch.empty_like(q)
+    ws = torch.full((pb.paged_attention_workspace(S, 2, pool, pages),), 255, dtype=torch.uint8, device="cuda")
+    run = lambda o: pb.op_paged_attention(1, q, pool, tables, lens, o, scale=0.125, workspace=ws)  # noqa: E731
+    run(out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(out)
+    for most in (4096, 30, 4097, 1, 0, 3000, 4096):
+        lens.copy_(torch.from_numpy(rs.randint(0, most + 1, S).astype(np.int32)))
+        run(eager)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out.nan_to_num(7), eager.nan_to_num(7)), most
+        assert torch.isnan(out).flatten(1).all(1).tolist() == (lens > 4096).tolist()
+        assert torch.all(out[lens == 0] == 0)
+
+
 def test_the_readme_s_step_runs():
     """The step as the README shows it: scores, parents and alive [prompts, beams], q scaled."""
     import os
