@@ -201,6 +201,59 @@ int pb_op_page_fork(int32_t dtype, const pb_kv_pool* pool, int32_t n_layers, int
                     int32_t* short_of, void* workspace, size_t workspace_bytes, void* stream);
 size_t pb_op_page_fork_workspace(int32_t out_rows, int32_t n_pages);
 
+/* ---- linear layers in 8 bits ------------------------------------------------
+ *
+ * Rows of 8-bit integers with an fp32 scale each: activations per token, weights
+ * per output channel.  pb_op_quant_q8 makes them (of weights once), pb_op_norm_q8
+ * makes a norm's in the pass that adds a layer's output to the residual stream,
+ * pb_op_gemm_q8 multiplies them.  A layer runs norm_q8, gemm_q8 (q, k, v),
+ * attention, quant_q8, gemm_q8 (o, onto the stream), norm_q8, gemm_q8 (fc1),
+ * quant_q8, gemm_q8 (fc2).  Calls only enqueue kernels, allocate nothing and can be
+ * captured into a HIP graph; every buffer and the stream belong to the current
+ * device; outputs must not overlap inputs or each other, but where said.
+ *
+ * A row y in 8 bits: scale = max |y| / 127 as fp32, q = y / scale to the nearest
+ * integer, ties to even.  (Formed in fp64 from the operands as they are stored:
+ * neither order nor launch shape shows.)  A row whose scale would be below 2^-126
+ * is one of zeros: scale 0, q 0.  A row with a NaN, an infinity or a scale past the
+ * largest float: scale NaN, q 0, so that its products are NaN.  Row strides are in
+ * elements; that of a single row is not used. */
+
+/* The residual's addition, the norm and its 8 bits: per row of d elements
+ *   s = x + delta              (fp32, rounded to x's type; delta NULL: s = x)
+ *   y = s / sqrt(mean(s^2) + eps) g + b                       (layer = 0: RMS)
+ *   y = (s - mean(s)) / sqrt(mean((s - mean(s))^2) + eps) g + b    (layer != 0)
+ * x and sum fp32 (x_f32 != 0) or dt, delta, g, b [d] and out dt.  sum (NULL: not
+ * kept; may be x, with its stride) gets s, out (may be NULL) y, q and scale (may both
+ * be NULL) y in 8 bits, formed before out's rounding.  b may be NULL.
+ * 1 <= d <= 16384; any strides of at least d. */
+int pb_op_norm_q8(int32_t dtype, int32_t layer, const void* x, int64_t ld_x, int32_t x_f32, const void* delta,
+                  int64_t ld_delta, void* sum, int64_t ld_sum, const void* g, const void* b, float eps,
+                  void* out, int64_t ld_out, int8_t* q, int64_t ld_q, float* scale, int32_t rows, int32_t d,
+                  void* stream);
+
+/* Rows of x (fp32 where x_f32 != 0, else dt) in 8 bits.  1 <= cols <= 2^30. */
+int pb_op_quant_q8(int32_t dtype, const void* x, int64_t ld_x, int32_t x_f32, int8_t* q, int64_t ld_q,
+                   float* scale, int32_t rows, int32_t cols, void* stream);
+
+/* Y[m, n] = sx[m] sw[n] sum_k X[m, k] W[n, k] + bias[n], the sum exact in 32 bits,
+ * with the epilogues of pb_op_gemm and one that stores fp32:
+ *   epi 0: C = dt(Y * (n < qcols ? qscale : 1))
+ *   epi 1: C = dt(max(Y, 0))
+ *   epi 2: R += Y
+ *   epi 3: R = Y                                             (logits)
+ * bias [N] dt or NULL; C dt or R fp32 [M, N] with row stride ldo.  X and W hold any
+ * 8-bit integers; both 16-byte aligned, row strides multiples of 16 up to 2^23.
+ * K is a multiple of 16, at most 131056; any M and N whose tiles of 64 x 64 stay
+ * below 2^23.  workspace (may be NULL): partial sums where K is split, up to
+ * pb_op_gemm_q8_workspace bytes (0 for refused sizes); results do not depend on it.
+ * It carries nothing from one call to the next. */
+int pb_op_gemm_q8(int32_t dtype, int32_t epi, const int8_t* X, int64_t ldx, const float* sx, const int8_t* W,
+                  int64_t ldw, const float* sw, const void* bias, void* C, float* R, int64_t ldo, int32_t M,
+                  int32_t N, int32_t K, float qscale, int32_t qcols, void* workspace, size_t workspace_bytes,
+                  void* stream);
+size_t pb_op_gemm_q8_workspace(int32_t M, int32_t N, int32_t K);
+
 #ifdef __cplusplus
 }
 #endif

@@ -168,6 +168,17 @@ _SIGS = {
                                        ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
                                        ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     "pb_op_page_fork_workspace": (ctypes.c_size_t, [ctypes.c_int32, ctypes.c_int32]),
+    "pb_op_norm_q8": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32,
+                                     ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                     ctypes.c_void_p, ctypes.c_float, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                     ctypes.c_int64, ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p]),
+    "pb_op_quant_q8": (ctypes.c_int, [ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p,
+                                      ctypes.c_int64, ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p]),
+    "pb_op_gemm_q8": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                     ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                     ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                                     ctypes.c_float, ctypes.c_int32, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "pb_op_gemm_q8_workspace": (ctypes.c_size_t, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32]),
 }
 
 _lib = None
@@ -901,5 +912,122 @@ def op_page_fork(dtype: int, pools, parents, tables, lens, refs, grow, out_table
                                tables.data_ptr(), width, lens.data_ptr(), S, refs.data_ptr(), grow.data_ptr(),
                                out_tables.data_ptr(), out_start.data_ptr(), out_lens.data_ptr(), out_refs.data_ptr(),
                                short_of.data_ptr(), _ptr(workspace), _nbytes(workspace), _stream(stream))
+    if rc:
+        check(rc)
+
+
+# ---- linear layers in 8 bits ------------------------------------------------------
+# 8-bit rows are int8 [rows, cols] with contiguous rows; their scales float32 [rows].
+
+
+def _checked8(op, stream, dtype, sized, q8, f32):
+    """_checked, and: (name, tensor, shape) of q8 int8 with contiguous rows, of f32 contiguous float32."""
+    torch = _checked(op, stream, dtype, sized, (), [t for _, t, _ in q8] + [t for _, t, _ in f32])
+    for name, t, shape in q8:
+        if t.dtype is not torch.int8 or t.shape != shape or (t.stride(1) != 1 and shape[1] > 1):
+            raise PbError(PB_EINVAL, "%s: %s must be int8 %s with contiguous rows" % (op, name, list(shape)))
+    for name, t, shape in f32:
+        if t.dtype is not torch.float32 or t.shape != shape or not t.is_contiguous():
+            raise PbError(PB_EINVAL, "%s: %s must be contiguous float32 %s" % (op, name, list(shape)))
+    return torch
+
+
+def _rows_of(op, name, t, shape):
+    """Row stride of a matrix with contiguous rows."""
+    if t.shape != shape or (t.stride(1) != 1 and shape[1] > 1):
+        raise PbError(PB_EINVAL, "%s: %s must be %s with contiguous rows" % (op, name, list(shape)))
+    return t.stride(0)
+
+
+def _is_stream(op, dtype, t):
+    """Whether a stream is float32; else it is dtype's type."""
+    import torch
+
+    if t.dtype is torch.float32:
+        return 1
+    if t.dtype is not (torch.float16 if dtype == PB_F16 else torch.bfloat16):
+        raise PbError(PB_EINVAL, "%s: %s operand with dtype %d" % (op, t.dtype, dtype))
+    return 0
+
+
+def op_norm_q8(dtype: int, x, g, q=None, scale=None, delta=None, sum=None, b=None, out=None, layer: bool = False,
+               eps: float = 1e-5, stream=None):
+    """pb_op_norm_q8: x [rows, d] float32 or dtype's type; delta (dtype's type) is added and the sum stored in `sum`
+    (x's type; may be x); its RMS norm (layer: layer norm) with gain g and bias b [d] goes to q int8 [rows, d] with
+    scale float32 [rows], and to out (dtype's type) where given.  Rows may be strided."""
+    op = "op_norm_q8"
+    of = x.shape
+    if len(of) != 2:
+        raise PbError(PB_EINVAL, "%s: x must be [rows, d]" % op)
+    f32 = _is_stream(op, dtype, x)
+    if sum is not None and sum.dtype is not x.dtype:
+        raise PbError(PB_EINVAL, "%s: sum must have x's type" % op)
+    if (q is None) != (scale is None):
+        raise PbError(PB_EINVAL, "%s: q and scale go together" % op)
+    rows, d = of
+    _checked8(op, stream, dtype, [t for t in (g, b, delta, out) if t is not None],
+              () if q is None else (("q", q, of),), () if q is None else (("scale", scale, (rows,)),))
+    dev = g.get_device()
+    for t in (x, sum):
+        if t is not None and t.get_device() != dev:
+            raise PbError(PB_EINVAL, "%s: tensors on %s and on %s" % (op, g.device, t.device))
+    for name, t in (("g", g), ("b", b)):
+        if t is not None and (t.shape != (d,) or not t.is_contiguous()):
+            raise PbError(PB_EINVAL, "%s: %s must be contiguous [%d]" % (op, name, d))
+    lds = [0 if t is None else _rows_of(op, name, t, of)
+           for name, t in (("x", x), ("delta", delta), ("sum", sum), ("out", out))]
+    rc = lib().pb_op_norm_q8(dtype, layer, x.data_ptr(), lds[0], f32, _ptr(delta), lds[1], _ptr(sum), lds[2],
+                             g.data_ptr(), _ptr(b), eps, _ptr(out), lds[3], _ptr(q), 0 if q is None else q.stride(0),
+                             _ptr(scale), rows, d, _stream(stream))
+    if rc:
+        check(rc)
+
+
+def op_quant_q8(dtype: int, x, q, scale, stream=None):
+    """pb_op_quant_q8: x [rows, cols] (float32 or dtype's type) to q int8 [rows, cols] and scale float32 [rows]."""
+    op = "op_quant_q8"
+    of = x.shape
+    if len(of) != 2:
+        raise PbError(PB_EINVAL, "%s: x must be [rows, cols]" % op)
+    f32 = _is_stream(op, dtype, x)
+    rows, cols = of
+    _checked8(op, stream, dtype, (), (("q", q, of),), (("scale", scale, (rows,)),))
+    if x.get_device() != q.get_device():
+        raise PbError(PB_EINVAL, "%s: tensors on %s and on %s" % (op, q.device, x.device))
+    rc = lib().pb_op_quant_q8(dtype, x.data_ptr(), _rows_of(op, "x", x, of), f32, q.data_ptr(), q.stride(0),
+                              scale.data_ptr(), rows, cols, _stream(stream))
+    if rc:
+        check(rc)
+
+
+def gemm_q8_workspace(M: int, N: int, K: int) -> int:
+    """Bytes of workspace with which op_gemm_q8 splits K as it likes."""
+    return lib().pb_op_gemm_q8_workspace(M, N, K)
+
+
+def op_gemm_q8(dtype: int, epi: int, X, sx, W, sw, bias=None, C=None, R=None, qscale: float = 1.0, qcols: int = 0,
+               workspace=None, stream=None):
+    """pb_op_gemm_q8: X int8 [M, K] with sx [M], W int8 [N, K] with sw [N], bias [N] of dtype's type or None; epilogues 0
+    and 1 write C [M, N] (dtype's type), 2 adds to R [M, N] (float32), 3 writes it.  Rows may be strided."""
+    op = "op_gemm_q8"
+    if X.dim() != 2 or W.dim() != 2:
+        raise PbError(PB_EINVAL, "%s: X must be [M, K] and W [N, K]" % op)
+    M, K = X.shape
+    N = W.shape[0]
+    out, ldo = (C, R)[epi >= 2], 0
+    torch = _checked8(op, stream, dtype, [t for t in (bias, None if epi >= 2 else C) if t is not None],
+                      (("X", X, (M, K)), ("W", W, (N, K))), (("sx", sx, (M,)), ("sw", sw, (N,))))
+    if out is not None:
+        ldo = _rows_of(op, "R" if epi >= 2 else "C", out, (M, N))
+        if epi >= 2 and out.dtype is not torch.float32:
+            raise PbError(PB_EINVAL, "%s: R must be float32" % op)
+    for t in (out, workspace):
+        if t is not None and t.get_device() != X.get_device():
+            raise PbError(PB_EINVAL, "%s: tensors on %s and on %s" % (op, X.device, t.device))
+    if bias is not None and (bias.shape != (N,) or not bias.is_contiguous()):
+        raise PbError(PB_EINVAL, "%s: bias must be contiguous [%d]" % (op, N))
+    rc = lib().pb_op_gemm_q8(dtype, epi, X.data_ptr(), X.stride(0), sx.data_ptr(), W.data_ptr(), W.stride(0),
+                             sw.data_ptr(), _ptr(bias), _ptr(C), _ptr(R), ldo, M, N, K, qscale, qcols, _ptr(workspace),
+                             _nbytes(workspace), _stream(stream))
     if rc:
         check(rc)

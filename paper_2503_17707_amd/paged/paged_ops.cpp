@@ -1,35 +1,15 @@
 // Entry points of the paged cache and beam selection (include/pipeboost_ops.h):
 // argument checks, then the launch.
-#include <hip/hip_runtime.h>
-
-#include <cstdarg>
-#include <cstdio>
-
-#include "../../include/pipeboost.h"
 #include "../../include/pipeboost_ops.h"
+#include "../op_checks.h"
 #include "paged.h"
 
-__attribute__((visibility("hidden"))) int pb_fail_status(int code, const char* msg);  // model.cpp
+using pb::aligned;
+using pb::launched;
+using pb::overlap;
+using pb::refuse;
 
 namespace {
-
-int refuse(const char* fmt, ...) {
-    char buf[256];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(buf, sizeof(buf), fmt, ap);
-    va_end(ap);
-    return pb_fail_status(PB_EINVAL, buf);
-}
-
-int launched(const char* op, hipError_t e) {
-    if (e == hipSuccess) return PB_OK;
-    char buf[256];
-    snprintf(buf, sizeof(buf), "%s: launch failed: %s", op, hipGetErrorString(e));
-    return pb_fail_status(PB_EHIP, buf);
-}
-
-bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
 bool sizes_ok(const pb_kv_pool* c) {
     return c && c->n_pages >= 1 && c->n_pages <= (1 << 30) && c->page_size >= 1 && c->page_size <= 4096 && c->n_kv_heads >= 1 &&
@@ -78,10 +58,6 @@ int check_tables(const char* op, const int32_t* tables, int32_t width, int64_t l
 
 bool rows_ok(const void* p, int64_t ld, int64_t rows, int64_t cols) {
     return p && aligned(p, 16) && (rows <= 1 || (ld >= cols && ld % 8 == 0));
-}
-
-bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-    return a && b && na && nb && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
 }
 
 }  // namespace

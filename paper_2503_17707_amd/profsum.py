@@ -92,7 +92,7 @@ def kind_of(name):
         return "decode_attention"
     for k, kind in (("paged_attention", "paged_attention"), ("paged_join", "paged_attention"),
                     ("paged_cut", "paged_attention"), ("kv_append", "kv_append"), ("fork_", "page_fork"),
-                    ("beam_", "beam_select")):
+                    ("beam_", "beam_select"), ("norm_q8", "norm_q8"), ("quant_q8", "quant_q8"), ("q8_", "gemm_q8")):
         if k in name:
             return kind
     if "row_shrink" in name:
