@@ -8,6 +8,9 @@
 // the step's 64; which of the 64 a lane holds does not matter as long as both operands
 // agree, and sums of integers do not depend on their order: every variant gives the
 // same bits.
+#include <algorithm>
+#include <type_traits>
+
 #include "../csrc/common.h"
 #include "q8.h"
 
@@ -47,86 +50,626 @@ __device__ __forceinline__ void load4(const T* p, int left, float (&f)[4]) {
     for (int r = 0; r < 4; ++r) f[r] = (float)t[r];
 }
 
+// What the epilogue knows of features n .. n+3.
+struct Features {
+    float sw[4], b[4];
+    int left;  // of them inside N: 4 or more, or fewer
+};
+
+__device__ __forceinline__ Features load_features(const GemmQ8Params& p, int n) {
+    Features f;
+    f.left = p.N - n;
+    load4(p.sw + n, f.left, f.sw);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) f.b[r] = 0.f;
+    if (p.bias) {
+        if (p.bf16) load4((const __bf16*)p.bias + n, f.left, f.b);
+        else load4((const _Float16*)p.bias + n, f.left, f.b);
+    }
+    return f;
+}
+
 // Features n .. n+3 of token m: (sum rounded to fp32, times sx) times sw plus bias,
 // the second product and the sum rounded once; then the epilogue.  Rows of the output
 // may start at any element (N odd): vectors go there as they come.
-__device__ __forceinline__ void epilogue8(const GemmQ8Params& p, int m, int n, i32x4 acc) {
-    const int left = p.N - n;
-    const float sx = p.sx[m];
-    float sw[4], b[4] = {0.f, 0.f, 0.f, 0.f}, y[4];
-    load4(p.sw + n, left, sw);
-    if (p.bias) {
-        if (p.bf16) load4((const __bf16*)p.bias + n, left, b);
-        else load4((const _Float16*)p.bias + n, left, b);
-    }
+__device__ __forceinline__ void epilogue8(const GemmQ8Params& p, int m, int n, float sx, const Features& f, i32x4 acc) {
+    float y[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        y[r] = fmaf((float)acc[r] * sx, sw[r], b[r]);
+        y[r] = fmaf((float)acc[r] * sx, f.sw[r], f.b[r]);
         if (p.epi == Q8_RELU) y[r] = y[r] < 0.f ? 0.f : y[r];  // (NaN stays)
         if (p.epi == Q8_QKV && n + r < p.qcols) y[r] *= p.qscale;
+        // the 16-bit rounding apart from the product before it, in every kernel
+        asm volatile("" : "+v"(y[r]));
     }
     const int64_t at = (int64_t)m * p.ldo + n;
     if (p.epi >= Q8_RESID) {
         float* out = (float*)p.out + at;
         if (p.epi == Q8_RESID) {
             float old[4];
-            load4(out, left, old);
+            load4(out, f.left, old);
 #pragma unroll
             for (int r = 0; r < 4; ++r) y[r] += old[r];
         }
-        store4(out, left, y);
+        store4(out, f.left, y);
     } else if (p.bf16) {
-        store4((__bf16*)p.out + at, left, y);
+        store4((__bf16*)p.out + at, f.left, y);
     } else {
-        store4((_Float16*)p.out + at, left, y);
+        store4((_Float16*)p.out + at, f.left, y);
     }
 }
 
-// 64 tokens x 64 features a block, four waves of 32 x 32, operands straight from memory.
-__global__ __launch_bounds__(256) void q8_plain_kernel(GemmQ8Params p, int tiles_n) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int lr = lane & 15, lg = lane >> 4;
-    const int m0 = ((int)blockIdx.x / tiles_n) * 64 + (wave & 1) * 32;
-    const int n0 = ((int)blockIdx.x % tiles_n) * 64 + (wave >> 1) * 32;
-    const int8_t *x[2], *w[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {  // rows past the edge re-read the last one
-        x[i] = p.X + (int64_t)min(m0 + 16 * i + lr, p.M - 1) * p.ldx;
-        w[i] = p.W + (int64_t)min(n0 + 16 * i + lr, p.N - 1) * p.ldw;
+// ---- which block does what ----------------------------------------------------------
+
+// Tiles 0 .. full-1 run over the whole of K; the others' K tiles (of 128) are cut into
+// `splits` ranges of kt, the last one taking the rest and what lies past the last whole
+// K tile.  Range s of tile full + i leaves its sums at ws + (s tail + i) BM BN.
+struct Split {
+    int full, tail, splits, kt;
+};
+
+// The hardware deals consecutive blocks round-robin to the 8 XCDs: piece i of n such that
+// each XCD gets a contiguous run of pieces.
+__device__ __forceinline__ int of_xcd(int i, int n) {
+    const int x = i & 7, each = n >> 3, rest = n & 7;
+    return x * each + min(x, rest) + (i >> 3);
+}
+
+struct Job {
+    int m0, n0, t0, nk;  // corner; first K tile and how many
+    bool last, partial;  // takes what lies past the last whole K tile; leaves sums
+    int32_t* sums;       // [BM][BN]
+};
+
+// Tiles are walked in groups of 8 tile-rows: blocks that share an XCD's L2 share rows of
+// X and of W.
+constexpr int GROUP_M = 8;
+
+template <int BM, int BN>
+__device__ __forceinline__ void tile_corner(const GemmQ8Params& p, int tile, int& m0, int& n0) {
+    const int tiles_m = (p.M + BM - 1) / BM, tiles_n = (p.N + BN - 1) / BN;
+    const int per_group = GROUP_M * tiles_n;
+    const int first_m = (tile / per_group) * GROUP_M;
+    const int rows = min(tiles_m - first_m, GROUP_M);
+    m0 = (first_m + (tile % per_group) % rows) * BM;
+    n0 = ((tile % per_group) / rows) * BN;
+}
+
+template <int BM, int BN, int BK>
+__device__ __forceinline__ Job tile_job(const GemmQ8Params& p, const Split& sp) {
+    const int bid = (int)blockIdx.x, nblk = (int)gridDim.x;
+    const int whole = p.K / BK;
+    Job j;
+    int tile;
+    if (bid < sp.full) {
+        tile = of_xcd(bid, sp.full);
+        j.t0 = 0;
+        j.nk = whole;
+        j.last = true;
+        j.partial = false;
+        j.sums = nullptr;
+    } else {
+        const int r = of_xcd(bid - sp.full, nblk - sp.full);
+        const int i = r % sp.tail, s = r / sp.tail;
+        tile = sp.full + i;
+        j.t0 = s * sp.kt;
+        j.last = s == sp.splits - 1;
+        j.nk = j.last ? whole - j.t0 : sp.kt;
+        j.partial = true;
+        j.sums = p.ws + ((int64_t)s * sp.tail + i) * (BM * BN);
     }
-    i32x4 acc[2][2] = {};
-    for (int k = 16 * lg; k - 16 * lg < p.K; k += 64) {
-        const i32x4 zero = {0, 0, 0, 0};
-        const bool in = k < p.K;  // K is a multiple of 16
-        i32x4 a[2], b[2];
+    tile_corner<BM, BN>(p, tile, j.m0, j.n0);
+    return j;
+}
+
+// A wave's sums: acc[i][j] holds features nb + 16 i + 4 lg + r of token mb + 16 j + lr.
+template <int BN, int MF, int NF>
+__device__ __forceinline__ void store_tile(const GemmQ8Params& p, const Job& jb, int mb, int nb, int lr, int lg,
+                                           const i32x4 (&acc)[NF][MF]) {
+    if (jb.partial) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            a[i] = in ? *(const i32x4*)(w[i] + k) : zero;
-            b[i] = in ? *(const i32x4*)(x[i] + k) : zero;
+        for (int j = 0; j < MF; ++j) {
+            const int m = mb + 16 * j + lr;
+            if (m >= p.M) continue;
+#pragma unroll
+            for (int i = 0; i < NF; ++i)
+                *(i32x4*)(jb.sums + (int64_t)(m - jb.m0) * BN + (nb + 16 * i + 4 * lg - jb.n0)) = acc[i][j];
         }
+        return;
+    }
+    Features f[NF];
+#pragma unroll
+    for (int i = 0; i < NF; ++i) f[i] = load_features(p, nb + 16 * i + 4 * lg);
+    float sx[MF];
+#pragma unroll
+    for (int j = 0; j < MF; ++j) sx[j] = p.sx[min(mb + 16 * j + lr, p.M - 1)];
+#pragma unroll
+    for (int j = 0; j < MF; ++j) {
+        const int m = mb + 16 * j + lr;
+        if (m >= p.M) continue;
+#pragma unroll
+        for (int i = 0; i < NF; ++i)
+            if (f[i].left > 0) epilogue8(p, m, nb + 16 * i + 4 * lg, sx[j], f[i], acc[i][j]);
+    }
+}
+
+// What lies past the last whole K tile (K is a multiple of 16, a lane's 16 bytes are in
+// or out as a whole), straight from memory.
+template <int MF, int NF>
+__device__ __forceinline__ void add_rest(const GemmQ8Params& p, int k0, int mb, int nb, int lr, int lg,
+                                         i32x4 (&acc)[NF][MF]) {
+    for (int k = k0 + 16 * lg; k - 16 * lg < p.K; k += 64) {
+        i32x4 a[NF], b[MF];
+        const bool in = k < p.K;
+#pragma unroll
+        for (int i = 0; i < NF; ++i) {
+            a[i] = i32x4{0, 0, 0, 0};
+            if (in) a[i] = *(const i32x4*)(p.W + (int64_t)min(nb + 16 * i + lr, p.N - 1) * p.ldw + k);
+        }
+#pragma unroll
+        for (int j = 0; j < MF; ++j) {
+            b[j] = i32x4{0, 0, 0, 0};
+            if (in) b[j] = *(const i32x4*)(p.X + (int64_t)min(mb + 16 * j + lr, p.M - 1) * p.ldx + k);
+        }
+#pragma unroll
+        for (int i = 0; i < NF; ++i)
+#pragma unroll
+            for (int j = 0; j < MF; ++j) acc[i][j] = mma8(a[i], b[j], acc[i][j]);
+    }
+}
+
+// ---- 256-feature tiles: two wave groups in ping-pong ----------------------------------
+// 64 XF tokens x 256 features, eight waves (2 x 4) of 32 XF x 64, K tiles of 128 bytes in
+// two LDS stages, filled by LDS-DMA.  A K tile is four phases, one per quadrant of the
+// wave tile, and a phase has two slots, each closed by a barrier: a memory slot (operand
+// reads of the quadrant into registers, one or two copies) and a product slot (4 XF
+// products at raised wave priority).  Waves 4-7 run one slot behind waves 0-3 and share
+// their SIMDs: one of the two is always in its product slot while the other reads LDS.
+//
+// A stage is four regions in order of need: Wa (32 of each wave's 64 features), X0 (half
+// of its tokens), Wb, X1.  Quadrants go (Wa, X0), (Wb, X0), (Wb, X1), (Wa, X1); Wa of the
+// next tile is read in the last phase, into the registers of this tile's Wb, so even
+// tiles start with feature half 0 and odd ones with half 1.  A region is free once both
+// groups have read it, one slot later, and is then refilled with tile t + 2: a copy has
+// seven phases to land, and every wait is for all but the youngest one and a half tiles
+// of a wave's copies.  Past the last tile the copies re-read it (nobody reads them).
+// LDS rows are 128 bytes, 16-byte chunks XOR-permuted by row & 7: operand reads of 16
+// rows are free of bank conflicts.
+template <int XF>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void q8_wide_kernel(GemmQ8Params p, Split sp) {
+    constexpr int BM = 64 * XF, BN = 256, RB = 128;
+    constexpr int XH = 16 * XF;                // tokens of a wave's X half
+    constexpr int XC = BM / 2 / 8;             // copies of an X region
+    constexpr int XQ = (XC + 7) / 8;           // ... per wave (XF = 3: four waves repeat the last one)
+    constexpr int LAG = (4 + 2 * XQ) * 3 / 2;  // copies younger than the one a slot needs
+    constexpr int STAGE = (BM + BN) * RB;
+    __shared__ __attribute__((aligned(16))) uint8_t smem[2 * STAGE];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave & 1, wn = wave >> 1;
+    const Job jb = tile_job<BM, BN, RB>(p, sp);
+    const int m0 = jb.m0, n0 = jb.n0, nk = jb.nk;
+
+    // copies: region X h is token rows (2 g + h) XH .. + XH - 1 (g = 0, 1), region W h
+    // feature rows 64 g + 32 h .. + 31 (g = 0 .. 3), 8 rows per copy; copy q of this wave
+    // is number wave + 8 q of its region.  Lane i writes row i / 8, physical chunk i % 8.
+    // Rows past the edge re-read the last one.
+    const int lrow = lane >> 3, chk = ((lane & 7) ^ lrow) * 16;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
+    const int8_t* Xb = p.X + (int64_t)m0 * p.ldx + (int64_t)jb.t0 * RB;
+    const int8_t* Wb = p.W + (int64_t)n0 * p.ldw + (int64_t)jb.t0 * RB;
+    int xrow[2 * XQ], wrow[4];  // first row of copy q of region h: [XQ h + q], [2 h + q]
+    uint32_t xoff[2 * XQ], woff[4];
+#pragma unroll
+    for (int i = 0; i < 2 * XQ; ++i) {
+        const int h = i / XQ, c = min(wave + 8 * (i % XQ), XC - 1);
+        xrow[i] = (2 * (c / (XC / 2)) + h) * XH + (c % (XC / 2)) * 8;
+        xoff[i] = (uint32_t)min(xrow[i] + lrow, p.M - 1 - m0) * (uint32_t)p.ldx + chk;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int h = i >> 1, c = wave + 8 * (i & 1);
+        wrow[i] = (c >> 2) * 64 + h * 32 + (c & 3) * 8;
+        woff[i] = (uint32_t)min(wrow[i] + lrow, p.N - 1 - n0) * (uint32_t)p.ldw + chk;
+    }
+    auto copy_x = [&](int t, int stage, int h) {
+        const int8_t* b = Xb + (int64_t)t * RB;
+#pragma unroll
+        for (int i = XQ * h; i < XQ * h + XQ; ++i) dma16s(b, xoff[i], lds0 + stage * STAGE + xrow[i] * RB);
+    };
+    auto copy_w = [&](int t, int stage, int h) {
+        const int8_t* b = Wb + (int64_t)t * RB;
+#pragma unroll
+        for (int i = 2 * h; i < 2 * h + 2; ++i) dma16s(b, woff[i], lds0 + stage * STAGE + (BM + wrow[i]) * RB);
+    };
+
+    i32x4 acc[4][2 * XF] = {};
+    const int lr = lane & 15, lg = lane >> 4;
+    i32x4 w0[2][2], w1[2][2], x[XF][2];  // [fragment][k half]
+    const uint32_t lk[2] = {(uint32_t)(lr * RB + ((lg ^ (lr & 7)) << 4)), (uint32_t)(lr * RB + (((4 + lg) ^ (lr & 7)) << 4))};
+    auto read_w = [&](i32x4(&w)[2][2], int stage, int h) {
+        const uint8_t* s = smem + stage * STAGE + (BM + wn * 64 + h * 32) * RB;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) acc[i][j] = mma8(a[i], b[j], acc[i][j]);
+            for (int kk = 0; kk < 2; ++kk) w[i][kk] = *(const i32x4*)(s + i * 16 * RB + lk[kk]);
+    };
+    auto read_x = [&](int stage, int h) {
+        const uint8_t* s = smem + stage * STAGE + (2 * wm + h) * XH * RB;
+#pragma unroll
+        for (int j = 0; j < XF; ++j)
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) x[j][kk] = *(const i32x4*)(s + j * 16 * RB + lk[kk]);
+    };
+    // nothing moves across the end of a slot
+    auto barrier = [] { asm volatile("s_barrier" ::: "memory"); };
+    auto end_memory = [&] {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto products = [&](const i32x4(&w)[2][2], int fi, int fj) {
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < XF; ++j) acc[fi + i][fj + j] = mma8(w[i][kk], x[j][kk], acc[fi + i][fj + j]);
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+        barrier();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    const int last = nk - 1;  // (a launch has a K tile for every block)
+    auto fill = [&](int t, int stage) {  // a whole stage, in order of need
+        copy_w(t, stage, stage);
+        copy_x(t, stage, 0);
+        copy_w(t, stage, 1 - stage);
+        copy_x(t, stage, 1);
+    };
+    fill(0, 0);
+    fill(min(1, last), 1);
+    wait_vmcnt<LAG>();
+    barrier();
+    read_w(w0, 0, 0);
+    end_memory();              // both groups hold Wa of tile 0: its region may be refilled
+    if (wave >= 4) barrier();  // one slot behind from here on
+    auto tile = [&](int t, auto parity) {
+        constexpr int P = decltype(parity)::value;  // t % 2: the stage, and the feature half of Wa
+        auto& wa = P ? w1 : w0;
+        auto& wb = P ? w0 : w1;
+        const int tn = min(t + 2, last);
+        read_x(P, 0);
+        copy_w(tn, P, P);
+        wait_vmcnt<LAG>();  // Wb landed
+        end_memory();
+        products(wa, 2 * P, 0);
+        read_w(wb, P, 1 - P);
+        copy_x(tn, P, 0);
+        wait_vmcnt<LAG>();  // X1 landed
+        end_memory();
+        products(wb, 2 - 2 * P, 0);
+        read_x(P, 1);
+        copy_w(tn, P, 1 - P);
+        wait_vmcnt<LAG>();  // Wa of t + 1 landed
+        end_memory();
+        products(wb, 2 - 2 * P, XF);
+        read_w(wb, 1 - P, 1 - P);  // Wa of t + 1
+        copy_x(tn, P, 1);
+        wait_vmcnt<LAG>();  // X0 of t + 1 landed
+        end_memory();
+        products(wa, 2 * P, XF);
+    };
+    const std::integral_constant<int, 0> even;
+    const std::integral_constant<int, 1> odd;
+    int t = 0;
+    for (; t + 1 < nk; t += 2) {
+        tile(t, even);
+        tile(t + 1, odd);
+    }
+    if (t < nk) tile(t, even);
+    if (wave < 4) barrier();  // as many barriers in both groups
+    const int mb = m0 + wm * 2 * XH, nb = n0 + wn * 64;
+    if (jb.last) add_rest<2 * XF, 4>(p, p.K / RB * RB, mb, nb, lr, lg, acc);
+    store_tile<BN, 2 * XF, 4>(p, jb, mb, nb, lr, lg, acc);
+    wait_vmcnt<0>();  // the last copies have landed before the block's LDS is given back
+}
+
+// ---- smaller tiles: a ring of wide rows ------------------------------------------------
+// BM tokens x BN features, the waves WGM x WGN; a ring stage holds BK bytes of the BM token
+// rows and BN weight rows, so a copy fetches whole 128- to 512-byte row pieces; S - 1 stages
+// are in flight while one is multiplied.  16-byte chunks are XOR-permuted by the low row bits.
+template <int BM, int BN, int WGM, int WGN, int BK, int S>
+__global__ __launch_bounds__(64 * WGM * WGN) void q8_ring_kernel(GemmQ8Params p, Split sp) {
+    constexpr int NW = WGM * WGN;
+    constexpr int WM = BM / WGM, WN = BN / WGN;
+    constexpr int MF = WM / 16, NF = WN / 16;
+    constexpr int CPR = BK / 16;              // chunks per row
+    constexpr int MASK = (CPR < 16 ? CPR : 16) - 1;
+    constexpr int RPI = 1024 / BK;            // rows per copy
+    constexpr int NL = (BM + BN) / RPI / NW;  // copies per wave and stage
+    constexpr int STAGE = (BM + BN) * BK;
+    static_assert(BM % (RPI * NW) == 0 && BN % (RPI * NW) == 0, "copies split into X and W");
+    static_assert(S >= 2 && (S - 2) * NL < 64, "pipeline depth");
+    __shared__ __attribute__((aligned(16))) uint8_t smem[S * STAGE];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave % WGM, wn = wave / WGM;
+    const int lr = lane & 15, lg = lane >> 4;
+    const Job jb = tile_job<BM, BN, BK>(p, sp);
+    const int m0 = jb.m0, n0 = jb.n0, nk = jb.nk;
+
+    const int8_t* Xb = p.X + (int64_t)m0 * p.ldx + (int64_t)jb.t0 * BK;
+    const int8_t* Wb = p.W + (int64_t)n0 * p.ldw + (int64_t)jb.t0 * BK;
+    uint32_t off[NL];
+#pragma unroll
+    for (int j = 0; j < NL; ++j) {
+        const int row = (wave + NW * j) * RPI + lane / CPR;
+        const int ch = (lane % CPR) ^ (row & MASK);
+        off[j] = ((wave + NW * j) * RPI < BM ? (uint32_t)min(row, p.M - 1 - m0) * (uint32_t)p.ldx
+                                             : (uint32_t)min(row - BM, p.N - 1 - n0) * (uint32_t)p.ldw) + ch * 16;
+    }
+    const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
+    auto issue = [&](int t, int stage) {
+        const int8_t* xk = Xb + (int64_t)t * BK;
+        const int8_t* wk = Wb + (int64_t)t * BK;
+#pragma unroll
+        for (int j = 0; j < NL; ++j)
+            dma16s((wave + NW * j) * RPI < BM ? xk : wk, off[j], lds0 + stage * STAGE + (wave + NW * j) * 1024);
+    };
+    i32x4 acc[NF][MF] = {};
+    auto compute = [&](int stage) {
+        const uint8_t* s = smem + stage * STAGE;
+#pragma unroll
+        for (int kk = 0; kk < BK / 64; ++kk) {
+            const int ch = kk * 4 + lg;
+            i32x4 b[MF];
+#pragma unroll
+            for (int j = 0; j < MF; ++j) {
+                const int row = wm * WM + j * 16 + lr;
+                b[j] = *(const i32x4*)(s + row * BK + ((ch ^ (row & MASK)) << 4));
+            }
+#pragma unroll
+            for (int i = 0; i < NF; ++i) {
+                const int row = BM + wn * WN + i * 16 + lr;
+                const i32x4 a = *(const i32x4*)(s + row * BK + ((ch ^ (row & MASK)) << 4));
+#pragma unroll
+                for (int j = 0; j < MF; ++j) acc[i][j] = mma8(a, b[j], acc[i][j]);
+            }
+        }
+    };
+#pragma unroll
+    for (int q = 0; q < S - 1; ++q)
+        if (q < nk) issue(q, q);
+    int t = 0, st = 0;
+    for (; t + S - 1 < nk; ++t) {
+        wait_vmcnt<(S - 2) * NL>();
+        __syncthreads();  // stage st visible to all waves; the stage before it free
+        issue(t + S - 1, st == 0 ? S - 1 : st - 1);
+        compute(st);
+        st = st == S - 1 ? 0 : st + 1;
+    }
+    for (; t < nk; ++t) {
+        wait_vmcnt<0>();
+        __syncthreads();
+        compute(st);
+        st = st == S - 1 ? 0 : st + 1;
+    }
+    const int mb = m0 + wm * WM, nb = n0 + wn * WN;
+    if (jb.last) add_rest<MF, NF>(p, p.K / BK * BK, mb, nb, lr, lg, acc);
+    store_tile<BN, MF, NF>(p, jb, mb, nb, lr, lg, acc);
+}
+
+// ---- up to 16 tokens: weights from memory into the matrix operands ----------------------
+// 16 NF features a block; its KW waves take pieces of 256 bytes of K in turn and add their
+// sums through LDS.  Nothing is shared between waves, so weights need no LDS: a wave has
+// the next piece's loads in flight while it multiplies one.  Lanes of tokens that do not
+// exist load nothing and multiply zeros.
+template <int NF, int KW>
+__global__ __launch_bounds__(64 * KW) void q8_few_kernel(GemmQ8Params p) {
+    __shared__ i32x4 part[KW][NF][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lr = lane & 15, lg = lane >> 4;
+    const int n0 = (int)blockIdx.x * 16 * NF;
+    const int8_t* w[NF];
+#pragma unroll
+    for (int i = 0; i < NF; ++i) w[i] = p.W + (int64_t)min(n0 + 16 * i + lr, p.N - 1) * p.ldw + 16 * lg;
+    const int8_t* x = p.X + (int64_t)min(lr, p.M - 1) * p.ldx + 16 * lg;
+    const bool here = lr < p.M;
+    struct Piece {
+        i32x4 a[4][NF], b[4];
+    };
+    auto load = [&](Piece& c, int k) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+#pragma unroll
+            for (int i = 0; i < NF; ++i) c.a[q][i] = __builtin_nontemporal_load((const i32x4*)(w[i] + k + 64 * q));
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            c.b[q] = i32x4{0, 0, 0, 0};
+            if (here) c.b[q] = *(const i32x4*)(x + k + 64 * q);
+        }
+    };
+    i32x4 acc[NF] = {};
+    auto multiply = [&](const Piece& c) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int i = 0; i < NF; ++i) acc[i] = mma8(c.a[q][i], c.b[q], acc[i]);
+    };
+    const int pieces = p.K / 256;
+    Piece c0, c1;
+    int t = wave;
+    if (t < pieces) load(c0, t * 256);
+    for (; t < pieces; t += 2 * KW) {
+        if (t + KW < pieces) load(c1, (t + KW) * 256);
+        multiply(c0);
+        if (t + 2 * KW < pieces) load(c0, (t + 2 * KW) * 256);
+        if (t + KW < pieces) multiply(c1);
+    }
+    if (pieces * 256 < p.K && wave == pieces % KW) {  // the rest, to the wave whose turn it is
+        for (int k = pieces * 256; k < p.K; k += 64) {
+            const bool in = k + 16 * lg < p.K;
+            i32x4 b = {0, 0, 0, 0};
+            if (in && here) b = *(const i32x4*)(x + k);
+#pragma unroll
+            for (int i = 0; i < NF; ++i) {
+                i32x4 a = {0, 0, 0, 0};
+                if (in) a = *(const i32x4*)(w[i] + k);
+                acc[i] = mma8(a, b, acc[i]);
+            }
+        }
     }
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int i = 0; i < NF; ++i) part[wave][i][lane] = acc[i];
+    __syncthreads();
+    for (int i = wave; i < NF; i += KW) {
+        i32x4 v = part[0][i][lane];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int m = m0 + 16 * j + lr, n = n0 + 16 * i + 4 * lg;
-            if (m < p.M && n < p.N) epilogue8(p, m, n, acc[i][j]);
+        for (int k = 1; k < KW; ++k) {
+            const i32x4 o = part[k][i][lane];
+            v += o;
         }
+        const int n = n0 + 16 * i + 4 * lg;
+        if (here && n < p.N) epilogue8(p, lr, n, p.sx[lr], load_features(p, n), v);
+    }
+}
+
+// ---- the sums of split tiles -------------------------------------------------------------
+// A thread adds the ranges' sums of four features of one token.
+template <int BM, int BN>
+__global__ __launch_bounds__(256) void q8_join_kernel(GemmQ8Params p, Split sp) {
+    constexpr int GROUPS = BM * BN / 4 / 256;  // blocks per tile
+    const int i = (int)blockIdx.x / GROUPS;
+    const int at = ((int)blockIdx.x % GROUPS * 256 + (int)threadIdx.x) * 4;
+    int m0, n0;
+    tile_corner<BM, BN>(p, sp.full + i, m0, n0);
+    const int m = m0 + at / BN, n = n0 + at % BN;
+    if (m >= p.M || n >= p.N) return;
+    const int64_t stride = (int64_t)sp.tail * (BM * BN);
+    const int32_t* src = p.ws + (int64_t)i * (BM * BN) + at;
+    i32x4 v = *(const i32x4*)src;
+    int s = 1;
+    for (; s + 3 < sp.splits; s += 4) {
+        i32x4 o[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) o[q] = *(const i32x4*)(src + (s + q) * stride);
+        v += (o[0] + o[1]) + (o[2] + o[3]);
+    }
+    for (; s < sp.splits; ++s) v += *(const i32x4*)(src + s * stride);
+    epilogue8(p, m, n, p.sx[m], load_features(p, n), v);
+}
+
+// ---- launches ----------------------------------------------------------------------------
+
+enum Kind { FEW, RING_32, RING_64, RING_128, WIDE };
+
+// splits > 1: the K tiles of the last `tail` tiles in that many ranges.
+struct Plan {
+    Kind kind;
+    int bm, bn, bk;
+    int splits, tail;
+};
+
+int64_t tiles_of(const GemmQ8Params& p, int bm, int bn) {
+    return (((int64_t)p.M + bm - 1) / bm) * (((int64_t)p.N + bn - 1) / bn);
+}
+
+size_t bytes_of(const Plan& c) { return c.splits > 1 ? (size_t)c.tail * c.splits * c.bm * c.bn * 4 : 0; }
+
+template <int BM, int BN, typename F>
+void launch_tiles(F kernel, int threads, const GemmQ8Params& p, const Plan& c, hipStream_t s) {
+    const int tiles = (int)tiles_of(p, BM, BN), whole = p.K / c.bk;
+    Split sp{tiles, 0, 1, whole};
+    if (c.splits > 1) {
+        sp.kt = (whole + c.splits - 1) / c.splits;
+        sp.splits = (whole + sp.kt - 1) / sp.kt;
+        if (sp.splits > 1) {
+            sp.tail = c.tail;
+            sp.full = tiles - c.tail;
+        }
+    }
+    PB_LAUNCH(kernel, sp.full + sp.tail * sp.splits, threads, 0, s, p, sp);
+    if (sp.tail)
+        PB_LAUNCH((q8_join_kernel<BM, BN>), sp.tail * (BM * BN / 4 / 256), 256, 0, s, p, sp);
+}
+
+template <int XF>
+void launch_wide(const GemmQ8Params& p, const Plan& c, hipStream_t s) {
+    launch_tiles<64 * XF, 256>(q8_wide_kernel<XF>, 512, p, c, s);
+}
+
+template <int BM, int BN, int WGM, int WGN, int BK, int S>
+void launch_ring(const GemmQ8Params& p, const Plan& c, hipStream_t s) {
+    launch_tiles<BM, BN>(q8_ring_kernel<BM, BN, WGM, WGN, BK, S>, 64 * WGM * WGN, p, c, s);
+}
+
+template <int NF, int KW>
+void launch_few(const GemmQ8Params& p, hipStream_t s) {
+    PB_LAUNCH((q8_few_kernel<NF, KW>), (p.N + 16 * NF - 1) / (16 * NF), 64 * KW, 0, s, p);
+}
+
+void launch_plan(const GemmQ8Params& p, const Plan& c, hipStream_t s) {
+    switch (c.kind) {
+        case FEW:  // bn: features, bk: waves
+            if (c.bn == 16 && c.bk == 4) launch_few<1, 4>(p, s);
+            else if (c.bn == 16 && c.bk == 8) launch_few<1, 8>(p, s);
+            else if (c.bn == 16) launch_few<1, 16>(p, s);
+            else if (c.bk == 4) launch_few<2, 4>(p, s);
+            else launch_few<2, 8>(p, s);
+            break;
+        case RING_32:
+            if (c.bn == 32) launch_ring<32, 32, 1, 2, 256, 4>(p, c, s);
+            else if (c.bk == 256) launch_ring<32, 64, 1, 4, 256, 4>(p, c, s);
+            else launch_ring<32, 64, 1, 4, 512, 3>(p, c, s);
+            break;
+        case RING_64:
+            if (c.bn == 64) launch_ring<64, 64, 1, 4, 256, 4>(p, c, s);
+            else launch_ring<64, 128, 2, 4, 128, 4>(p, c, s);
+            break;
+        case RING_128:
+            if (c.bn == 64) launch_ring<128, 64, 2, 2, 256, 3>(p, c, s);
+            else launch_ring<128, 128, 2, 4, 128, 4>(p, c, s);
+            break;
+        case WIDE:
+            if (c.bm == 128) launch_wide<2>(p, c, s);
+            else if (c.bm == 192) launch_wide<3>(p, c, s);
+            else launch_wide<4>(p, c, s);
+            break;
+    }
+}
+
+
+Plan plan_of(const GemmQ8Params& p, size_t room) {
+    if (p.M <= 16) return {FEW, 16, 16, p.N / 16 <= 256 && p.K >= 4096 ? 16 : 8, 1, 0};
+    Plan c = p.M <= 32 ? Plan{RING_32, 32, 64, 256, 1, 0} : p.M <= 512 || p.K < 256 ? Plan{RING_128, 128, 128, 128, 1, 0}
+             : Plan{WIDE, 256, 256, 128, 1, 0};
+    const int64_t tiles = tiles_of(p, c.bm, c.bn);
+    if (tiles < 256) {
+        const int s = (int)std::min<int64_t>({256 / tiles, 8, std::max(1, p.K / c.bk / 8)});
+        const Plan cut{c.kind, c.bm, c.bn, c.bk, s, (int)tiles};
+        if (s > 1 && bytes_of(cut) <= room) return cut;
+    }
+    return c;
 }
 
 }  // namespace
 
-bool gemm_q8_fits(int M, int N) { return (((int64_t)M + 63) / 64) * (((int64_t)N + 63) / 64) < (1 << 23); }
+bool gemm_q8_fits(int M, int N) {
+    return M <= (1 << 24) && N <= (1 << 24) && (((int64_t)M + 63) / 64) * (((int64_t)N + 63) / 64) < (1 << 23);
+}
 
-size_t gemm_q8_workspace(int, int, int) { return 0; }
+size_t gemm_q8_workspace(int M, int N, int K) {
+    GemmQ8Params p{};
+    p.M = M; p.N = N; p.K = K;
+    return bytes_of(plan_of(p, (size_t)1 << 60));
+}
 
 hipError_t launch_gemm_q8(const GemmQ8Params& p, hipStream_t s) {
-    const int tm = (p.M + 63) / 64, tn = (p.N + 63) / 64;
-    PB_LAUNCH(q8_plain_kernel, tm * tn, 256, 0, s, p, tn);
+    launch_plan(p, plan_of(p, p.ws_bytes), s);
     return hipGetLastError();
 }
 
