@@ -217,7 +217,7 @@ size_t pb_op_page_fork_workspace(int32_t out_rows, int32_t n_pages);
  * neither order nor launch shape shows.)  A row whose scale would be below 2^-126
  * is one of zeros: scale 0, q 0.  A row with a NaN, an infinity or a scale past the
  * largest float: scale NaN, q 0, so that its products are NaN.  Row strides are in
- * elements; that of a single row is not used. */
+ * elements; that of a single row is not used.  At most 2^30 rows. */
 
 /* The residual's addition, the norm and its 8 bits: per row of d elements
  *   s = x + delta              (fp32, rounded to x's type; delta NULL: s = x)
@@ -232,7 +232,7 @@ int pb_op_norm_q8(int32_t dtype, int32_t layer, const void* x, int64_t ld_x, int
                   void* out, int64_t ld_out, int8_t* q, int64_t ld_q, float* scale, int32_t rows, int32_t d,
                   void* stream);
 
-/* Rows of x (fp32 where x_f32 != 0, else dt) in 8 bits.  1 <= cols <= 2^30. */
+/* Rows of x (fp32 where x_f32 != 0, else dt) in 8 bits.  1 <= cols <= 2^24. */
 int pb_op_quant_q8(int32_t dtype, const void* x, int64_t ld_x, int32_t x_f32, int8_t* q, int64_t ld_q,
                    float* scale, int32_t rows, int32_t cols, void* stream);
 

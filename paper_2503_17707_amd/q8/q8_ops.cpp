@@ -45,8 +45,8 @@ extern "C" int pb_op_norm_q8(int32_t dtype, int32_t layer, const void* x, int64_
                              void* stream) {
     const char* op = "pb_op_norm_q8";
     if (dtype != PB_BF16 && dtype != PB_F16) return refuse("%s: bad dtype %d", op, dtype);
-    if (rows < 0 || d < 1 || d > pb::NORM_Q8_MAX)
-        return refuse("%s: %d rows of %d (1..%d elements)", op, rows, d, pb::NORM_Q8_MAX);
+    if (rows < 0 || rows > (1 << 30) || d < 1 || d > pb::NORM_Q8_MAX)
+        return refuse("%s: %d rows (up to 2^30) of %d (1..%d)", op, rows, d, pb::NORM_Q8_MAX);
     if (!(eps >= 0.f) || !(eps - eps == 0.f)) return refuse("%s: eps=%g", op, (double)eps);
     if (rows == 0) return PB_OK;
     const int xs = x_f32 ? 4 : 2;
@@ -76,7 +76,7 @@ extern "C" int pb_op_quant_q8(int32_t dtype, const void* x, int64_t ld_x, int32_
                               float* scale, int32_t rows, int32_t cols, void* stream) {
     const char* op = "pb_op_quant_q8";
     if (dtype != PB_BF16 && dtype != PB_F16) return refuse("%s: bad dtype %d", op, dtype);
-    if (rows < 0 || cols < 1 || cols > (1 << 30)) return refuse("%s: %d rows of %d (1..2^30)", op, rows, cols);
+    if (rows < 0 || rows > (1 << 30) || cols < 1 || cols > (1 << 24)) return refuse("%s: %d rows (up to 2^30) of %d (1..2^24)", op, rows, cols);
     if (rows == 0) return PB_OK;
     const int xs = x_f32 ? 4 : 2;
     if (!rows_ok(x, ld_x, rows, cols, xs) || !rows_ok(q, ld_q, rows, cols, 1))

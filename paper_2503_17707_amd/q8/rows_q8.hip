@@ -21,279 +21,415 @@ namespace pb {
 
 namespace {
 
-// Elements at any address of their own type: rows of odd widths start anywhere, and
+// VEC elements at any address of their own type: rows of odd widths start anywhere, and
 // global memory serves vectors there too.
-template <typename T, int N>
-struct Vec {
-    T v[N];
+template <typename T, int VEC>
+struct Pack {
+    T v[VEC];
 };
 
-template <typename T, int N>
-__device__ __forceinline__ void load_some(const T* p, int left, float (&f)[N]) {
-    if (left >= N) {
-        Vec<T, N> a;
-        __builtin_memcpy(&a, p, sizeof(a));
-#pragma unroll
-        for (int e = 0; e < N; ++e) f[e] = (float)a.v[e];
-    } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e) f[e] = e < left ? (float)p[e] : 0.f;
-    }
+template <int VEC, typename T>
+__device__ __forceinline__ Pack<T, VEC> load_pack(const T* p) {
+    Pack<T, VEC> a;
+    __builtin_memcpy(&a, p, sizeof(a));
+    return a;
 }
 
-template <typename T, typename F, int N>
-__device__ __forceinline__ void store_some(T* p, int left, const F (&f)[N]) {
-    if (left >= N) {
-        Vec<T, N> a;
+template <typename T, typename F, int VEC>
+__device__ __forceinline__ void store_pack(T* p, const F (&f)[VEC]) {
+    Pack<T, VEC> a;
 #pragma unroll
-        for (int e = 0; e < N; ++e) a.v[e] = (T)f[e];
-        __builtin_memcpy(p, &a, sizeof(a));
-    } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-            if (e < left) p[e] = (T)f[e];
-    }
+    for (int e = 0; e < VEC; ++e) a.v[e] = (T)f[e];
+    __builtin_memcpy(p, &a, sizeof(a));
 }
 
-// Two values over the TPR threads of a row: the sum of a, the larger of m.
-template <int TPR>
-__device__ __forceinline__ void row_reduce(double& a, double& m, double* lds) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        a += __shfl_xor(a, o, 64);
-        m = fmax(m, __shfl_xor(m, o, 64));
+// Piece i of a lane: VEC elements of a row of d >= VEC.  The last one, where it is cut
+// short, is moved back to end with the row, over `over` elements of the piece before it
+// (as all pieces past the end are: over >= VEC).  So every lane loads whole vectors, with
+// no branch between one load and the next, and an element taken twice gives the same
+// result twice; only sums have to leave it out.  Only a lane's last piece can be so: the
+// launches give a row as many pieces as it needs and no more.
+template <int VEC>
+struct Place {
+    uint32_t at;
+    int over;
+    __device__ Place(int i, bool last, int threads, int lane, int d) {
+        const int c = (i * threads + lane) * VEC;
+        at = last ? min(c, d - VEC) : c;
+        over = c - (int)at;
     }
-    if (TPR > 64) {
-        constexpr int NW = TPR / 64;
-        const int wave = threadIdx.x >> 6;
+};
+
+// Other lanes' values without a way through LDS: within rows of 16 by DPP (quad_perm 1 0
+// 3 2, quad_perm 2 3 0 1, row_half_mirror, row_mirror), across rows by permlane swaps.
+template <int STEP>
+__device__ __forceinline__ uint32_t from_lane(uint32_t v) {
+    if constexpr (STEP == 0) return __builtin_amdgcn_mov_dpp(v, 0xB1, 0xf, 0xf, false);
+    if constexpr (STEP == 1) return __builtin_amdgcn_mov_dpp(v, 0x4E, 0xf, 0xf, false);
+    if constexpr (STEP == 2) return __builtin_amdgcn_mov_dpp(v, 0x141, 0xf, 0xf, false);
+    return __builtin_amdgcn_mov_dpp(v, 0x140, 0xf, 0xf, false);
+}
+
+// One value over groups of 16, 32 or 64 lanes.
+template <int LANES, typename F>
+__device__ __forceinline__ double lanes_fold(double v, F f) {
+    auto word = [&](int k) { return (uint32_t)(__builtin_bit_cast(uint64_t, v) >> (32 * k)); };
+    auto value = [](uint32_t lo, uint32_t hi) { return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo); };
+    v = f(v, value(from_lane<0>(word(0)), from_lane<0>(word(1))));
+    v = f(v, value(from_lane<1>(word(0)), from_lane<1>(word(1))));
+    v = f(v, value(from_lane<2>(word(0)), from_lane<2>(word(1))));
+    v = f(v, value(from_lane<3>(word(0)), from_lane<3>(word(1))));
+    if constexpr (LANES > 16) {
+        const auto lo = __builtin_amdgcn_permlane16_swap(word(0), word(0), false, false);
+        const auto hi = __builtin_amdgcn_permlane16_swap(word(1), word(1), false, false);
+        v = f(value(lo[0], hi[0]), value(lo[1], hi[1]));
+    }
+    if constexpr (LANES > 32) {
+        const auto lo = __builtin_amdgcn_permlane32_swap(word(0), word(0), false, false);
+        const auto hi = __builtin_amdgcn_permlane32_swap(word(1), word(1), false, false);
+        v = f(value(lo[0], hi[0]), value(lo[1], hi[1]));
+    }
+    return v;
+}
+
+// One value over a row's threads: LANES of a wave, or (LANES = 0) a block of any number of
+// waves, by one use of `lds`.
+template <int LANES, typename F>
+__device__ __forceinline__ double row_fold(double v, double* lds, F f) {
+    v = lanes_fold<(LANES ? LANES : 64)>(v, f);
+    if constexpr (LANES == 0) {
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+        lds_barrier();
+        v = lds[0];
+        for (int w = 1; w < (int)blockDim.x / 64; ++w) v = f(v, lds[w]);
+    }
+    return v;
+}
+
+// Two at once.
+template <int LANES, typename F, typename G>
+__device__ __forceinline__ void row_fold2(double& a, double& b, double (*lds)[2], F f, G g) {
+    a = lanes_fold<(LANES ? LANES : 64)>(a, f);
+    b = lanes_fold<(LANES ? LANES : 64)>(b, g);
+    if constexpr (LANES == 0) {
         if ((threadIdx.x & 63) == 0) {
-            lds[wave] = a;
-            lds[NW + wave] = m;
+            lds[threadIdx.x >> 6][0] = a;
+            lds[threadIdx.x >> 6][1] = b;
         }
         lds_barrier();
-        a = lds[0];
-        m = lds[NW];
-#pragma unroll
-        for (int w = 1; w < NW; ++w) {
-            a += lds[w];
-            m = fmax(m, lds[NW + w]);
+        a = lds[0][0];
+        b = lds[0][1];
+        for (int w = 1; w < (int)blockDim.x / 64; ++w) {
+            a = f(a, lds[w][0]);
+            b = g(b, lds[w][1]);
         }
-        lds_barrier();
     }
 }
 
-// The scale of a row whose largest magnitude is `top` (NaN where a value is no number).
+struct Plus {
+    __device__ double operator()(double a, double b) const { return a + b; }
+};
+struct Larger {
+    __device__ double operator()(double a, double b) const { return fmax(a, b); }
+};
+
+// Keeps the compiler from holding a conversion made before this point: kept as fp64, a
+// row's elements would take the registers of half the waves.
+template <typename T, int VEC>
+__device__ __forceinline__ void again(Pack<T, VEC>& x) {
+    if constexpr (sizeof(x) % 4 == 0) {
+        uint32_t w[sizeof(x) / 4];
+        __builtin_memcpy(w, &x, sizeof(x));
+#pragma unroll
+        for (uint32_t& k : w) asm volatile("" : "+v"(k));
+        __builtin_memcpy(&x, w, sizeof(x));
+    }
+}
+
+template <int VEC>
+__device__ __forceinline__ void again(float (&x)[VEC]) {
+#pragma unroll
+    for (float& k : x) asm volatile("" : "+v"(k));
+}
+
+// The scale of a row whose largest magnitude is `top` (NaN: some value is no number).
 __device__ __forceinline__ float row_scale(double top) {
     const float s = (float)(top / 127.0);
     if (!(s <= 3.402823466e38f)) return __builtin_nanf("");
     return s < 1.17549435e-38f ? 0.f : s;  // rows below it are zeros: a subnormal scale holds too few bits
 }
 
-// rint(y / scale): the quotient correctly rounded (a product with the rounded
-// reciprocal and one correction), so that ties are ties.
+// rint(y / scale): a product with the reciprocal and one correction, exact where the
+// quotient is a number of 53 bits, so that ties are ties.
 __device__ __forceinline__ int quotient(double y, double scale, double inv) {
     const double t = y * inv;
     return (int)rint(fma(fma(-scale, t, y), inv, t));
 }
 
-template <int N>
-__device__ __forceinline__ void store_q(int8_t* p, int left, const double (&y)[N], float scale, double inv) {
-    int r[N];
+// (a scale that is zero or no number: zeros)
+template <int VEC>
+__device__ __forceinline__ void store_q(int8_t* p, const double (&y)[VEC], float scale, double inv) {
+    int r[VEC] = {};
+    if (scale > 0.f) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) r[e] = scale > 0.f ? quotient(y[e], (double)scale, inv) : 0;
-    store_some<int8_t, int, N>(p, left, r);
+        for (int e = 0; e < VEC; ++e) r[e] = quotient(y[e], (double)scale, inv);
+    }
+    store_pack<int8_t, int, VEC>(p, r);
 }
 
-// S: type of the stream, T: storage type.  TPR threads take a row in NV pieces of VEC
-// elements each.
-template <typename T, typename S, int NV, int TPR>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_q8_kernel(NormQ8Params p) {
-    constexpr int VEC = 16 / sizeof(S);
-    constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
-    __shared__ double lds[2 * (TPR / 64)];
-    const int lane = threadIdx.x % TPR;
-    for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR; row < p.rows; row += (int64_t)gridDim.x * RPB) {
+// S: type of the stream, T: storage type.  LANES threads (0: a block) take a row of d >= VEC
+// in NV pieces of VEC elements each; BIAS: b is given (without it the largest magnitude is
+// known with the sum of squares).
+template <typename T, typename S, int VEC, int NV, int LANES, bool BIAS>
+__global__ __launch_bounds__(LANES ? 256 : 1024) __attribute__((amdgpu_waves_per_eu(4))) void norm_q8_kernel(NormQ8Params p) {
+    constexpr int RPB = LANES ? 256 / LANES : 1;
+    __shared__ double lds1[16], lds3[16], lds2[16][2];
+    const int lane = LANES ? threadIdx.x % LANES : threadIdx.x;
+    const int threads = LANES ? LANES : blockDim.x;
+    const int first = LANES ? (int)blockIdx.x * RPB + (int)threadIdx.x / LANES : blockIdx.x;
+    for (int row = first; row < p.rows; row += (int)gridDim.x * RPB) {
+        Pack<T, VEC> g[NV], b[NV];
         float s[NV][VEC];
-        double sum = 0.0, top = 0.0, square = 0.0, check = 0.0;
+        {
+            Pack<S, VEC> x[NV];
+            Pack<T, VEC> t[NV];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (i * TPR + lane) * VEC, left = p.d - c;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) s[i][e] = 0.f;
-            if (left <= 0) continue;
-            load_some<S, VEC>((const S*)p.x + row * p.ld_x + c, left, s[i]);
+            for (int i = 0; i < NV; ++i) x[i] = load_pack<VEC>((const S*)p.x + (int64_t)row * p.ld_x + Place<VEC>(i, i == NV - 1, threads, lane, p.d).at);
             if (p.delta) {
-                float t[VEC];
-                load_some<T, VEC>((const T*)p.delta + row * p.ld_delta + c, left, t);
-                // the norm is taken of the sum as the stream keeps it
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) s[i][e] = (float)(S)(s[i][e] + t[e]);
-                if (p.sum) store_some<S, float, VEC>((S*)p.sum + row * p.ld_sum + c, left, s[i]);
+                for (int i = 0; i < NV; ++i)
+                    t[i] = load_pack<VEC>((const T*)p.delta + (int64_t)row * p.ld_delta + Place<VEC>(i, i == NV - 1, threads, lane, p.d).at);
+            }
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                g[i] = load_pack<VEC>((const T*)p.g + Place<VEC>(i, i == NV - 1, threads, lane, p.d).at);
+                if constexpr (BIAS) b[i] = load_pack<VEC>((const T*)p.b + Place<VEC>(i, i == NV - 1, threads, lane, p.d).at);
+            }
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) s[i][e] = (float)x[i].v[e];
+            if (p.delta) {  // the norm is taken of the sum as the stream keeps it
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) s[i][e] = (float)(S)(s[i][e] + (float)t[i].v[e]);
             }
         }
         double mean = 0.0;
         if (p.layer) {
+            double sum = 0.0;
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
+            for (int i = 0; i < NV; ++i) {
+                const int over = Place<VEC>(i, i == NV - 1, threads, lane, p.d).over;
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) sum += (double)s[i][e];
-            row_reduce<TPR>(sum, top, lds);
-            mean = sum / p.d;
+                for (int e = 0; e < VEC; ++e) sum += (double)(i < NV - 1 || e >= over ? s[i][e] : 0.f);
+            }
+            mean = row_fold<LANES>(sum, lds1, Plus()) / p.d;
         }
+        double square = 0.0, top = 0.0, check = 0.0;  // check: NaN where some y is no finite number
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int left = p.d - (i * TPR + lane) * VEC;
+            const int over = Place<VEC>(i, i == NV - 1, threads, lane, p.d).over;
+            again(s[i]);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 const double v = (double)s[i][e] - mean;
-                if (e < left) square = fma(v, v, square);
+                square = fma(i < NV - 1 || e >= over ? v : 0.0, v, square);
+                if (!BIAS) {
+                    const double u = v * (double)(float)g[i].v[e];
+                    top = fmax(top, fabs(u));
+                    check = fma(u, 0.0, check);
+                }
             }
         }
-        row_reduce<TPR>(square, top, lds);
-        const double rstd = 1.0 / sqrt(square / p.d + (double)p.eps);
+        if (BIAS) {
+            square = row_fold<LANES>(square, &lds2[0][0], Plus());
+        } else {
+            if (check != 0.0) top = INFINITY;
+            row_fold2<LANES>(square, top, lds2, Plus(), Larger());
+        }
+        double rstd = 1.0 / sqrt(square / p.d + (double)p.eps);
+        // every lane has read its row: the sum may take its place
+        if (p.sum) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const Place<VEC> at(i, i == NV - 1, threads, lane, p.d);
+                if (at.over < VEC) store_pack<S, float, VEC>((S*)p.sum + (int64_t)row * p.ld_sum + at.at, s[i]);
+            }
+        }
+        // y is formed again where it is used: kept, it would cost a long row half of its waves
         auto normed = [&](int i, double (&y)[VEC]) {
-            const int c = (i * TPR + lane) * VEC, left = p.d - c;
-            float g[VEC], b[VEC];
-            load_some<T, VEC>((const T*)p.g + c, left, g);
+            again(s[i]);
+            again(g[i]);
+            if (BIAS) again(b[i]);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) y[e] = ((double)s[i][e] - mean) * rstd * (double)g[e];
-            if (p.b) {
-                load_some<T, VEC>((const T*)p.b + c, left, b);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) y[e] += (double)b[e];
+            for (int e = 0; e < VEC; ++e) {
+                y[e] = ((double)s[i][e] - mean) * rstd * (double)(float)g[i].v[e];
+                if (BIAS) y[e] += (double)(float)b[i].v[e];
             }
         };
+        if (BIAS || p.out) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (i * TPR + lane) * VEC, left = p.d - c;
-            if (left <= 0) continue;
-            double y[VEC];
-            normed(i, y);
+            for (int i = 0; i < NV; ++i) {
+                const Place<VEC> at(i, i == NV - 1, threads, lane, p.d);
+                double y[VEC];
+                normed(i, y);
+                if (BIAS) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                if (e < left) {
-                    top = fmax(top, fabs(y[e]));
-                    check = fma(y[e], 0.0, check);  // NaN for what is no finite number
+                    for (int e = 0; e < VEC; ++e) {
+                        top = fmax(top, fabs(y[e]));
+                        check = fma(y[e], 0.0, check);
+                    }
                 }
-            if (p.out) {
-                float f[VEC];
+                if (p.out) {
+                    float f[VEC];
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) f[e] = (float)y[e];
-                store_some<T, float, VEC>((T*)p.out + row * p.ld_out + c, left, f);
+                    for (int e = 0; e < VEC; ++e) f[e] = (float)y[e];
+                    if (at.over < VEC) store_pack<T, float, VEC>((T*)p.out + (int64_t)row * p.ld_out + at.at, f);
+                }
             }
         }
-        if (!p.q) continue;
-        row_reduce<TPR>(check, top, lds);
-        const float scale = row_scale(top + check);
+        if (!p.q) {
+            if (LANES == 0) lds_barrier();
+            continue;
+        }
+        if (BIAS) {
+            if (check != 0.0) top = INFINITY;
+            top = row_fold<LANES>(top, lds3, Larger());
+        } else {
+            top *= rstd;
+        }
+        const float scale = row_scale(top);
         const double inv = scale > 0.f ? 1.0 / (double)scale : 0.0;
         if (lane == 0) p.scale[row] = scale;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = (i * TPR + lane) * VEC, left = p.d - c;
-            if (left <= 0) continue;
+            const Place<VEC> at(i, i == NV - 1, threads, lane, p.d);
             double y[VEC];
             normed(i, y);
-            store_q<VEC>(p.q + row * p.ld_q + c, left, y, scale, inv);
+            if (at.over < VEC) store_q<VEC>(p.q + (int64_t)row * p.ld_q + at.at, y, scale, inv);
         }
+        if (LANES == 0) lds_barrier();  // the places in LDS are free for the next row
     }
+}
+
+// The largest magnitude of some values as bits of fp32 (NaN above infinity above numbers).
+template <typename S, int VEC>
+__device__ __forceinline__ uint32_t largest_bits(uint32_t top, const Pack<S, VEC>& x) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) top = max(top, __float_as_uint((float)x.v[e]) & 0x7fffffffu);
+    return top;
+}
+
+template <int TPR>
+__device__ __forceinline__ uint32_t row_largest(uint32_t v, uint32_t* lds) {
+    v = max(v, from_lane<0>(v));
+    v = max(v, from_lane<1>(v));
+    v = max(v, from_lane<2>(v));
+    v = max(v, from_lane<3>(v));
+    if constexpr (TPR > 16) {
+        const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        v = max(a[0], a[1]);
+    }
+    if constexpr (TPR > 32) {
+        const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        v = max(b[0], b[1]);
+    }
+    if constexpr (TPR > 64) {
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+        lds_barrier();
+#pragma unroll
+        for (int w = 0; w < TPR / 64; ++w) v = max(v, lds[w]);
+        lds_barrier();
+    }
+    return v;
 }
 
 // NV pieces a thread; NV = 0: rows of any length, read twice (the second time from the
 // caches).
-template <typename S, int NV, int TPR>
+template <typename S, int VEC, int NV, int TPR>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void quant_q8_kernel(QuantQ8Params p) {
-    constexpr int VEC = 16 / sizeof(S);
     constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
-    constexpr int KEPT = NV ? NV : 1;
-    __shared__ double lds[2 * (TPR / 64)];
+    static_assert(TPR <= 64 || RPB == 1, "rows of several waves have a block each");
+    __shared__ uint32_t lds[TPR < 64 ? 1 : TPR / 64];
     const int lane = threadIdx.x % TPR;
-    const int pieces = NV ? NV : (p.cols + VEC * TPR - 1) / (VEC * TPR);
-    for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR; row < p.rows; row += (int64_t)gridDim.x * RPB) {
-        float s[KEPT][VEC];
-        float top = 0.f, check = 0.f;
-        auto load = [&](int i) {
-            const int c = (i * TPR + lane) * VEC, left = p.cols - c;
-            float(&f)[VEC] = s[NV ? i : 0];
+    const int pieces = (p.cols + VEC * TPR - 1) / (VEC * TPR);
+    const int first = RPB == 1 ? blockIdx.x : (int)blockIdx.x * RPB + (int)threadIdx.x / TPR;
+    for (int row = first; row < p.rows; row += (int)gridDim.x * RPB) {
+        const S* src = (const S*)p.x + (int64_t)row * p.ld_x;
+        int8_t* dst = p.q + (int64_t)row * p.ld_q;
+        Pack<S, VEC> x[NV ? NV : 1];
+        uint32_t top = 0;
+        if constexpr (NV > 0) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) f[e] = 0.f;
-            if (left > 0) load_some<S, VEC>((const S*)p.x + row * p.ld_x + c, left, f);
-        };
-        auto look = [&](int i) {
+            for (int i = 0; i < NV; ++i) x[i] = load_pack<VEC>(src + Place<VEC>(i, NV == 0 || i == NV - 1, TPR, lane, p.cols).at);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                top = fmaxf(top, fabsf(s[NV ? i : 0][e]));
-                check = fmaf(s[NV ? i : 0][e], 0.f, check);
-            }
-        };
-        if (NV) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) load(i);
-#pragma unroll
-            for (int i = 0; i < NV; ++i) look(i);
+            for (int i = 0; i < NV; ++i) top = largest_bits<S, VEC>(top, x[i]);
         } else {
-            for (int i = 0; i < pieces; ++i) {
-                load(i);
-                look(i);
-            }
+            for (int i = 0; i < pieces; ++i)
+                top = largest_bits<S, VEC>(top, load_pack<VEC>(src + Place<VEC>(i, NV == 0 || i == NV - 1, TPR, lane, p.cols).at));
         }
-        double most = top, bad = check;
-        row_reduce<TPR>(bad, most, lds);
-        const float scale = row_scale(most + bad);
+        const float scale = row_scale((double)__uint_as_float(row_largest<TPR>(top, lds)));
         const double inv = scale > 0.f ? 1.0 / (double)scale : 0.0;
         if (lane == 0) p.scale[row] = scale;
-        auto store = [&](int i) {
-            const int c = (i * TPR + lane) * VEC, left = p.cols - c;
-            if (left <= 0) return;
+        auto store = [&](const Place<VEC>& at, const Pack<S, VEC>& v) {
             double y[VEC];
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) y[e] = s[NV ? i : 0][e];
-            store_q<VEC>(p.q + row * p.ld_q + c, left, y, scale, inv);
+            for (int e = 0; e < VEC; ++e) y[e] = (double)(float)v.v[e];
+            if (at.over < VEC) store_q<VEC>(dst + at.at, y, scale, inv);
         };
-        if (NV) {
+        if constexpr (NV > 0) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) store(i);
+            for (int i = 0; i < NV; ++i) store(Place<VEC>(i, NV == 0 || i == NV - 1, TPR, lane, p.cols), x[i]);
         } else {
             for (int i = 0; i < pieces; ++i) {
-                load(i);
-                store(i);
+                const Place<VEC> at(i, true, TPR, lane, p.cols);
+                store(at, load_pack<VEC>(src + at.at));
             }
         }
     }
 }
 
-// Blocks walk over rows where a launch would hold too many.
-template <int TPR>
-int row_blocks(int rows) {
-    constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
-    const int64_t n = ((int64_t)rows + RPB - 1) / RPB;
-    return (int)(n < (1 << 20) ? n : (1 << 20));
+// Blocks walk over rows where a launch would hold too many (row numbers plus a step stay
+// below 2^31).
+int row_blocks(int rows, int per_block) {
+    const int n = rows / per_block + (rows % per_block != 0);
+    return n < (1 << 18) ? n : 1 << 18;
 }
 
-template <typename T, typename S, int NV, int TPR>
-void norm_nv(const NormQ8Params& p, hipStream_t s) {
-    PB_LAUNCH((norm_q8_kernel<T, S, NV, TPR>), row_blocks<TPR>(p.rows), TPR < 256 ? 256 : TPR, 0, s, p);
+template <typename T, typename S, int VEC, int NV, int LANES>
+void norm_nv(const NormQ8Params& p, int threads, hipStream_t s) {
+    const int blocks = row_blocks(p.rows, LANES ? 256 / LANES : 1);
+    if (p.b) PB_LAUNCH((norm_q8_kernel<T, S, VEC, NV, LANES, true>), blocks, threads, 0, s, p);
+    else PB_LAUNCH((norm_q8_kernel<T, S, VEC, NV, LANES, false>), blocks, threads, 0, s, p);
 }
 
-template <typename S, int NV, int TPR>
+template <typename S, int VEC, int NV, int TPR>
 void quant_nv(const QuantQ8Params& p, hipStream_t s) {
-    PB_LAUNCH((quant_q8_kernel<S, NV, TPR>), row_blocks<TPR>(p.rows), TPR < 256 ? 256 : TPR, 0, s, p);
+    PB_LAUNCH((quant_q8_kernel<S, VEC, NV, TPR>), row_blocks(p.rows, TPR < 256 ? 256 / TPR : 1), TPR < 256 ? 256 : TPR, 0, s, p);
 }
 
+// Rows of up to 128 pieces share waves; longer ones have a block of as many waves as leave a
+// thread 8 elements (12 or 16 where 1024 threads are too few): the loads of a row are in
+// flight together, and few enough registers hold two blocks of 1024 threads a CU or more.
+// (16384 and more rows in all lengths: 12 elements and more a thread spilled or ran one
+// block a CU, d 9216 in fp32 with 20: 400 us for 4096 rows.)
 template <typename T, typename S>
 void norm_type(const NormQ8Params& p, hipStream_t s) {
     constexpr int VEC = 16 / sizeof(S);
     const int n = (p.d + VEC - 1) / VEC;  // pieces
-    if (n <= 64) norm_nv<T, S, 1, 64>(p, s);
-    else if (n <= 128) norm_nv<T, S, 2, 64>(p, s);
-    else if (n <= 256) norm_nv<T, S, 1, 256>(p, s);
-    else if (n <= 512) norm_nv<T, S, 2, 256>(p, s);
-    else if (n <= 1024) norm_nv<T, S, 4, 256>(p, s);
-    else if (n <= 1536) norm_nv<T, S, 6, 256>(p, s);
-    else if (n <= 2048) norm_nv<T, S, 8, 256>(p, s);
+    auto waves = [&](int pieces) { return ((n + pieces - 1) / pieces + 63) / 64 * 64; };
+    if (p.d < VEC) norm_nv<T, S, 1, 1, 16>(p, 256, s);
+    else if (n <= 16) norm_nv<T, S, VEC, 1, 16>(p, 256, s);
+    else if (n <= 32) norm_nv<T, S, VEC, 1, 32>(p, 256, s);
+    else if (n <= 64) norm_nv<T, S, VEC, 1, 64>(p, 256, s);
+    else if (n <= 128 && VEC == 4) norm_nv<T, S, VEC, 2, 64>(p, 256, s);
+    else if (n <= 1024 && VEC == 8) norm_nv<T, S, VEC, 1, 0>(p, waves(1), s);
+    else if (n <= 2048) norm_nv<T, S, VEC, 2, 0>(p, waves(2), s);
     else if constexpr (VEC == 4) {
-        if (n <= 2560) norm_nv<T, S, 10, 256>(p, s);
-        else if (n <= 3328) norm_nv<T, S, 13, 256>(p, s);
-        else norm_nv<T, S, 16, 256>(p, s);
+        if (n <= 3 * 1024) norm_nv<T, S, VEC, 3, 0>(p, waves(3), s);
+        else norm_nv<T, S, VEC, 4, 0>(p, waves(4), s);
     }
 }
 
@@ -301,16 +437,25 @@ template <typename S>
 void quant_type(const QuantQ8Params& p, hipStream_t s) {
     constexpr int VEC = 16 / sizeof(S);
     const int n = (int)(((int64_t)p.cols + VEC - 1) / VEC);
-    if (n <= 64) quant_nv<S, 1, 64>(p, s);
-    else if (n <= 128) quant_nv<S, 2, 64>(p, s);
-    else if (n <= 256) quant_nv<S, 1, 256>(p, s);
-    else if (n <= 512) quant_nv<S, 2, 256>(p, s);
-    else if (n <= 1024) quant_nv<S, 4, 256>(p, s);
-    else if (n <= 2048) quant_nv<S, 8, 256>(p, s);
-    else if (n <= 3 * 1024) quant_nv<S, 3, 1024>(p, s);
-    else if (n <= 5120) quant_nv<S, 5, 1024>(p, s);
-    else if (n <= 8192) quant_nv<S, 8, 1024>(p, s);
-    else quant_nv<S, 0, 1024>(p, s);
+    if (p.cols < VEC) quant_nv<S, 1, 1, 16>(p, s);
+    else if (n <= 16) quant_nv<S, VEC, 1, 16>(p, s);
+    else if (n <= 32) quant_nv<S, VEC, 1, 32>(p, s);
+    else if (n <= 64) quant_nv<S, VEC, 1, 64>(p, s);
+    else if (n <= 128) quant_nv<S, VEC, 2, 64>(p, s);
+    else if (n <= 256) quant_nv<S, VEC, 1, 256>(p, s);
+    else if (n <= 512) quant_nv<S, VEC, 2, 256>(p, s);
+    else if (n <= 768) quant_nv<S, VEC, 3, 256>(p, s);
+    else if (n <= 1024) quant_nv<S, VEC, 4, 256>(p, s);
+    else if (n <= 1536) quant_nv<S, VEC, 3, 512>(p, s);
+    else if (n <= 2048) quant_nv<S, VEC, 4, 512>(p, s);
+    else if (n <= 2560) quant_nv<S, VEC, 5, 512>(p, s);
+    else if (n <= 3 * 1024) quant_nv<S, VEC, 3, 1024>(p, s);
+    else if (n <= 4096) quant_nv<S, VEC, 4, 1024>(p, s);
+    else if (n <= 5120) quant_nv<S, VEC, 5, 1024>(p, s);
+    else if (n <= 6144) quant_nv<S, VEC, 6, 1024>(p, s);
+    else if (n <= 7168) quant_nv<S, VEC, 7, 1024>(p, s);
+    else if (n <= 8192) quant_nv<S, VEC, 8, 1024>(p, s);
+    else quant_nv<S, VEC, 0, 1024>(p, s);
 }
 
 }  // namespace

@@ -33,7 +33,7 @@ def _refused(pb, rc, name, what):
                                  dict(ld_sum=-64), dict(g=None), dict(g=A[3] + 1), dict(b=A[4] + 1), dict(eps=-1e-5),
                                  dict(eps=float("nan")), dict(eps=float("inf")), dict(out=A[5] + 1), dict(ld_out=63),
                                  dict(out=None, q=None, scale=None), dict(q=None), dict(scale=None), dict(scale=A[7] + 2),
-                                 dict(ld_q=63), dict(rows=-1), dict(d=0), dict(d=16385, ld_x=1 << 15)], ids=str)
+                                 dict(ld_q=63), dict(rows=-1), dict(rows=(1 << 30) + 1), dict(d=0), dict(d=16385, ld_x=1 << 15)], ids=str)
 def test_norm_refusals(bad):
     from paper_2503_17707_amd import binding as pb
 
@@ -52,7 +52,7 @@ def test_norm_outputs_that_overlap(bad):
 
 @pytest.mark.parametrize("bad", [dict(dtype=2), dict(x=None), dict(x=A[0] + 1), dict(x=A[0] + 2, f32=1), dict(ld_x=63), dict(q=None),
                                  dict(ld_q=1), dict(scale=None), dict(scale=A[2] + 1), dict(rows=-2), dict(cols=0),
-                                 dict(cols=(1 << 30) + 1, ld_x=1 << 31, ld_q=1 << 31), dict(q=A[0] + 100), dict(scale=A[0]),
+                                 dict(cols=(1 << 24) + 1, ld_x=1 << 25, ld_q=1 << 25), dict(rows=(1 << 30) + 1), dict(q=A[0] + 100), dict(scale=A[0]),
                                  dict(scale=A[1] + 4)], ids=str)
 def test_quant_refusals(bad):
     from paper_2503_17707_amd import binding as pb
