@@ -8,7 +8,7 @@
 // the step's 64; which of the 64 a lane holds does not matter as long as both operands
 // agree, and sums of integers do not depend on their order: every variant gives the
 // same bits.
-#include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "../csrc/common.h"
@@ -463,42 +463,36 @@ __global__ __launch_bounds__(64 * WGM * WGN) void q8_ring_kernel(GemmQ8Params p,
 }
 
 // ---- up to 16 tokens: weights from memory into the matrix operands ----------------------
-// 16 NF features a block; its KW waves take pieces of 256 bytes of K in turn and add their
+// 16 features a block; its KW waves take pieces of 256 bytes of K in turn and add their
 // sums through LDS.  Nothing is shared between waves, so weights need no LDS: a wave has
 // the next piece's loads in flight while it multiplies one.  Lanes of tokens that do not
-// exist load nothing and multiply zeros.
-template <int NF, int KW>
+// exist load nothing and multiply zeros.  Bound by launch and load latency up to some 20 MB
+// of weights (one token, N 6144, K 2048: 5.8 us in a recorded graph), by memory above.
+template <int KW>
 __global__ __launch_bounds__(64 * KW) void q8_few_kernel(GemmQ8Params p) {
-    __shared__ i32x4 part[KW][NF][64];
+    __shared__ i32x4 part[KW][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int lr = lane & 15, lg = lane >> 4;
-    const int n0 = (int)blockIdx.x * 16 * NF;
-    const int8_t* w[NF];
-#pragma unroll
-    for (int i = 0; i < NF; ++i) w[i] = p.W + (int64_t)min(n0 + 16 * i + lr, p.N - 1) * p.ldw + 16 * lg;
+    const int n0 = (int)blockIdx.x * 16;
+    const int8_t* w = p.W + (int64_t)min(n0 + lr, p.N - 1) * p.ldw + 16 * lg;
     const int8_t* x = p.X + (int64_t)min(lr, p.M - 1) * p.ldx + 16 * lg;
     const bool here = lr < p.M;
     struct Piece {
-        i32x4 a[4][NF], b[4];
+        i32x4 a[4], b[4];
     };
     auto load = [&](Piece& c, int k) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-#pragma unroll
-            for (int i = 0; i < NF; ++i) c.a[q][i] = __builtin_nontemporal_load((const i32x4*)(w[i] + k + 64 * q));
-        }
+        for (int q = 0; q < 4; ++q) c.a[q] = __builtin_nontemporal_load((const i32x4*)(w + k + 64 * q));
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             c.b[q] = i32x4{0, 0, 0, 0};
             if (here) c.b[q] = *(const i32x4*)(x + k + 64 * q);
         }
     };
-    i32x4 acc[NF] = {};
+    i32x4 acc = {0, 0, 0, 0};
     auto multiply = [&](const Piece& c) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-            for (int i = 0; i < NF; ++i) acc[i] = mma8(c.a[q][i], c.b[q], acc[i]);
+        for (int q = 0; q < 4; ++q) acc = mma8(c.a[q], c.b[q], acc);
     };
     const int pieces = p.K / 256;
     Piece c0, c1;
@@ -513,29 +507,19 @@ __global__ __launch_bounds__(64 * KW) void q8_few_kernel(GemmQ8Params p) {
     if (pieces * 256 < p.K && wave == pieces % KW) {  // the rest, to the wave whose turn it is
         for (int k = pieces * 256; k < p.K; k += 64) {
             const bool in = k + 16 * lg < p.K;
-            i32x4 b = {0, 0, 0, 0};
+            i32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
+            if (in) a = *(const i32x4*)(w + k);
             if (in && here) b = *(const i32x4*)(x + k);
-#pragma unroll
-            for (int i = 0; i < NF; ++i) {
-                i32x4 a = {0, 0, 0, 0};
-                if (in) a = *(const i32x4*)(w[i] + k);
-                acc[i] = mma8(a, b, acc[i]);
-            }
+            acc = mma8(a, b, acc);
         }
     }
-#pragma unroll
-    for (int i = 0; i < NF; ++i) part[wave][i][lane] = acc[i];
+    part[wave][lane] = acc;
     __syncthreads();
-    for (int i = wave; i < NF; i += KW) {
-        i32x4 v = part[0][i][lane];
+    if (wave > 0) return;
 #pragma unroll
-        for (int k = 1; k < KW; ++k) {
-            const i32x4 o = part[k][i][lane];
-            v += o;
-        }
-        const int n = n0 + 16 * i + 4 * lg;
-        if (here && n < p.N) epilogue8(p, lr, n, p.sx[lr], load_features(p, n), v);
-    }
+    for (int k = 1; k < KW; ++k) acc += part[k][lane];
+    const int n = n0 + 4 * lg;
+    if (here && n < p.N) epilogue8(p, lr, n, p.sx[lr], load_features(p, n), acc);
 }
 
 // ---- the sums of split tiles -------------------------------------------------------------
@@ -565,24 +549,117 @@ __global__ __launch_bounds__(256) void q8_join_kernel(GemmQ8Params p, Split sp) 
 
 // ---- launches ----------------------------------------------------------------------------
 
-enum Kind { FEW, RING_32, RING_64, RING_128, WIDE };
+enum Kind { FEW, RING, WIDE };
 
-// splits > 1: the K tiles of the last `tail` tiles in that many ranges.
-struct Plan {
+// A kernel and what its launches cost, in us: `start` and `both` as below; a K step (bk
+// bytes of it) of all blocks at once; the weights' bytes at tbs TB/s; `skew`: the share by
+// which a step grows where rows do not start on 128 bytes; a further round of blocks; a
+// join and its bytes; `channels`: the share by which weights slow down where the ranges
+// are a multiple of 4 KB apart and read the same memory channels.
+struct Shape {
     Kind kind;
-    int bm, bn, bk;
-    int splits, tail;
+    int bm, bn, bk, threads_or_waves, slots;  // slots: blocks that run at once on 256 CUs
+    float start, step, tbs, both, skew, round, join, join_tbs, channels;
 };
 
-int64_t tiles_of(const GemmQ8Params& p, int bm, int bn) {
-    return (((int64_t)p.M + bm - 1) / bm) * (((int64_t)p.N + bn - 1) / bn);
+// Fitted to 13 000 launches of 420 products (M 1 .. 4096, N 64 .. 50272, K 16 .. 36864, cold
+// weights, in recorded graphs; mean error 4-9% a kernel).  The chosen kernel and split was 2.0%
+// above the fastest of 15 kernels in up to 16 splits in the mean, 7% at the 90th percentile.
+// Kernels that gained less than 0.2% beside these are not kept (16 waves and 32 features for
+// few tokens, 512-byte rows).
+constexpr Shape SHAPES[] = {
+    {FEW, 16, 16, 256, 4, 2048, 2.68f, 0.192f, 5.67f, 1.0f, 0.42f, 0.15f, 0, 0, 0},
+    {FEW, 16, 16, 256, 8, 1024, 2.48f, 0.150f, 3.68f, 0.35f, 0, 3.0f, 0, 0, 0},
+    {RING, 32, 32, 256, 128, 512, 3.18f, 0.246f, 6.75f, 0.63f, 0.27f, 2.0f, 2.5f, 5.9f, 0.14f},
+    {RING, 32, 64, 256, 256, 256, 3.27f, 0.301f, 8.25f, 0.69f, 0.51f, 2.3f, 2.8f, 34.f, 0.15f},
+    {RING, 64, 64, 256, 256, 256, 3.80f, 0.480f, 7.15f, 0.31f, 0.23f, 3.0f, 2.6f, 26.f, 0.18f},
+    {RING, 64, 128, 128, 512, 256, 3.87f, 0.339f, 8.99f, 0.65f, 0.48f, 2.6f, 2.0f, 10.4f, 0.29f},
+    {RING, 128, 64, 256, 256, 256, 5.69f, 0.721f, 5.28f, 0.11f, 0.11f, 4.0f, 1.9f, 31.f, 0.09f},
+    {RING, 128, 128, 128, 512, 256, 5.49f, 0.474f, 7.47f, 0.35f, 0.38f, 4.3f, 2.2f, 11.4f, 0.27f},
+    {WIDE, 128, 256, 128, 512, 256, 8.74f, 0.717f, 8.78f, 0.64f, 0.60f, 5.6f, 1.2f, 10.8f, 0.29f},
+    {WIDE, 192, 256, 128, 512, 256, 11.1f, 0.901f, 7.85f, 0.36f, 0.37f, 7.9f, 0.2f, 10.6f, 0.43f},
+    {WIDE, 256, 256, 128, 512, 256, 12.8f, 1.090f, 6.19f, 0.09f, 0.40f, 10.1f, 0.0f, 11.0f, 0.67f},
+};
+constexpr int N_SHAPES = sizeof(SHAPES) / sizeof(SHAPES[0]);
+
+// splits > 1: the K steps of the last `tail` tiles in that many ranges.
+struct Plan {
+    int shape, splits, tail;
+};
+
+int tiles_of(const GemmQ8Params& p, const Shape& c) { return ((p.M + c.bm - 1) / c.bm) * ((p.N + c.bn - 1) / c.bn); }
+
+size_t bytes_of(const Plan& c) {
+    return c.splits > 1 ? (size_t)c.tail * c.splits * SHAPES[c.shape].bm * SHAPES[c.shape].bn * 4 : 0;
 }
 
-size_t bytes_of(const Plan& c) { return c.splits > 1 ? (size_t)c.tail * c.splits * c.bm * c.bn * 4 : 0; }
+// Predicted time of a launch: whole rounds of tiles, then what is left of them, then the
+// ranges of split tiles, each round as long as its K steps; beside it the weights, of the
+// shorter one the share `both`.
+float time_of(const GemmQ8Params& p, const Plan& plan, int tiles, int whole) {
+    const Shape& c = SHAPES[plan.shape];
+    int kt = whole, splits = 1, tail = 0;
+    if (plan.splits > 1) {
+        kt = (whole + plan.splits - 1) / plan.splits;
+        splits = (whole + kt - 1) / kt;
+        tail = splits > 1 ? plan.tail : 0;
+    }
+    const int rounds = (tiles - tail + c.slots - 1) / c.slots, cut = (tail * splits + c.slots - 1) / c.slots;
+    float work = (float)(rounds * whole + cut * kt) * c.step, weights = (float)p.N * (float)p.K * 1e-6f / c.tbs;
+    if (p.K % 128) work *= 1.f + c.skew;
+    if (c.kind == FEW) work *= 1.f + (c.threads_or_waves == 4 ? 0.103f : 0.045f) * (float)p.M;
+    if (tail && kt * c.bk % 4096 == 0) weights *= 1.f + c.channels;
+    float t = c.start + fmaxf(work, weights) + c.both * fminf(work, weights) + (float)(rounds + cut - 1) * c.round;
+    if (p.K % c.bk) t += 0.6f;
+    // (0.5: the join's launch where no graph replays it)
+    if (tail) t += c.join + 0.5f + (float)tail * (float)splits * (float)(c.bm * c.bn) * 8e-6f / c.join_tbs;
+    return t;
+}
+
+Plan plan_of(const GemmQ8Params& p, size_t room) {
+    Plan best{-1, 1, 0};
+    float best_t = 0.f;
+    auto consider = [&](const Plan& c, int tiles, int whole) {
+        if (bytes_of(c) > room) return;
+        const float t = time_of(p, c, tiles, whole);
+        if (best.shape >= 0 && t >= best_t) return;
+        best = c;
+        best_t = t;
+    };
+    for (int i = 0; i < N_SHAPES; ++i) {
+        const Shape& c = SHAPES[i];
+        if (c.kind == FEW) {
+            // measured side by side: 4 waves from 12288 features on, where blocks are many
+            if (p.M <= 16 && (c.threads_or_waves == 4) == (p.N >= 12288)) consider({i, 1, 0}, tiles_of(p, c), p.K / c.bk);
+            continue;
+        }
+        if (c.kind == WIDE ? p.M <= 64 || p.K < 128 : c.bm == 32 ? p.M > 64 : c.bm == 64 ? p.M > 512 : p.M <= 32) continue;
+        const int tiles = tiles_of(p, c), whole = p.K / c.bk;
+        consider({i, 1, 0}, tiles, whole);
+        // the splits that come next to filling the chip: of all tiles, or of a last round's
+        int tried = 0;
+        if (tiles < c.slots) {
+            for (const int s : {16, 12, 8, 6, 5, 4, 3, 2})
+                if (tried < 3 && s * tiles <= c.slots && whole >= 2 * s) {
+                    consider({i, s, tiles}, tiles, whole);
+                    ++tried;
+                }
+            if (!tried && whole >= 4) consider({i, 2, tiles}, tiles, whole);
+        } else if (const int tail = tiles % 256) {
+            for (const int s : {8, 6, 5, 4, 3, 2})
+                if (tried < 2 && s * tail <= 256 && whole >= 2 * s) {
+                    consider({i, s, tail}, tiles, whole);
+                    ++tried;
+                }
+        }
+    }
+    return best;
+}
 
 template <int BM, int BN, typename F>
-void launch_tiles(F kernel, int threads, const GemmQ8Params& p, const Plan& c, hipStream_t s) {
-    const int tiles = (int)tiles_of(p, BM, BN), whole = p.K / c.bk;
+void launch_tiles(F kernel, const GemmQ8Params& p, const Plan& c, hipStream_t s) {
+    const Shape& shape = SHAPES[c.shape];
+    const int tiles = tiles_of(p, shape), whole = p.K / shape.bk;
     Split sp{tiles, 0, 1, whole};
     if (c.splits > 1) {
         sp.kt = (whole + c.splits - 1) / c.splits;
@@ -592,68 +669,34 @@ void launch_tiles(F kernel, int threads, const GemmQ8Params& p, const Plan& c, h
             sp.full = tiles - c.tail;
         }
     }
-    PB_LAUNCH(kernel, sp.full + sp.tail * sp.splits, threads, 0, s, p, sp);
-    if (sp.tail)
-        PB_LAUNCH((q8_join_kernel<BM, BN>), sp.tail * (BM * BN / 4 / 256), 256, 0, s, p, sp);
-}
-
-template <int XF>
-void launch_wide(const GemmQ8Params& p, const Plan& c, hipStream_t s) {
-    launch_tiles<64 * XF, 256>(q8_wide_kernel<XF>, 512, p, c, s);
+    PB_LAUNCH(kernel, sp.full + sp.tail * sp.splits, shape.threads_or_waves, 0, s, p, sp);
+    if (sp.tail) PB_LAUNCH((q8_join_kernel<BM, BN>), sp.tail * (BM * BN / 4 / 256), 256, 0, s, p, sp);
 }
 
 template <int BM, int BN, int WGM, int WGN, int BK, int S>
 void launch_ring(const GemmQ8Params& p, const Plan& c, hipStream_t s) {
-    launch_tiles<BM, BN>(q8_ring_kernel<BM, BN, WGM, WGN, BK, S>, 64 * WGM * WGN, p, c, s);
+    launch_tiles<BM, BN>(q8_ring_kernel<BM, BN, WGM, WGN, BK, S>, p, c, s);
 }
 
-template <int NF, int KW>
+template <int KW>
 void launch_few(const GemmQ8Params& p, hipStream_t s) {
-    PB_LAUNCH((q8_few_kernel<NF, KW>), (p.N + 16 * NF - 1) / (16 * NF), 64 * KW, 0, s, p);
+    PB_LAUNCH((q8_few_kernel<KW>), (p.N + 15) / 16, 64 * KW, 0, s, p);
 }
 
 void launch_plan(const GemmQ8Params& p, const Plan& c, hipStream_t s) {
-    switch (c.kind) {
-        case FEW:  // bn: features, bk: waves
-            if (c.bn == 16 && c.bk == 4) launch_few<1, 4>(p, s);
-            else if (c.bn == 16 && c.bk == 8) launch_few<1, 8>(p, s);
-            else if (c.bn == 16) launch_few<1, 16>(p, s);
-            else if (c.bk == 4) launch_few<2, 4>(p, s);
-            else launch_few<2, 8>(p, s);
-            break;
-        case RING_32:
-            if (c.bn == 32) launch_ring<32, 32, 1, 2, 256, 4>(p, c, s);
-            else if (c.bk == 256) launch_ring<32, 64, 1, 4, 256, 4>(p, c, s);
-            else launch_ring<32, 64, 1, 4, 512, 3>(p, c, s);
-            break;
-        case RING_64:
-            if (c.bn == 64) launch_ring<64, 64, 1, 4, 256, 4>(p, c, s);
-            else launch_ring<64, 128, 2, 4, 128, 4>(p, c, s);
-            break;
-        case RING_128:
-            if (c.bn == 64) launch_ring<128, 64, 2, 2, 256, 3>(p, c, s);
-            else launch_ring<128, 128, 2, 4, 128, 4>(p, c, s);
-            break;
-        case WIDE:
-            if (c.bm == 128) launch_wide<2>(p, c, s);
-            else if (c.bm == 192) launch_wide<3>(p, c, s);
-            else launch_wide<4>(p, c, s);
-            break;
+    switch (c.shape) {
+        case 0: launch_few<4>(p, s); break;
+        case 1: launch_few<8>(p, s); break;
+        case 2: launch_ring<32, 32, 1, 2, 256, 4>(p, c, s); break;
+        case 3: launch_ring<32, 64, 1, 4, 256, 4>(p, c, s); break;
+        case 4: launch_ring<64, 64, 1, 4, 256, 4>(p, c, s); break;
+        case 5: launch_ring<64, 128, 2, 4, 128, 4>(p, c, s); break;
+        case 6: launch_ring<128, 64, 2, 2, 256, 3>(p, c, s); break;
+        case 7: launch_ring<128, 128, 2, 4, 128, 4>(p, c, s); break;
+        case 8: launch_tiles<128, 256>(q8_wide_kernel<2>, p, c, s); break;
+        case 9: launch_tiles<192, 256>(q8_wide_kernel<3>, p, c, s); break;
+        case 10: launch_tiles<256, 256>(q8_wide_kernel<4>, p, c, s); break;
     }
-}
-
-
-Plan plan_of(const GemmQ8Params& p, size_t room) {
-    if (p.M <= 16) return {FEW, 16, 16, p.N / 16 <= 256 && p.K >= 4096 ? 16 : 8, 1, 0};
-    Plan c = p.M <= 32 ? Plan{RING_32, 32, 64, 256, 1, 0} : p.M <= 512 || p.K < 256 ? Plan{RING_128, 128, 128, 128, 1, 0}
-             : Plan{WIDE, 256, 256, 128, 1, 0};
-    const int64_t tiles = tiles_of(p, c.bm, c.bn);
-    if (tiles < 256) {
-        const int s = (int)std::min<int64_t>({256 / tiles, 8, std::max(1, p.K / c.bk / 8)});
-        const Plan cut{c.kind, c.bm, c.bn, c.bk, s, (int)tiles};
-        if (s > 1 && bytes_of(cut) <= room) return cut;
-    }
-    return c;
 }
 
 }  // namespace
