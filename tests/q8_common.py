@@ -58,7 +58,7 @@ def check_rows8(q, scale, y, err, what=""):
 
 
 def gemm64(X, sx, W, sw, bias, epi, qscale, qcols, old, dt):
-    """(out, tolerance) in float64, on the CPU.
+    """(out, tolerance) in float64.
 
     The integer sum is exact; it is rounded to fp32, multiplied by sx, multiplied by sw and
     added to the bias with one rounding, multiplied by qscale, added to the old value: each
@@ -69,7 +69,7 @@ def gemm64(X, sx, W, sw, bias, epi, qscale, qcols, old, dt):
     y = p + (0 if bias is None else bias.double()[None])
     tol = 2.01 * u * p.abs() + u * y.abs()
     if epi == 0:
-        f = torch.where(torch.arange(W.shape[0]) < qcols, float(np.float32(qscale)), 1.0)[None]
+        f = torch.where(torch.arange(W.shape[0], device=W.device) < qcols, float(np.float32(qscale)), 1.0)[None]
         y, tol = y * f, tol * f + u * (y * f).abs()
     elif epi == 1:
         y = y.clamp(min=0)

@@ -82,6 +82,49 @@ def test_sizes(M, N, K):
         _check(c, got, epi, kind)
 
 
+# Small products that the rule of sizes gives to each kernel: whole tiles, all tiles split, the
+# last round's split; K in whole steps and with a rest.
+KERNELS = [
+    (1, 12373, 256), (13, 15858, 64), (1, 32, 256), (1, 32, 64),  # up to 16 tokens
+    (1, 44, 9984), (1, 32, 7552), (1, 16552, 7392), (17, 32, 256), (19, 35, 80),  # 32 x 32
+    (1, 677, 8192), (1, 637, 8320), (1, 18401, 7680), (1, 16437, 8064), (1, 12100, 768), (1, 12199, 640),  # 32 x 64
+    (67, 36, 11520), (76, 47, 9520), (48, 17268, 8704), (1, 19002, 7856), (78, 33, 256), (67, 36, 64),  # 64 x 64
+    (11, 49, 5760), (68, 32, 2240), (68, 32, 128), (20, 16566, 64),  # 64 x 128
+    (597, 32, 2048), (523, 32, 2608), (76, 18124, 3760), (589, 36, 256), (520, 35, 160),  # 128 x 64
+    (616, 32, 1408), (549, 40, 1936), (648, 5403, 2816), (493, 8400, 1888), (593, 33, 128), (555, 32, 80),  # 128 x 128
+    (1054, 1222, 8320), (863, 1775, 9632), (970, 8278, 14208), (135, 22328, 128), (132, 22859, 160),  # 128 x 256
+    (142, 6242, 10240), (134, 7007, 8784), (1294, 12451, 2176), (566, 27430, 1472), (283, 23145, 128),
+    (306, 26156, 144),  # 192 x 256
+    (227, 8456, 9600), (229, 5384, 10704), (983, 16718, 1664), (683, 21867, 1616), (402, 22195, 128),
+    (400, 26092, 144),  # 256 x 256
+]
+
+
+@pytest.mark.parametrize("M,N,K", KERNELS)
+def test_every_kernel(M, N, K):
+    import torch
+
+    from paper_2503_17707_amd import binding as pb
+    from q8_common import gemm64
+
+    log("gemm", M, N, K)
+    g = torch.Generator("cuda").manual_seed(M + N + K)
+    draw = lambda *of: torch.randint(-128, 128, of, generator=g, device="cuda").to(torch.int8)  # noqa: E731
+    X, W = draw(M, K), draw(N, K)
+    sx = torch.rand(M, generator=g, device="cuda") * 0.02 + 0.01
+    sw = torch.rand(N, generator=g, device="cuda") * 0.01 / math.sqrt(K) + 1e-4
+    bias = torch.randn(N, generator=g, device="cuda").half()
+    old = torch.randn(M, N, generator=g, device="cuda")
+    R = old.clone()
+    pb.op_gemm_q8(1, 2, X, sx, W, sw, bias, R=R, workspace=_ws(M, N, K))
+    want, tol = gemm64(X, sx, W, sw, bias, 2, 1.0, 0, old, torch.float16)
+    assert bool(((R.double() - want).abs() <= tol).all())
+    C = torch.zeros(M, N, dtype=torch.float16, device="cuda")
+    pb.op_gemm_q8(1, 1, X, sx, W, sw, bias, C=C, workspace=_ws(M, N, K))
+    want, tol = gemm64(X, sx, W, sw, bias, 1, 1.0, 0, old, torch.float16)
+    assert bool(((C.double() - want).abs() <= tol).all())
+
+
 @pytest.mark.parametrize("M,N,K", [(1, 300, 2048), (7, 130, 1040), (40, 515, 2064), (150, 260, 528), (600, 600, 320),
                                    (2100, 300, 96)])
 @pytest.mark.parametrize("pad", [(16, 48, 8), (112, 16, 1), (4096, 32, 3), (32, 4096, 31)], ids=str)
