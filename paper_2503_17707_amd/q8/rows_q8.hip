@@ -60,6 +60,17 @@ struct Place {
     }
 };
 
+// Element `at` of a row (rows of a block share a scalar base: a lane's part is 32 bits).
+template <typename T>
+__device__ __forceinline__ const T* element(const T* row, uint32_t at) {
+    return (const T*)((const char*)row + (uint32_t)(at * (uint32_t)sizeof(T)));
+}
+
+template <typename T>
+__device__ __forceinline__ T* element(T* row, uint32_t at) {
+    return (T*)((char*)row + (uint32_t)(at * (uint32_t)sizeof(T)));
+}
+
 // Other lanes' values without a way through LDS: within rows of 16 by DPP (quad_perm 1 0
 // 3 2, quad_perm 2 3 0 1, row_half_mirror, row_mirror), across rows by permlane swaps.
 template <int STEP>
@@ -97,11 +108,12 @@ __device__ __forceinline__ double lanes_fold(double v, F f) {
 template <int LANES, typename F>
 __device__ __forceinline__ double row_fold(double v, double* lds, F f) {
     v = lanes_fold<(LANES ? LANES : 64)>(v, f);
-    if constexpr (LANES == 0) {
-        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    if constexpr (LANES == 0) {  // (folds of zero and more than 16 waves there are none)
+        const int lane = threadIdx.x & 63;
+        if (lane == 0) lds[threadIdx.x >> 6] = v;
         lds_barrier();
-        v = lds[0];
-        for (int w = 1; w < (int)blockDim.x / 64; ++w) v = f(v, lds[w]);
+        v = (lane & 15) < (int)blockDim.x / 64 ? lds[lane & 15] : 0.0;
+        v = lanes_fold<16>(v, f);
     }
     return v;
 }
@@ -117,12 +129,10 @@ __device__ __forceinline__ void row_fold2(double& a, double& b, double (*lds)[2]
             lds[threadIdx.x >> 6][1] = b;
         }
         lds_barrier();
-        a = lds[0][0];
-        b = lds[0][1];
-        for (int w = 1; w < (int)blockDim.x / 64; ++w) {
-            a = f(a, lds[w][0]);
-            b = g(b, lds[w][1]);
-        }
+        const int lane = threadIdx.x & 63;
+        const bool in = (lane & 15) < (int)blockDim.x / 64;
+        a = lanes_fold<16>(in ? lds[lane & 15][0] : 0.0, f);
+        b = lanes_fold<16>(in ? lds[lane & 15][1] : 0.0, g);
     }
 }
 
@@ -132,6 +142,12 @@ struct Plus {
 struct Larger {
     __device__ double operator()(double a, double b) const { return fmax(a, b); }
 };
+
+// max(top, |y|) in one instruction (fmax() quiets both operands first; a NaN is left out here).
+__device__ __forceinline__ double max_abs(double top, double y) {
+    asm("v_max_f64 %0, %0, |%1|" : "+v"(top) : "v"(y));
+    return top;
+}
 
 // Keeps the compiler from holding a conversion made before this point: kept as fp64, a
 // row's elements would take the registers of half the waves.
@@ -152,9 +168,27 @@ __device__ __forceinline__ void again(float (&x)[VEC]) {
     for (float& k : x) asm volatile("" : "+v"(k));
 }
 
+// 1 / sqrt(x) and 1 / x from the hardware's approximations and two steps of Newton, a few units
+// of the last place off (the library's are 30 operations and more, of every wave of a row).
+__device__ __forceinline__ double rsqrt64(double x) {
+    double r = __builtin_amdgcn_rsq(x);
+    if (x > 0.0 && x < INFINITY) {
+        r = fma(r * 0.5, fma(-x * r, r, 1.0), r);
+        r = fma(r * 0.5, fma(-x * r, r, 1.0), r);
+    }
+    return r;
+}
+
+__device__ __forceinline__ double reciprocal64(float x) {  // (of a scale; 0 for none)
+    if (!(x > 0.f)) return 0.0;
+    double r = __builtin_amdgcn_rcp((double)x);
+    r = fma(fma(-(double)x, r, 1.0), r, r);
+    return fma(fma(-(double)x, r, 1.0), r, r);
+}
+
 // The scale of a row whose largest magnitude is `top` (NaN: some value is no number).
 __device__ __forceinline__ float row_scale(double top) {
-    const float s = (float)(top / 127.0);
+    const float s = (float)(top * (1.0 / 127.0));
     if (!(s <= 3.402823466e38f)) return __builtin_nanf("");
     return s < 1.17549435e-38f ? 0.f : s;  // rows below it are zeros: a subnormal scale holds too few bits
 }
@@ -177,6 +211,9 @@ __device__ __forceinline__ void store_q(int8_t* p, const double (&y)[VEC], float
     store_pack<int8_t, int, VEC>(p, r);
 }
 
+// (12 fp32 or 16 16-bit elements a thread; 16 fp32 ones leave no registers for more)
+constexpr bool loads_ahead(int vec, int nv, int lanes) { return lanes == 0 && (vec == 4 ? nv == 3 : nv == 2); }
+
 // S: type of the stream, T: storage type.  LANES threads (0: a block) take a row of d >= VEC
 // in NV pieces of VEC elements each; BIAS: b is given (without it the largest magnitude is
 // known with the sum of squares).
@@ -187,50 +224,64 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) __attribute__((amdgpu_waves_per
     const int lane = LANES ? threadIdx.x % LANES : threadIdx.x;
     const int threads = LANES ? LANES : blockDim.x;
     const int first = LANES ? (int)blockIdx.x * RPB + (int)threadIdx.x / LANES : blockIdx.x;
-    for (int row = first; row < p.rows; row += (int)gridDim.x * RPB) {
-        Pack<T, VEC> g[NV], b[NV];
+    const int step = (int)gridDim.x * RPB;
+    // Long rows, whose blocks have a CU to themselves, are walked over, the next one loaded
+    // while one is worked on; gains and biases stay (4096 x 9216: 114 -> 96 us).
+    constexpr bool AHEAD = loads_ahead(VEC, NV, LANES);
+    Pack<S, VEC> x[NV];
+    Pack<T, VEC> t[NV], g[NV], b[NV];
+    auto place = [&](int i) { return Place<VEC>(i, i == NV - 1, threads, lane, p.d); };
+    auto load_row = [&](int row) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) x[i] = load_pack<VEC>(element((const S*)p.x + (int64_t)row * p.ld_x, place(i).at));
+        if (p.delta) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) t[i] = load_pack<VEC>(element((const T*)p.delta + (int64_t)row * p.ld_delta, place(i).at));
+        }
+    };
+    auto load_gains = [&] {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            g[i] = load_pack<VEC>(element((const T*)p.g, place(i).at));
+            if constexpr (BIAS) b[i] = load_pack<VEC>(element((const T*)p.b, place(i).at));
+        }
+    };
+    if (AHEAD) {
+        load_row(min(first, p.rows - 1));
+        load_gains();
+    }
+    for (int row = first; row < p.rows; row += step) {
+        if (!AHEAD) {
+            load_row(row);
+            load_gains();
+        }
         float s[NV][VEC];
-        {
-            Pack<S, VEC> x[NV];
-            Pack<T, VEC> t[NV];
 #pragma unroll
-            for (int i = 0; i < NV; ++i) x[i] = load_pack<VEC>((const S*)p.x + (int64_t)row * p.ld_x + Place<VEC>(i, i == NV - 1, threads, lane, p.d).at);
-            if (p.delta) {
+        for (int i = 0; i < NV; ++i)
 #pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    t[i] = load_pack<VEC>((const T*)p.delta + (int64_t)row * p.ld_delta + Place<VEC>(i, i == NV - 1, threads, lane, p.d).at);
-            }
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                g[i] = load_pack<VEC>((const T*)p.g + Place<VEC>(i, i == NV - 1, threads, lane, p.d).at);
-                if constexpr (BIAS) b[i] = load_pack<VEC>((const T*)p.b + Place<VEC>(i, i == NV - 1, threads, lane, p.d).at);
-            }
+            for (int e = 0; e < VEC; ++e) s[i][e] = (float)x[i].v[e];
+        if (p.delta) {  // the norm is taken of the sum as the stream keeps it
 #pragma unroll
             for (int i = 0; i < NV; ++i)
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) s[i][e] = (float)x[i].v[e];
-            if (p.delta) {  // the norm is taken of the sum as the stream keeps it
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) s[i][e] = (float)(S)(s[i][e] + (float)t[i].v[e]);
-            }
+                for (int e = 0; e < VEC; ++e) s[i][e] = (float)(S)(s[i][e] + (float)t[i].v[e]);
         }
+        if (AHEAD && row + step < p.rows) load_row(row + step);
         double mean = 0.0;
         if (p.layer) {
             double sum = 0.0;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int over = Place<VEC>(i, i == NV - 1, threads, lane, p.d).over;
+                const int over = place(i).over;
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) sum += (double)(i < NV - 1 || e >= over ? s[i][e] : 0.f);
             }
-            mean = row_fold<LANES>(sum, lds1, Plus()) / p.d;
+            mean = row_fold<LANES>(sum, lds1, Plus()) * p.inv_d;
         }
         double square = 0.0, top = 0.0, check = 0.0;  // check: NaN where some y is no finite number
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int over = Place<VEC>(i, i == NV - 1, threads, lane, p.d).over;
+            const int over = place(i).over;
             again(s[i]);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
@@ -238,7 +289,7 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) __attribute__((amdgpu_waves_per
                 square = fma(i < NV - 1 || e >= over ? v : 0.0, v, square);
                 if (!BIAS) {
                     const double u = v * (double)(float)g[i].v[e];
-                    top = fmax(top, fabs(u));
+                    top = max_abs(top, u);
                     check = fma(u, 0.0, check);
                 }
             }
@@ -249,16 +300,18 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) __attribute__((amdgpu_waves_per
             if (check != 0.0) top = INFINITY;
             row_fold2<LANES>(square, top, lds2, Plus(), Larger());
         }
-        double rstd = 1.0 / sqrt(square / p.d + (double)p.eps);
+        double rstd = rsqrt64(fma(square, p.inv_d, (double)p.eps));
         // every lane has read its row: the sum may take its place
         if (p.sum) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const Place<VEC> at(i, i == NV - 1, threads, lane, p.d);
-                if (at.over < VEC) store_pack<S, float, VEC>((S*)p.sum + (int64_t)row * p.ld_sum + at.at, s[i]);
+                const Place<VEC> at = place(i);
+                if (at.over < VEC) store_pack<S, float, VEC>(element((S*)p.sum + (int64_t)row * p.ld_sum, at.at), s[i]);
             }
         }
-        // y is formed again where it is used: kept, it would cost a long row half of its waves
+        // y is kept for the second use where a thread has one piece; of more it is formed again
+        // (kept, it would cost a long row half of its waves)
+        constexpr bool KEPT = NV == 1;
         auto normed = [&](int i, double (&y)[VEC]) {
             again(s[i]);
             again(g[i]);
@@ -269,24 +322,26 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) __attribute__((amdgpu_waves_per
                 if (BIAS) y[e] += (double)(float)b[i].v[e];
             }
         };
+        double y[VEC];
+        if (KEPT) normed(0, y);
         if (BIAS || p.out) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const Place<VEC> at(i, i == NV - 1, threads, lane, p.d);
-                double y[VEC];
-                normed(i, y);
+                const Place<VEC> at = place(i);
+                if (!KEPT) normed(i, y);
                 if (BIAS) {
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) {
-                        top = fmax(top, fabs(y[e]));
+                        top = max_abs(top, y[e]);
                         check = fma(y[e], 0.0, check);
                     }
+                    asm volatile("" : "+v"(check));  // (y is used up here)
                 }
                 if (p.out) {
                     float f[VEC];
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) f[e] = (float)y[e];
-                    if (at.over < VEC) store_pack<T, float, VEC>((T*)p.out + (int64_t)row * p.ld_out + at.at, f);
+                    if (at.over < VEC) store_pack<T, float, VEC>(element((T*)p.out + (int64_t)row * p.ld_out, at.at), f);
                 }
             }
         }
@@ -301,14 +356,13 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) __attribute__((amdgpu_waves_per
             top *= rstd;
         }
         const float scale = row_scale(top);
-        const double inv = scale > 0.f ? 1.0 / (double)scale : 0.0;
+        const double inv = reciprocal64(scale);
         if (lane == 0) p.scale[row] = scale;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const Place<VEC> at(i, i == NV - 1, threads, lane, p.d);
-            double y[VEC];
-            normed(i, y);
-            if (at.over < VEC) store_q<VEC>(p.q + (int64_t)row * p.ld_q + at.at, y, scale, inv);
+            const Place<VEC> at = place(i);
+            if (!KEPT) normed(i, y);
+            if (at.over < VEC) store_q<VEC>(element(p.q + (int64_t)row * p.ld_q, at.at), y, scale, inv);
         }
         if (LANES == 0) lds_barrier();  // the places in LDS are free for the next row
     }
@@ -371,7 +425,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void quant_q8_kernel(QuantQ8
                 top = largest_bits<S, VEC>(top, load_pack<VEC>(src + Place<VEC>(i, NV == 0 || i == NV - 1, TPR, lane, p.cols).at));
         }
         const float scale = row_scale((double)__uint_as_float(row_largest<TPR>(top, lds)));
-        const double inv = scale > 0.f ? 1.0 / (double)scale : 0.0;
+        const double inv = reciprocal64(scale);
         if (lane == 0) p.scale[row] = scale;
         auto store = [&](const Place<VEC>& at, const Pack<S, VEC>& v) {
             double y[VEC];
@@ -400,7 +454,8 @@ int row_blocks(int rows, int per_block) {
 
 template <typename T, typename S, int VEC, int NV, int LANES>
 void norm_nv(const NormQ8Params& p, int threads, hipStream_t s) {
-    const int blocks = row_blocks(p.rows, LANES ? 256 / LANES : 1);
+    int blocks = row_blocks(p.rows, LANES ? 256 / LANES : 1);
+    if (loads_ahead(VEC, NV, LANES) && blocks > 256) blocks = 256;  // one a CU
     if (p.b) PB_LAUNCH((norm_q8_kernel<T, S, VEC, NV, LANES, true>), blocks, threads, 0, s, p);
     else PB_LAUNCH((norm_q8_kernel<T, S, VEC, NV, LANES, false>), blocks, threads, 0, s, p);
 }
@@ -419,7 +474,11 @@ template <typename T, typename S>
 void norm_type(const NormQ8Params& p, hipStream_t s) {
     constexpr int VEC = 16 / sizeof(S);
     const int n = (p.d + VEC - 1) / VEC;  // pieces
-    auto waves = [&](int pieces) { return ((n + pieces - 1) / pieces + 63) / 64 * 64; };
+    auto waves = [&](int pieces) {
+        // (waves in fours, one to each SIMD, where that leaves few idle: 5120 in fp32 96 -> 85 us)
+        const int t = (n + pieces - 1) / pieces, fours = (t + 255) / 256 * 256;
+        return fours * 5 <= t * 6 ? fours : (t + 63) / 64 * 64;
+    };
     if (p.d < VEC) norm_nv<T, S, 1, 1, 16>(p, 256, s);
     else if (n <= 16) norm_nv<T, S, VEC, 1, 16>(p, 256, s);
     else if (n <= 32) norm_nv<T, S, VEC, 1, 32>(p, 256, s);

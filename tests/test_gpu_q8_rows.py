@@ -8,12 +8,24 @@ from gpu_common import log
 pytestmark = pytest.mark.gpu
 
 
+def _out_tolerance(y, b, err, dt):
+    """With e = 2^-24, in fp32: v = (s - mean_hi) - mean_lo has error 2 e |v|, u = v rstd (rstd rounded, one product)
+    4 e |u|, y = u g + b: 4 e |u g| + e |y| <= 5 e |y| + 4 e |b|, and 2^-48 of the mean, below err; then half a step of
+    the type, and half its smallest one."""
+    from q8_common import HALF
+
+    half, least = HALF[dt]
+    e = 2.0 ** -24
+    fp32 = 5.01 * e * y.abs() + (0 if b is None else 4.01 * e * b.double().abs()[None])
+    return err + fp32 + half * (y.abs() + fp32) + least
+
+
 def _norm(kind, rows, d, f32, layer, delta, out, bias, seed=0, eps=1e-5, pad=(0, 0, 0, 0, 0), x=None, in_place=False):
     """One call on rows with `pad` more columns in x, delta, sum, out, q; every output checked."""
     import torch
 
     from paper_2503_17707_amd import binding as pb
-    from q8_common import CODE, DT, HALF, check_rows8, norm64, strided, untouched
+    from q8_common import CODE, DT, check_rows8, norm64, strided, untouched
 
     g = torch.Generator().manual_seed(seed)
     dt = DT[kind]
@@ -41,10 +53,8 @@ def _norm(kind, rows, d, f32, layer, delta, out, bias, seed=0, eps=1e-5, pad=(0,
     y, err = norm64(s, gain, b, layer, eps)
     check_rows8(qv, scale, y, err, (kind, rows, d))
     assert untouched(qb, d, pad[4] // 2)
-    if out:  # to fp32, then to the type
-        half, least = HALF[dt]
-        off = (ov.cpu().double() - y).abs()
-        assert bool((off <= err + (half + 2.0 ** -23) * y.abs() + least).all())
+    if out:  # formed in fp32, then rounded to the type
+        assert bool(((ov.cpu().double() - y).abs() <= _out_tolerance(y, b, err, dt)).all())
         assert untouched(ob, d, pad[3] // 2)
     return qv.clone(), scale
 
@@ -75,13 +85,20 @@ def test_norm_in_place_and_more_rows_than_blocks():
     q2, s2 = _norm("bf16", 70, 300, True, False, True, False, False, seed=5, in_place=True, pad=(4, 0, 0, 0, 4))
     assert bool((q0 == q2).all()) and bool((s0 == s2).all())
     _norm("f16", 3000, 33, False, True, True, True, True, seed=6)
+    # rows that blocks walk over, the next one loaded ahead
+    for rows, d, f32, bias in ((600, 9000, True, True), (513, 9000, True, False), (530, 9216, False, True), (257, 16384, False, False)):
+        for layer in (False, True):
+            q0, s0 = _norm("f16", rows, d, f32, layer, True, False, bias, seed=rows)
+        q1, s1 = _norm("f16", rows, d, f32, layer, True, True, bias, seed=rows, in_place=True)
+        assert bool((q0 == q1).all()) and bool((s0 == s1).all())
+        _norm("bf16", rows, d, f32, layer, False, False, bias, seed=rows, pad=(8, 0, 0, 0, 1))
 
 
 def test_norm_without_quantization_and_with_large_offsets():
     import torch
 
     from paper_2503_17707_amd import binding as pb
-    from q8_common import HALF, norm64
+    from q8_common import norm64
 
     g = torch.Generator().manual_seed(3)
     x = torch.randn(4, 500, generator=g) * 1e-3 + 1e4  # a mean far above the spread
@@ -89,8 +106,7 @@ def test_norm_without_quantization_and_with_large_offsets():
     out = torch.zeros(4, 500, dtype=torch.float16, device="cuda")
     pb.op_norm_q8(1, x.cuda(), gain.cuda(), out=out, layer=True)
     y, err = norm64(x, gain, None, True, 1e-5)
-    half, least = HALF[torch.float16]
-    assert bool(((out.cpu().double() - y).abs() <= err + (half + 2.0 ** -23) * y.abs() + least).all())
+    assert bool(((out.cpu().double() - y).abs() <= _out_tolerance(y, None, err, torch.float16)).all())
 
 
 @pytest.mark.parametrize("f32", [False, True])
