@@ -6,8 +6,12 @@
 // n) and its B operand the tokens m: a lane ends up with four consecutive features of
 // one token.  Lane l gives 16 bytes of row l % 16, the 16 at K offset 16 (l / 16) of
 // the step's 64; which of the 64 a lane holds does not matter as long as both operands
-// agree, and sums of integers do not depend on their order: every variant gives the
-// same bits.
+// agree, and sums of integers do not depend on their order: every kernel and split gives
+// the same bits, so a rule of predicted times chooses freely among them (below).
+//
+// What bounds them: one to some sixty tokens, reading the weights once; thousands, the
+// matrix units (2 M N K operations, twice those of 16 bits a cycle) about as much as the
+// copies that feed them; between, the copies alone (see the wide tiles).
 #include <cmath>
 #include <type_traits>
 
@@ -235,6 +239,15 @@ __device__ __forceinline__ void add_rest(const GemmQ8Params& p, int k0, int mb, 
 // of a wave's copies.  Past the last tile the copies re-read it (nobody reads them).
 // LDS rows are 128 bytes, 16-byte chunks XOR-permuted by row & 7: operand reads of 16
 // rows are free of bank conflicts.
+//
+// 4096 x 36864 x 9216: 1016 us, 2.74 POP/s (the vendor library's 8-bit product 1212 us).  All
+// tile heights copy 42-46 GB/s a CU (11 TB/s in all) into LDS, and that is the bound: one
+// round of 240 blocks (M 1511, N 4992, K 5120) takes 46.8 us with cold weights, 45 with a
+// sixteenth of its products, 36.7 if every copy finds its lines in the L2, 32.4 without
+// copies; of the large tile of 4096 tokens products and copies alone take 0.87 of the time
+// each.  So a block takes as many tokens as fill tiles.  Two phases a tile, three stages, stages
+// of uneven depth for tokens and weights and K ranges that start apart took as long, weights
+// from memory into registers 1.7 times as long.
 template <int XF>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void q8_wide_kernel(GemmQ8Params p, Split sp) {
     constexpr int BM = 64 * XF, BN = 256, RB = 128;
@@ -379,8 +392,10 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void q
 
 // ---- smaller tiles: a ring of wide rows ------------------------------------------------
 // BM tokens x BN features, the waves WGM x WGN; a ring stage holds BK bytes of the BM token
-// rows and BN weight rows, so a copy fetches whole 128- to 512-byte row pieces; S - 1 stages
-// are in flight while one is multiplied.  16-byte chunks are XOR-permuted by the low row bits.
+// rows and BN weight rows, so a copy fetches row pieces of 128 or 256 bytes; S - 1 stages are
+// in flight while one is multiplied.  Bound by the weights' stream: 24 x 16384 x 4096 17.2 us
+// from memory (3.9 TB/s; 12.9 from the last-level cache), 64 x 36864 x 9216 70 us (4.9 TB/s).
+//  16-byte chunks are XOR-permuted by the low row bits.
 template <int BM, int BN, int WGM, int WGN, int BK, int S>
 __global__ __launch_bounds__(64 * WGM * WGN) void q8_ring_kernel(GemmQ8Params p, Split sp) {
     constexpr int NW = WGM * WGN;
@@ -523,7 +538,8 @@ __global__ __launch_bounds__(64 * KW) void q8_few_kernel(GemmQ8Params p) {
 }
 
 // ---- the sums of split tiles -------------------------------------------------------------
-// A thread adds the ranges' sums of four features of one token.
+// A thread adds the ranges' sums of four features of one token.  Bound by memory (40 tiles of
+// 192 x 256 in six ranges 12 us, 4.6 TB/s); splits are worth it where tiles leave CUs idle.
 template <int BM, int BN>
 __global__ __launch_bounds__(256) void q8_join_kernel(GemmQ8Params p, Split sp) {
     constexpr int GROUPS = BM * BN / 4 / 256;  // blocks per tile
@@ -535,50 +551,55 @@ __global__ __launch_bounds__(256) void q8_join_kernel(GemmQ8Params p, Split sp) 
     if (m >= p.M || n >= p.N) return;
     const int64_t stride = (int64_t)sp.tail * (BM * BN);
     const int32_t* src = p.ws + (int64_t)i * (BM * BN) + at;
-    i32x4 v = *(const i32x4*)src;
-    int s = 1;
-    for (; s + 3 < sp.splits; s += 4) {
-        i32x4 o[4];
+    const Features f = load_features(p, n);
+    const float sx = p.sx[m];
+    i32x4 v = {0, 0, 0, 0};
+    for (int s = 0; s < sp.splits; s += 8) {  // eight ranges' loads in flight together
+        i32x4 o[8];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) o[q] = *(const i32x4*)(src + (s + q) * stride);
-        v += (o[0] + o[1]) + (o[2] + o[3]);
+        for (int q = 0; q < 8; ++q) {
+            o[q] = i32x4{0, 0, 0, 0};
+            if (s + q < sp.splits) o[q] = __builtin_nontemporal_load((const i32x4*)(src + (s + q) * stride));
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v += o[q];
     }
-    for (; s < sp.splits; ++s) v += *(const i32x4*)(src + s * stride);
-    epilogue8(p, m, n, p.sx[m], load_features(p, n), v);
+    epilogue8(p, m, n, sx, f, v);
 }
 
 // ---- launches ----------------------------------------------------------------------------
 
 enum Kind { FEW, RING, WIDE };
 
-// A kernel and what its launches cost, in us: `start` and `both` as below; a K step (bk
-// bytes of it) of all blocks at once; the weights' bytes at tbs TB/s; `skew`: the share by
-// which a step grows where rows do not start on 128 bytes; a further round of blocks; a
-// join and its bytes; `channels`: the share by which weights slow down where the ranges
-// are a multiple of 4 KB apart and read the same memory channels.
+// A kernel and what its launches cost, in us: `start`; a K step (bk bytes of it) of all
+// blocks that run at once, and the share by which it grows with each token; the weights'
+// bytes at tbs TB/s; the share of the shorter of steps and weights that shows; `skew`: the
+// share by which a step grows where rows do not start on 128 bytes; a further round of
+// blocks; a join and its bytes; `channels`: the share by which weights slow down where
+// ranges of K start a multiple of 4 KB apart and read the same memory channels.
 struct Shape {
     Kind kind;
-    int bm, bn, bk, threads_or_waves, slots;  // slots: blocks that run at once on 256 CUs
-    float start, step, tbs, both, skew, round, join, join_tbs, channels;
+    int bm, bn, bk, threads, slots;  // slots: blocks that run at once on 256 CUs
+    float start, step, token, tbs, both, skew, round, join, join_tbs, channels;
 };
 
 // Fitted to 13 000 launches of 420 products (M 1 .. 4096, N 64 .. 50272, K 16 .. 36864, cold
-// weights, in recorded graphs; mean error 4-9% a kernel).  The chosen kernel and split was 2.0%
-// above the fastest of 15 kernels in up to 16 splits in the mean, 7% at the 90th percentile.
-// Kernels that gained less than 0.2% beside these are not kept (16 waves and 32 features for
+// weights, in recorded graphs; mean error 4-9% a kernel).  The chosen kernel and split was 1.7%
+// above the fastest of 15 kernels in up to 16 splits in the mean, 6% at the 90th percentile.
+// Kernels that gained less than 0.2% beside these are not kept (16 waves or 32 features for
 // few tokens, 512-byte rows).
 constexpr Shape SHAPES[] = {
-    {FEW, 16, 16, 256, 4, 2048, 2.68f, 0.192f, 5.67f, 1.0f, 0.42f, 0.15f, 0, 0, 0},
-    {FEW, 16, 16, 256, 8, 1024, 2.48f, 0.150f, 3.68f, 0.35f, 0, 3.0f, 0, 0, 0},
-    {RING, 32, 32, 256, 128, 512, 3.18f, 0.246f, 6.75f, 0.63f, 0.27f, 2.0f, 2.5f, 5.9f, 0.14f},
-    {RING, 32, 64, 256, 256, 256, 3.27f, 0.301f, 8.25f, 0.69f, 0.51f, 2.3f, 2.8f, 34.f, 0.15f},
-    {RING, 64, 64, 256, 256, 256, 3.80f, 0.480f, 7.15f, 0.31f, 0.23f, 3.0f, 2.6f, 26.f, 0.18f},
-    {RING, 64, 128, 128, 512, 256, 3.87f, 0.339f, 8.99f, 0.65f, 0.48f, 2.6f, 2.0f, 10.4f, 0.29f},
-    {RING, 128, 64, 256, 256, 256, 5.69f, 0.721f, 5.28f, 0.11f, 0.11f, 4.0f, 1.9f, 31.f, 0.09f},
-    {RING, 128, 128, 128, 512, 256, 5.49f, 0.474f, 7.47f, 0.35f, 0.38f, 4.3f, 2.2f, 11.4f, 0.27f},
-    {WIDE, 128, 256, 128, 512, 256, 8.74f, 0.717f, 8.78f, 0.64f, 0.60f, 5.6f, 1.2f, 10.8f, 0.29f},
-    {WIDE, 192, 256, 128, 512, 256, 11.1f, 0.901f, 7.85f, 0.36f, 0.37f, 7.9f, 0.2f, 10.6f, 0.43f},
-    {WIDE, 256, 256, 128, 512, 256, 12.8f, 1.090f, 6.19f, 0.09f, 0.40f, 10.1f, 0.0f, 11.0f, 0.67f},
+    {FEW, 16, 16, 256, 256, 2048, 2.68f, 0.192f, 0.103f, 5.67f, 1.00f, 0.42f, 0.15f, 0, 0, 0},
+    {FEW, 16, 16, 256, 512, 256, 2.53f, 0.169f, 0.031f, 5.24f, 0.30f, 0, 0, 0, 0, 0},
+    {RING, 32, 32, 256, 128, 512, 3.18f, 0.246f, 0, 6.75f, 0.63f, 0.27f, 2.0f, 2.5f, 5.9f, 0.14f},
+    {RING, 32, 64, 256, 256, 256, 3.27f, 0.301f, 0, 8.25f, 0.69f, 0.51f, 2.3f, 2.8f, 34.f, 0.15f},
+    {RING, 64, 64, 256, 256, 256, 3.80f, 0.480f, 0, 7.15f, 0.31f, 0.23f, 3.0f, 2.6f, 26.f, 0.18f},
+    {RING, 64, 128, 128, 512, 256, 3.87f, 0.339f, 0, 8.99f, 0.65f, 0.48f, 2.6f, 2.0f, 10.4f, 0.29f},
+    {RING, 128, 64, 256, 256, 256, 5.69f, 0.721f, 0, 5.28f, 0.11f, 0.11f, 4.0f, 1.9f, 31.f, 0.09f},
+    {RING, 128, 128, 128, 512, 256, 5.49f, 0.474f, 0, 7.47f, 0.35f, 0.38f, 4.3f, 2.2f, 11.4f, 0.27f},
+    {WIDE, 128, 256, 128, 512, 256, 8.74f, 0.717f, 0, 8.78f, 0.64f, 0.60f, 5.6f, 1.2f, 10.8f, 0.29f},
+    {WIDE, 192, 256, 128, 512, 256, 11.1f, 0.901f, 0, 7.85f, 0.36f, 0.37f, 7.9f, 0.2f, 10.6f, 0.43f},
+    {WIDE, 256, 256, 128, 512, 256, 12.8f, 1.090f, 0, 6.19f, 0.09f, 0.40f, 10.1f, 0.0f, 11.0f, 0.67f},
 };
 constexpr int N_SHAPES = sizeof(SHAPES) / sizeof(SHAPES[0]);
 
@@ -591,6 +612,11 @@ int tiles_of(const GemmQ8Params& p, const Shape& c) { return ((p.M + c.bm - 1) /
 
 size_t bytes_of(const Plan& c) {
     return c.splits > 1 ? (size_t)c.tail * c.splits * SHAPES[c.shape].bm * SHAPES[c.shape].bn * 4 : 0;
+}
+
+// Whether some row starts inside 128 bytes (asked without operands: packed rows).
+bool skewed(const GemmQ8Params& p) {
+    return ((p.W ? (uintptr_t)p.W | (uintptr_t)p.X | (uintptr_t)p.ldw | (uintptr_t)p.ldx : (uintptr_t)p.K) & 127) != 0;
 }
 
 // Predicted time of a launch: whole rounds of tiles, then what is left of them, then the
@@ -606,8 +632,8 @@ float time_of(const GemmQ8Params& p, const Plan& plan, int tiles, int whole) {
     }
     const int rounds = (tiles - tail + c.slots - 1) / c.slots, cut = (tail * splits + c.slots - 1) / c.slots;
     float work = (float)(rounds * whole + cut * kt) * c.step, weights = (float)p.N * (float)p.K * 1e-6f / c.tbs;
-    if (p.K % 128) work *= 1.f + c.skew;
-    if (c.kind == FEW) work *= 1.f + (c.threads_or_waves == 4 ? 0.103f : 0.045f) * (float)p.M;
+    if (skewed(p)) work *= 1.f + c.skew;
+    work *= 1.f + c.token * (float)p.M;
     if (tail && kt * c.bk % 4096 == 0) weights *= 1.f + c.channels;
     float t = c.start + fmaxf(work, weights) + c.both * fminf(work, weights) + (float)(rounds + cut - 1) * c.round;
     if (p.K % c.bk) t += 0.6f;
@@ -630,7 +656,7 @@ Plan plan_of(const GemmQ8Params& p, size_t room) {
         const Shape& c = SHAPES[i];
         if (c.kind == FEW) {
             // measured side by side: 4 waves from 12288 features on, where blocks are many
-            if (p.M <= 16 && (c.threads_or_waves == 4) == (p.N >= 12288)) consider({i, 1, 0}, tiles_of(p, c), p.K / c.bk);
+            if (p.M <= 16 && (c.threads == 256) == (p.N >= 12288)) consider({i, 1, 0}, tiles_of(p, c), p.K / c.bk);
             continue;
         }
         if (c.kind == WIDE ? p.M <= 64 || p.K < 128 : c.bm == 32 ? p.M > 64 : c.bm == 64 ? p.M > 512 : p.M <= 32) continue;
@@ -669,7 +695,7 @@ void launch_tiles(F kernel, const GemmQ8Params& p, const Plan& c, hipStream_t s)
             sp.full = tiles - c.tail;
         }
     }
-    PB_LAUNCH(kernel, sp.full + sp.tail * sp.splits, shape.threads_or_waves, 0, s, p, sp);
+    PB_LAUNCH(kernel, sp.full + sp.tail * sp.splits, shape.threads, 0, s, p, sp);
     if (sp.tail) PB_LAUNCH((q8_join_kernel<BM, BN>), sp.tail * (BM * BN / 4 / 256), 256, 0, s, p, sp);
 }
 

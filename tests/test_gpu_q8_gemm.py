@@ -85,9 +85,9 @@ def test_sizes(M, N, K):
 # Small products that the rule of sizes gives to each kernel: whole tiles, all tiles split, the
 # last round's split; K in whole steps and with a rest.
 KERNELS = [
-    (1, 12373, 256), (13, 15858, 64), (1, 32, 256), (1, 32, 64),  # up to 16 tokens
+    (1, 12373, 256), (13, 15858, 64), (1, 32, 256), (1, 32, 64), (1, 12100, 768), (1, 12199, 640), (16, 4096, 5104),  # up to 16 tokens
     (1, 44, 9984), (1, 32, 7552), (1, 16552, 7392), (17, 32, 256), (19, 35, 80),  # 32 x 32
-    (1, 677, 8192), (1, 637, 8320), (1, 18401, 7680), (1, 16437, 8064), (1, 12100, 768), (1, 12199, 640),  # 32 x 64
+    (1, 677, 8192), (1, 637, 8320), (1, 18401, 7680), (1, 16437, 8064), (1, 13857, 768), (1, 12713, 896),  # 32 x 64
     (67, 36, 11520), (76, 47, 9520), (48, 17268, 8704), (1, 19002, 7856), (78, 33, 256), (67, 36, 64),  # 64 x 64
     (11, 49, 5760), (68, 32, 2240), (68, 32, 128), (20, 16566, 64),  # 64 x 128
     (597, 32, 2048), (523, 32, 2608), (76, 18124, 3760), (589, 36, 256), (520, 35, 160),  # 128 x 64
