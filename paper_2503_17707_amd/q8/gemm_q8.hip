@@ -105,11 +105,12 @@ __device__ __forceinline__ void epilogue8(const GemmQ8Params& p, int m, int n, f
 
 // ---- which block does what ----------------------------------------------------------
 
-// Tiles 0 .. full-1 run over the whole of K; the others' K tiles (of 128) are cut into
-// `splits` ranges of kt, the last one taking the rest and what lies past the last whole
-// K tile.  Range s of tile full + i leaves its sums at ws + (s tail + i) BM BN.
+// Tiles 0 .. full-1 run over the whole of K; the others' K tiles are cut into `splits` ranges
+// of kt, the last one taking the rest and what lies past the last whole K tile.  Range s of
+// tile full + i leaves its sums at ws + (s tail + i) BM BN.  Columns of tiles start at
+// `phases` places of their range, and go round.
 struct Split {
-    int full, tail, splits, kt;
+    int full, tail, splits, kt, phases;
 };
 
 // The hardware deals consecutive blocks round-robin to the 8 XCDs: piece i of n such that
@@ -121,6 +122,7 @@ __device__ __forceinline__ int of_xcd(int i, int n) {
 
 struct Job {
     int m0, n0, t0, nk;  // corner; first K tile and how many
+    int phase;           // the one of them that a ring begins with
     bool last, partial;  // takes what lies past the last whole K tile; leaves sums
     int32_t* sums;       // [BM][BN]
 };
@@ -163,6 +165,7 @@ __device__ __forceinline__ Job tile_job(const GemmQ8Params& p, const Split& sp) 
         j.sums = p.ws + ((int64_t)s * sp.tail + i) * (BM * BN);
     }
     tile_corner<BM, BN>(p, tile, j.m0, j.n0);
+    j.phase = (int)((uint32_t)(j.n0 / BN) % (uint32_t)sp.phases) * j.nk / sp.phases;
     return j;
 }
 
@@ -428,8 +431,9 @@ __global__ __launch_bounds__(64 * WGM * WGN) void q8_ring_kernel(GemmQ8Params p,
     }
     const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
     auto issue = [&](int t, int stage) {
-        const int8_t* xk = Xb + (int64_t)t * BK;
-        const int8_t* wk = Wb + (int64_t)t * BK;
+        t += jb.phase;
+        const int64_t at = (int64_t)(t >= nk ? t - nk : t) * BK;
+        const int8_t *xk = Xb + at, *wk = Wb + at;
 #pragma unroll
         for (int j = 0; j < NL; ++j)
             dma16s((wave + NW * j) * RPI < BM ? xk : wk, off[j], lds0 + stage * STAGE + (wave + NW * j) * 1024);
@@ -583,23 +587,23 @@ struct Shape {
     float start, step, token, tbs, both, skew, round, join, join_tbs, channels;
 };
 
-// Fitted to 13 000 launches of 420 products (M 1 .. 4096, N 64 .. 50272, K 16 .. 36864, cold
-// weights, in recorded graphs; mean error 4-9% a kernel).  The chosen kernel and split was 1.7%
-// above the fastest of 15 kernels in up to 16 splits in the mean, 6% at the 90th percentile.
-// Kernels that gained less than 0.2% beside these are not kept (16 waves or 32 features for
-// few tokens, 512-byte rows).
+// Fitted to 16 000 launches of 580 products (M 1 .. 4096, N 64 .. 50272, K 16 .. 36864, cold
+// weights, in recorded graphs; mean error 4-10% a kernel).  The chosen kernel and split was 1.6%
+// above the fastest in up to 16 splits in the mean, 6% at the 90th percentile.  Kernels that
+// gained less than 0.2% beside these are not kept (16 waves or 32 features for few tokens,
+// 512-byte rows).
 constexpr Shape SHAPES[] = {
-    {FEW, 16, 16, 256, 256, 2048, 2.68f, 0.192f, 0.103f, 5.67f, 1.00f, 0.42f, 0.15f, 0, 0, 0},
-    {FEW, 16, 16, 256, 512, 256, 2.53f, 0.169f, 0.031f, 5.24f, 0.30f, 0, 0, 0, 0, 0},
-    {RING, 32, 32, 256, 128, 512, 3.18f, 0.246f, 0, 6.75f, 0.63f, 0.27f, 2.0f, 2.5f, 5.9f, 0.14f},
-    {RING, 32, 64, 256, 256, 256, 3.27f, 0.301f, 0, 8.25f, 0.69f, 0.51f, 2.3f, 2.8f, 34.f, 0.15f},
-    {RING, 64, 64, 256, 256, 256, 3.80f, 0.480f, 0, 7.15f, 0.31f, 0.23f, 3.0f, 2.6f, 26.f, 0.18f},
-    {RING, 64, 128, 128, 512, 256, 3.87f, 0.339f, 0, 8.99f, 0.65f, 0.48f, 2.6f, 2.0f, 10.4f, 0.29f},
-    {RING, 128, 64, 256, 256, 256, 5.69f, 0.721f, 0, 5.28f, 0.11f, 0.11f, 4.0f, 1.9f, 31.f, 0.09f},
-    {RING, 128, 128, 128, 512, 256, 5.49f, 0.474f, 0, 7.47f, 0.35f, 0.38f, 4.3f, 2.2f, 11.4f, 0.27f},
-    {WIDE, 128, 256, 128, 512, 256, 8.74f, 0.717f, 0, 8.78f, 0.64f, 0.60f, 5.6f, 1.2f, 10.8f, 0.29f},
-    {WIDE, 192, 256, 128, 512, 256, 11.1f, 0.901f, 0, 7.85f, 0.36f, 0.37f, 7.9f, 0.2f, 10.6f, 0.43f},
-    {WIDE, 256, 256, 128, 512, 256, 12.8f, 1.090f, 0, 6.19f, 0.09f, 0.40f, 10.1f, 0.0f, 11.0f, 0.67f},
+    {FEW, 16, 16, 256, 256, 2048, 2.58f, 0.122f, 0.186f, 5.08f, 0.92f, 0.66f, 0.1f, 0, 0, 0},
+    {FEW, 16, 16, 256, 512, 256, 2.47f, 0.178f, 0.028f, 4.96f, 0.22f, 0.01f, 0, 0, 0, 0},
+    {RING, 32, 32, 256, 128, 512, 3.26f, 0.279f, 0, 7.78f, 0.78f, 0.15f, 2.0f, 2.3f, 5.1f, 0.01f},
+    {RING, 32, 64, 256, 256, 256, 3.47f, 0.301f, 0, 8.74f, 0.79f, 0.47f, 2.2f, 2.4f, 11.6f, 0.02f},
+    {RING, 64, 64, 256, 256, 256, 4.09f, 0.477f, 0, 7.50f, 0.34f, 0.22f, 3.0f, 2.1f, 14.6f, 0.04f},
+    {RING, 64, 128, 128, 512, 256, 4.10f, 0.337f, 0, 9.29f, 0.69f, 0.50f, 2.7f, 1.5f, 10.2f, 0.31f},
+    {RING, 128, 64, 256, 256, 256, 5.82f, 0.716f, 0, 5.34f, 0.23f, 0.12f, 4.2f, 1.3f, 29.f, 0.00f},
+    {RING, 128, 128, 128, 512, 256, 5.64f, 0.495f, 0, 6.90f, 0.37f, 0.34f, 4.4f, 1.6f, 10.6f, 0.23f},
+    {WIDE, 128, 256, 128, 512, 256, 8.84f, 0.714f, 0, 7.84f, 0.62f, 0.62f, 5.5f, 0.2f, 8.9f, 0.17f},
+    {WIDE, 192, 256, 128, 512, 256, 10.2f, 0.905f, 0, 6.87f, 0.35f, 0.37f, 6.3f, 0.0f, 8.0f, 0.09f},
+    {WIDE, 256, 256, 128, 512, 256, 11.9f, 1.080f, 0, 6.05f, 0.12f, 0.47f, 7.9f, 0.0f, 8.5f, 0.34f},
 };
 constexpr int N_SHAPES = sizeof(SHAPES) / sizeof(SHAPES[0]);
 
@@ -613,6 +617,13 @@ int tiles_of(const GemmQ8Params& p, const Shape& c) { return ((p.M + c.bm - 1) /
 size_t bytes_of(const Plan& c) {
     return c.splits > 1 ? (size_t)c.tail * c.splits * SHAPES[c.shape].bm * SHAPES[c.shape].bn * 4 : 0;
 }
+
+// Weight rows a multiple of 4 KB apart have the same K on the same memory channels, so blocks
+// in step ask few of them at a time: where copies fetch 256 bytes of a row, columns of tiles
+// start at 16 places of K (cold weights: 7 x 36864 x 8192 65 -> 58 us, 24 x 16384 x 4096 18.1 ->
+// 16.2, 48 x 16384 x 8192 34.5 -> 29.3).  Copies of 128 bytes lose by it (69 -> 90 us in tiles of
+// 64 x 128), as do more tokens, whose rows would come from beyond the L2 several times.
+int phases_of(const GemmQ8Params& p, const Shape& c) { return c.kind == RING && c.bk == 256 && p.M <= 128 && p.ldw % 4096 == 0 ? 16 : 1; }
 
 // Whether some row starts inside 128 bytes (asked without operands: packed rows).
 bool skewed(const GemmQ8Params& p) {
@@ -686,7 +697,7 @@ template <int BM, int BN, typename F>
 void launch_tiles(F kernel, const GemmQ8Params& p, const Plan& c, hipStream_t s) {
     const Shape& shape = SHAPES[c.shape];
     const int tiles = tiles_of(p, shape), whole = p.K / shape.bk;
-    Split sp{tiles, 0, 1, whole};
+    Split sp{tiles, 0, 1, whole, phases_of(p, shape)};
     if (c.splits > 1) {
         sp.kt = (whole + c.splits - 1) / c.splits;
         sp.splits = (whole + sp.kt - 1) / sp.kt;
@@ -733,7 +744,7 @@ bool gemm_q8_fits(int M, int N) {
 
 size_t gemm_q8_workspace(int M, int N, int K) {
     GemmQ8Params p{};
-    p.M = M; p.N = N; p.K = K;
+    p.M = M; p.N = N; p.K = K; p.ldx = p.ldw = K;
     return bytes_of(plan_of(p, (size_t)1 << 60));
 }
 

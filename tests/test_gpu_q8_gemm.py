@@ -97,6 +97,10 @@ KERNELS = [
     (306, 26156, 144),  # 192 x 256
     (227, 8456, 9600), (229, 5384, 10704), (983, 16718, 1664), (683, 21867, 1616), (402, 22195, 128),
     (400, 26092, 144),  # 256 x 256
+    (1, 13185, 2048), (1, 12146, 2176), (386, 4785, 6656), (88, 16863, 5328), (143, 6423, 9312), (566, 31211, 5504),
+    (556, 22808, 2224), (403, 8506, 6784), (198, 22556, 3872),
+    # weight rows a multiple of 4 KB apart: columns of tiles that start at other places of K
+    (20, 1000, 4096), (40, 600, 8192), (64, 2100, 12288), (100, 5000, 4096), (128, 20000, 4096), (90, 520, 16384),
 ]
 
 
