@@ -5,8 +5,9 @@
  * launcher splits) on caller-provided device buffers, on the given stream,
  * asynchronously.  They exist to test every kernel against the CPU oracle's
  * component functions and to time kernels in isolation; the model API in
- * pipeboost.h is the product path.  The last section is for programs that run
- * decode steps of their own over a cache of pages.  All pointers are device pointers, all
+ * pipeboost.h is the product path.  The last two sections are for programs
+ * that run steps of their own: decoding over a cache of pages, and linear layers in
+ * 8 bits.  All pointers are device pointers, all
  * matrices row-major with the reduction dimension contiguous; "dt" is
  * bfloat16 (dtype 0) or IEEE binary16 (dtype 1).  Every call returns a
  * pb_status (PB_EINVAL for unsupported shapes, PB_EHIP for launch failures,
@@ -247,7 +248,8 @@ int pb_op_quant_q8(int32_t dtype, const void* x, int64_t ld_x, int32_t x_f32, in
  * K is a multiple of 16, at most 131056; any M and N up to 2^24 whose tiles of 64 x 64
  * stay below 2^23.  workspace (may be NULL): partial sums where K is split, up to
  * pb_op_gemm_q8_workspace bytes (0 for refused sizes); results do not depend on it.
- * It carries nothing from one call to the next. */
+ * It carries nothing from one call to the next; calls that may run at the same time
+ * (on two streams, in two graphs) need one each. */
 int pb_op_gemm_q8(int32_t dtype, int32_t epi, const int8_t* X, int64_t ldx, const float* sx, const int8_t* W,
                   int64_t ldw, const float* sw, const void* bias, void* C, float* R, int64_t ldo, int32_t M,
                   int32_t N, int32_t K, float qscale, int32_t qcols, void* workspace, size_t workspace_bytes,

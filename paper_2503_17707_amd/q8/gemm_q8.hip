@@ -396,9 +396,9 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void q
 // ---- smaller tiles: a ring of wide rows ------------------------------------------------
 // BM tokens x BN features, the waves WGM x WGN; a ring stage holds BK bytes of the BM token
 // rows and BN weight rows, so a copy fetches row pieces of 128 or 256 bytes; S - 1 stages are
-// in flight while one is multiplied.  Bound by the weights' stream: 24 x 16384 x 4096 17.2 us
-// from memory (3.9 TB/s; 12.9 from the last-level cache), 64 x 36864 x 9216 70 us (4.9 TB/s).
-//  16-byte chunks are XOR-permuted by the low row bits.
+// in flight while one is multiplied.  Bound by the weights' stream: 24 x 16384 x 4096 16.2 us
+// from memory (4.2 TB/s; 12.9 from the last-level cache), 64 x 36864 x 9216 70 us (4.9 TB/s).
+// 16-byte chunks are XOR-permuted by the low row bits.
 template <int BM, int BN, int WGM, int WGN, int BK, int S>
 __global__ __launch_bounds__(64 * WGM * WGN) void q8_ring_kernel(GemmQ8Params p, Split sp) {
     constexpr int NW = WGM * WGN;

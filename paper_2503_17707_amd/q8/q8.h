@@ -18,7 +18,7 @@ struct NormQ8Params {
     int8_t* q; int64_t ld_q;              // NULL: not wanted (scale then too)
     float* scale;
     int rows, d;
-    double inv_d;  // 1 / d
+    double width, inv_d;  // d, 1 / d
     float eps;
     bool layer;
 };

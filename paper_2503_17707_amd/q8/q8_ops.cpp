@@ -12,9 +12,9 @@ using pb::refuse;
 namespace {
 
 // Rows of `cols` elements of `size` bytes at stride ld: non-NULL, on whole elements,
-// not over one another.  (The stride of a single row is not used.)
+// not over one another, their extent inside 64 bits.  (The stride of a single row is not used.)
 bool rows_ok(const void* p, int64_t ld, int64_t rows, int64_t cols, int size) {
-    return p && aligned(p, (uintptr_t)size) && (rows <= 1 || (ld >= cols && ld < ((int64_t)1 << 40)));
+    return p && aligned(p, (uintptr_t)size) && (rows <= 1 || (ld >= cols && ld < ((int64_t)1 << 40) && ld <= ((int64_t)1 << 56) / rows));
 }
 
 size_t span(int64_t ld, int64_t rows, int64_t cols, int size) {
@@ -68,7 +68,7 @@ extern "C" int pb_op_norm_q8(int32_t dtype, int32_t layer, const void* x, int64_
     pb::NormQ8Params p{};
     p.x = x; p.ld_x = ld_x; p.delta = delta; p.ld_delta = ld_delta; p.sum = sum; p.ld_sum = ld_sum;
     p.g = g; p.b = b; p.out = out; p.ld_out = ld_out; p.q = q; p.ld_q = ld_q; p.scale = scale;
-    p.rows = rows; p.d = d; p.inv_d = 1.0 / d; p.eps = eps; p.layer = layer != 0;
+    p.rows = rows; p.d = d; p.width = d; p.inv_d = 1.0 / d; p.eps = eps; p.layer = layer != 0;
     return launched(op, pb::launch_norm_q8(dtype, x_f32 != 0, p, (hipStream_t)stream));
 }
 

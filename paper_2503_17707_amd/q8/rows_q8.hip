@@ -6,11 +6,15 @@
 // quotient, so the numbers are those of the formula but where y / scale lies within
 // about 2^-45 of the border of two integers, and neither the order of a sum nor the
 // split of a row over lanes shows in them.  (In fp32 one number in some 50 000 would
-// be off by one step.)  CDNA4 does fp64 at the rate of fp32 outside the matrix units:
-// some ten operations an element are a tenth of the time the memory takes.
+// be off by one step.)  CDNA4 does fp64 outside the matrix units at half the rate of
+// fp32; some two dozen such operations an element keep the vector units busy for about 0.7
+// of the time that memory takes, and long and 16-bit streams run between the two bounds.
 //
-// Both read a row once into registers (fp32) and write it once: bound by memory, for
-// few rows by the latency of one load, the reductions and one store.
+// Both read a row once into registers (fp32) and write it once: 4096 rows of 9216, fp32
+// stream and fp16 delta, 84-90 us (4.7-4.9 TB/s, a large copy 4.76); 4096 of 36864 in fp16
+// 84-91 us (5.0-5.4); 2002 of 2048 in bf16 12 us (3.0: the vector units).  Few rows are bound
+// by the latency of one load, the reductions and one store (one of 2048: 2.6 us).
+#include <algorithm>
 #include <cmath>
 #include <type_traits>
 
@@ -149,6 +153,16 @@ __device__ __forceinline__ double max_abs(double top, double y) {
     return top;
 }
 
+// A value that all lanes hold, in scalar registers: it leaves vector registers for more waves
+// or loads (10000 rows of 3000 in fp32 82 -> 77 us, 1831 of 16384 in fp16 66 -> 65).
+template <bool SCALAR>
+__device__ __forceinline__ double of_row(double v) {
+    if constexpr (!SCALAR) return v;
+    const uint64_t w = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)w), hi = __builtin_amdgcn_readfirstlane((uint32_t)(w >> 32));
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
 // Keeps the compiler from holding a conversion made before this point: kept as fp64, a
 // row's elements would take the registers of half the waves.
 template <typename T, int VEC>
@@ -193,11 +207,12 @@ __device__ __forceinline__ float row_scale(double top) {
     return s < 1.17549435e-38f ? 0.f : s;  // rows below it are zeros: a subnormal scale holds too few bits
 }
 
-// rint(y / scale): a product with the reciprocal and one correction, exact where the
-// quotient is a number of 53 bits, so that ties are ties.
+// rint(y / scale), at most 127: a product with the reciprocal and one correction, exact where
+// the quotient is a number of 53 bits, so that ties are ties.  Added to 1.5 2^52, which has no
+// bits below 1, it is rounded to the nearest integer, ties to even, in the low word.
 __device__ __forceinline__ int quotient(double y, double scale, double inv) {
     const double t = y * inv;
-    return (int)rint(fma(fma(-scale, t, y), inv, t));
+    return (int)(uint32_t)__builtin_bit_cast(uint64_t, fma(fma(-scale, t, y), inv, t) + 6755399441055744.0);
 }
 
 // (a scale that is zero or no number: zeros)
@@ -225,9 +240,13 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) __attribute__((amdgpu_waves_per
     const int threads = LANES ? LANES : blockDim.x;
     const int first = LANES ? (int)blockIdx.x * RPB + (int)threadIdx.x / LANES : blockIdx.x;
     const int step = (int)gridDim.x * RPB;
-    // Long rows, whose blocks have a CU to themselves, are walked over, the next one loaded
-    // while one is worked on; gains and biases stay (4096 x 9216: 114 -> 96 us).
+    // Long rows are walked over, the next one loaded while one is worked on; gains and biases
+    // stay (4096 x 9216 in fp32: 114 -> 96 us).
     constexpr bool AHEAD = loads_ahead(VEC, NV, LANES);
+    // (not with a thread's one piece of eight elements: past 80 scalar registers a SIMD holds
+    // seven waves, not eight, and a CU one block of 1024; 3662 rows of 8192 in fp16 61 -> 83 us)
+    constexpr bool SCALAR = LANES == 0 && (VEC == 4 || NV > 1);
+    const double width = SCALAR ? p.width : (double)p.d;
     Pack<S, VEC> x[NV];
     Pack<T, VEC> t[NV], g[NV], b[NV];
     auto place = [&](int i) { return Place<VEC>(i, i == NV - 1, threads, lane, p.d); };
@@ -276,7 +295,9 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) __attribute__((amdgpu_waves_per
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) sum += (double)(i < NV - 1 || e >= over ? s[i][e] : 0.f);
             }
-            mean = row_fold<LANES>(sum, lds1, Plus()) * p.inv_d;
+            sum = row_fold<LANES>(sum, lds1, Plus());
+            mean = sum * p.inv_d;  // and one step of division: rows of one value have it as their mean
+            mean = of_row<SCALAR>(fma(fma(-width, mean, sum), p.inv_d, mean));
         }
         double square = 0.0, top = 0.0, check = 0.0;  // check: NaN where some y is no finite number
 #pragma unroll
@@ -300,7 +321,7 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) __attribute__((amdgpu_waves_per
             if (check != 0.0) top = INFINITY;
             row_fold2<LANES>(square, top, lds2, Plus(), Larger());
         }
-        double rstd = rsqrt64(fma(square, p.inv_d, (double)p.eps));
+        const double rstd = of_row<SCALAR>(rsqrt64(fma(square, p.inv_d, (double)p.eps)));
         // every lane has read its row: the sum may take its place
         if (p.sum) {
 #pragma unroll
@@ -455,7 +476,7 @@ int row_blocks(int rows, int per_block) {
 template <typename T, typename S, int VEC, int NV, int LANES>
 void norm_nv(const NormQ8Params& p, int threads, hipStream_t s) {
     int blocks = row_blocks(p.rows, LANES ? 256 / LANES : 1);
-    if (loads_ahead(VEC, NV, LANES) && blocks > 256) blocks = 256;  // one a CU
+    if (loads_ahead(VEC, NV, LANES)) blocks = std::min(blocks, 256 * (1024 / threads));  // 16 waves a CU
     if (p.b) PB_LAUNCH((norm_q8_kernel<T, S, VEC, NV, LANES, true>), blocks, threads, 0, s, p);
     else PB_LAUNCH((norm_q8_kernel<T, S, VEC, NV, LANES, false>), blocks, threads, 0, s, p);
 }
@@ -465,56 +486,57 @@ void quant_nv(const QuantQ8Params& p, hipStream_t s) {
     PB_LAUNCH((quant_q8_kernel<S, VEC, NV, TPR>), row_blocks(p.rows, TPR < 256 ? 256 / TPR : 1), TPR < 256 ? 256 : TPR, 0, s, p);
 }
 
-// Rows of up to 128 pieces share waves; longer ones have a block of as many waves as leave a
-// thread 8 elements (12 or 16 where 1024 threads are too few): the loads of a row are in
-// flight together, and few enough registers hold two blocks of 1024 threads a CU or more.
-// (16384 and more rows in all lengths: 12 elements and more a thread spilled or ran one
-// block a CU, d 9216 in fp32 with 20: 400 us for 4096 rows.)
+// Rows of up to 128 pieces share waves.  Longer ones have a block each, of a piece (16 bits) or
+// two (fp32) a thread, as many waves as may be; from there on rows are walked over with the
+// next one's loads in flight, 12 fp32 or 16 16-bit elements a thread, which leaves 16 waves a CU
+// (30 M elements in fp32, two pieces a thread without loads ahead -> three with: rows of 4104
+// 90 -> 78 us, 6144 72 -> 69, 8192 95 -> 76, but 3600 71 -> 83; in fp16, one piece -> two: 8192
+// 58 -> 53, 6656 64 -> 60, 6144 59 -> 62).  16 fp32 elements leave no registers to load ahead.
 template <typename T, typename S>
 void norm_type(const NormQ8Params& p, hipStream_t s) {
-    constexpr int VEC = 16 / sizeof(S);
+    constexpr int VEC = 16 / sizeof(S), MOST = 1024;
     const int n = (p.d + VEC - 1) / VEC;  // pieces
-    auto waves = [&](int pieces) {
-        // (waves in fours, one to each SIMD, where that leaves few idle: 5120 in fp32 96 -> 85 us)
-        const int t = (n + pieces - 1) / pieces, fours = (t + 255) / 256 * 256;
-        return fours * 5 <= t * 6 ? fours : (t + 63) / 64 * 64;
-    };
+    auto waves = [&](int pieces) { return ((n + pieces - 1) / pieces + 63) / 64 * 64; };
     if (p.d < VEC) norm_nv<T, S, 1, 1, 16>(p, 256, s);
     else if (n <= 16) norm_nv<T, S, VEC, 1, 16>(p, 256, s);
     else if (n <= 32) norm_nv<T, S, VEC, 1, 32>(p, 256, s);
     else if (n <= 64) norm_nv<T, S, VEC, 1, 64>(p, 256, s);
-    else if (n <= 128 && VEC == 4) norm_nv<T, S, VEC, 2, 64>(p, 256, s);
-    else if (n <= 1024 && VEC == 8) norm_nv<T, S, VEC, 1, 0>(p, waves(1), s);
-    else if (n <= 2048) norm_nv<T, S, VEC, 2, 0>(p, waves(2), s);
-    else if constexpr (VEC == 4) {
-        if (n <= 3 * 1024) norm_nv<T, S, VEC, 3, 0>(p, waves(3), s);
+    else if constexpr (VEC == 8) {
+        if (n <= 768) norm_nv<T, S, VEC, 1, 0>(p, waves(1), s);
+        else norm_nv<T, S, VEC, 2, 0>(p, waves(2), s);
+    } else {
+        if (n <= 128) norm_nv<T, S, VEC, 2, 64>(p, 256, s);
+        else if (n <= MOST) norm_nv<T, S, VEC, 2, 0>(p, waves(2), s);
+        else if (n <= 3 * MOST) norm_nv<T, S, VEC, 3, 0>(p, waves(3), s);
         else norm_nv<T, S, VEC, 4, 0>(p, waves(4), s);
     }
 }
 
+// A row of n pieces on TPR threads with NV pieces each, where they hold it.
+template <typename S, int VEC, int NV, int TPR>
+bool quant_on(const QuantQ8Params& p, int n, hipStream_t s) {
+    if (n > NV * TPR) return false;
+    quant_nv<S, VEC, NV, TPR>(p, s);
+    return true;
+}
+
+// The smallest number of registers that holds a row; longer rows than 1024 threads hold in
+// eight pieces are read twice (NV 0).
 template <typename S>
 void quant_type(const QuantQ8Params& p, hipStream_t s) {
     constexpr int VEC = 16 / sizeof(S);
     const int n = (int)(((int64_t)p.cols + VEC - 1) / VEC);
-    if (p.cols < VEC) quant_nv<S, 1, 1, 16>(p, s);
-    else if (n <= 16) quant_nv<S, VEC, 1, 16>(p, s);
-    else if (n <= 32) quant_nv<S, VEC, 1, 32>(p, s);
-    else if (n <= 64) quant_nv<S, VEC, 1, 64>(p, s);
-    else if (n <= 128) quant_nv<S, VEC, 2, 64>(p, s);
-    else if (n <= 256) quant_nv<S, VEC, 1, 256>(p, s);
-    else if (n <= 512) quant_nv<S, VEC, 2, 256>(p, s);
-    else if (n <= 768) quant_nv<S, VEC, 3, 256>(p, s);
-    else if (n <= 1024) quant_nv<S, VEC, 4, 256>(p, s);
-    else if (n <= 1536) quant_nv<S, VEC, 3, 512>(p, s);
-    else if (n <= 2048) quant_nv<S, VEC, 4, 512>(p, s);
-    else if (n <= 2560) quant_nv<S, VEC, 5, 512>(p, s);
-    else if (n <= 3 * 1024) quant_nv<S, VEC, 3, 1024>(p, s);
-    else if (n <= 4096) quant_nv<S, VEC, 4, 1024>(p, s);
-    else if (n <= 5120) quant_nv<S, VEC, 5, 1024>(p, s);
-    else if (n <= 6144) quant_nv<S, VEC, 6, 1024>(p, s);
-    else if (n <= 7168) quant_nv<S, VEC, 7, 1024>(p, s);
-    else if (n <= 8192) quant_nv<S, VEC, 8, 1024>(p, s);
-    else quant_nv<S, VEC, 0, 1024>(p, s);
+    if (p.cols < VEC) {
+        quant_nv<S, 1, 1, 16>(p, s);
+        return;
+    }
+    const bool held = quant_on<S, VEC, 1, 16>(p, n, s) || quant_on<S, VEC, 1, 32>(p, n, s) || quant_on<S, VEC, 1, 64>(p, n, s) ||
+                      quant_on<S, VEC, 2, 64>(p, n, s) || quant_on<S, VEC, 1, 256>(p, n, s) || quant_on<S, VEC, 2, 256>(p, n, s) ||
+                      quant_on<S, VEC, 3, 256>(p, n, s) || quant_on<S, VEC, 4, 256>(p, n, s) || quant_on<S, VEC, 3, 512>(p, n, s) ||
+                      quant_on<S, VEC, 4, 512>(p, n, s) || quant_on<S, VEC, 5, 512>(p, n, s) || quant_on<S, VEC, 3, 1024>(p, n, s) ||
+                      quant_on<S, VEC, 4, 1024>(p, n, s) || quant_on<S, VEC, 5, 1024>(p, n, s) || quant_on<S, VEC, 6, 1024>(p, n, s) ||
+                      quant_on<S, VEC, 7, 1024>(p, n, s) || quant_on<S, VEC, 8, 1024>(p, n, s);
+    if (!held) quant_nv<S, VEC, 0, 1024>(p, s);
 }
 
 }  // namespace

@@ -8,16 +8,14 @@ from gpu_common import log
 pytestmark = pytest.mark.gpu
 
 
-def _out_tolerance(y, b, err, dt):
-    """With e = 2^-24, in fp32: v = (s - mean_hi) - mean_lo has error 2 e |v|, u = v rstd (rstd rounded, one product)
-    4 e |u|, y = u g + b: 4 e |u g| + e |y| <= 5 e |y| + 4 e |b|, and 2^-48 of the mean, below err; then half a step of
-    the type, and half its smallest one."""
+def _out_tolerance(y, err, dt):
+    """y is formed in 64 bits (both sides within err), rounded to fp32 (2^-24 of it, or half of fp32's smallest step)
+    and from there to the type (half a step, or half its smallest one): at most err (1 + half) + (half + 2^-24 (1 + half))
+    |y| + both halves of smallest steps."""
     from q8_common import HALF
 
     half, least = HALF[dt]
-    e = 2.0 ** -24
-    fp32 = 5.01 * e * y.abs() + (0 if b is None else 4.01 * e * b.double().abs()[None])
-    return err + fp32 + half * (y.abs() + fp32) + least
+    return 2 * err + (half + 2.0 ** -24 * (1 + half)) * y.abs() + least + 2.0 ** -149
 
 
 def _norm(kind, rows, d, f32, layer, delta, out, bias, seed=0, eps=1e-5, pad=(0, 0, 0, 0, 0), x=None, in_place=False):
@@ -54,7 +52,7 @@ def _norm(kind, rows, d, f32, layer, delta, out, bias, seed=0, eps=1e-5, pad=(0,
     check_rows8(qv, scale, y, err, (kind, rows, d))
     assert untouched(qb, d, pad[4] // 2)
     if out:  # formed in fp32, then rounded to the type
-        assert bool(((ov.cpu().double() - y).abs() <= _out_tolerance(y, b, err, dt)).all())
+        assert bool(((ov.cpu().double() - y).abs() <= _out_tolerance(y, err, dt)).all())
         assert untouched(ob, d, pad[3] // 2)
     return qv.clone(), scale
 
@@ -106,7 +104,25 @@ def test_norm_without_quantization_and_with_large_offsets():
     out = torch.zeros(4, 500, dtype=torch.float16, device="cuda")
     pb.op_norm_q8(1, x.cuda(), gain.cuda(), out=out, layer=True)
     y, err = norm64(x, gain, None, True, 1e-5)
-    assert bool(((out.cpu().double() - y).abs() <= _out_tolerance(y, None, err, torch.float16)).all())
+    assert bool(((out.cpu().double() - y).abs() <= _out_tolerance(y, err, torch.float16)).all())
+
+
+@pytest.mark.parametrize("d", [3, 70, 777, 2048, 5003, 9216])
+def test_layer_norm_of_rows_of_one_value(d):
+    """Their mean is the value: sums of d equal fp32 values are exact in 64 bits (24 + 14 bits), the division rounds to it."""
+    import torch
+
+    from paper_2503_17707_amd import binding as pb
+
+    values = torch.tensor([2.5, -0.1, 1e-3, 65000.0, 1 / 3, 1e30, -7e-20])
+    for st in (torch.float32, torch.bfloat16):
+        x = values[:, None].expand(-1, d).to(st).cuda().contiguous()
+        gain = torch.ones(d, dtype=torch.bfloat16, device="cuda")
+        q, scale = torch.full((7, d), 5, dtype=torch.int8, device="cuda"), torch.ones(7, device="cuda")
+        out = torch.ones(7, d, dtype=torch.bfloat16, device="cuda")
+        for b in (None, torch.zeros_like(gain)):
+            pb.op_norm_q8(0, x, gain, q, scale, b=b, out=out, layer=True)
+            assert bool((scale == 0).all()) and bool((q == 0).all()) and bool((out == 0).all())
 
 
 @pytest.mark.parametrize("f32", [False, True])

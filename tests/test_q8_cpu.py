@@ -29,7 +29,8 @@ def _refused(pb, rc, name, what):
 
 
 @pytest.mark.parametrize("bad", [dict(dtype=2), dict(dtype=-1), dict(x=None), dict(x=A[0] + 1), dict(x=A[0] + 2, f32=1), dict(ld_x=63),
-                                 dict(ld_x=1 << 41), dict(delta=A[1] + 1), dict(ld_delta=10), dict(delta=None), dict(sum=A[2] + 1),
+                                 dict(ld_x=1 << 41), dict(ld_x=1 << 39, rows=1 << 29), dict(ld_q=1 << 38, rows=1 << 30),
+                                 dict(delta=A[1] + 1), dict(ld_delta=10), dict(delta=None), dict(sum=A[2] + 1),
                                  dict(ld_sum=-64), dict(g=None), dict(g=A[3] + 1), dict(b=A[4] + 1), dict(eps=-1e-5),
                                  dict(eps=float("nan")), dict(eps=float("inf")), dict(out=A[5] + 1), dict(ld_out=63),
                                  dict(out=None, q=None, scale=None), dict(q=None), dict(scale=None), dict(scale=A[7] + 2),
@@ -53,6 +54,7 @@ def test_norm_outputs_that_overlap(bad):
 @pytest.mark.parametrize("bad", [dict(dtype=2), dict(x=None), dict(x=A[0] + 1), dict(x=A[0] + 2, f32=1), dict(ld_x=63), dict(q=None),
                                  dict(ld_q=1), dict(scale=None), dict(scale=A[2] + 1), dict(rows=-2), dict(cols=0),
                                  dict(cols=(1 << 24) + 1, ld_x=1 << 25, ld_q=1 << 25), dict(rows=(1 << 30) + 1), dict(q=A[0] + 100), dict(scale=A[0]),
+                                 dict(ld_x=1 << 36, rows=1 << 30),
                                  dict(scale=A[1] + 4)], ids=str)
 def test_quant_refusals(bad):
     from paper_2503_17707_amd import binding as pb
@@ -66,7 +68,7 @@ def test_quant_refusals(bad):
                                  dict(bias=A[4] + 1), dict(C=None), dict(C=A[5] + 1), dict(epi=2, R=None),
                                  dict(epi=3, R=A[6] + 2), dict(ldo=31), dict(epi=2, ldo=8), dict(M=-1), dict(N=0), dict(K=0),
                                  dict(K=63), dict(K=72, ldx=80, ldw=80), dict(K=131072, ldx=131072, ldw=131072),
-                                 dict(M=1 << 30, N=1 << 20, ldo=1 << 20), dict(ws=A[7] + 4)], ids=str)
+                                 dict(M=1 << 30, N=1 << 20, ldo=1 << 20), dict(M=1 << 24, ldo=1 << 39), dict(ws=A[7] + 4)], ids=str)
 def test_gemm_refusals(bad):
     from paper_2503_17707_amd import binding as pb
 
