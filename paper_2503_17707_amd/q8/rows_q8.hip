@@ -7,13 +7,13 @@
 // about 2^-45 of the border of two integers, and neither the order of a sum nor the
 // split of a row over lanes shows in them.  (In fp32 one number in some 50 000 would
 // be off by one step.)  CDNA4 does fp64 outside the matrix units at half the rate of
-// fp32; some two dozen such operations an element keep the vector units busy for about 0.7
-// of the time that memory takes, and long and 16-bit streams run between the two bounds.
+// fp32; the fifteen or so such operations an element keep the vector units busy for up to
+// 0.7 of the time that memory takes.
 //
 // Both read a row once into registers (fp32) and write it once: 4096 rows of 9216, fp32
-// stream and fp16 delta, 84-90 us (4.7-4.9 TB/s, a large copy 4.76); 4096 of 36864 in fp16
-// 84-91 us (5.0-5.4); 2002 of 2048 in bf16 12 us (3.0: the vector units).  Few rows are bound
-// by the latency of one load, the reductions and one store (one of 2048: 2.6 us).
+// stream and fp16 delta, 82-89 us (4.7-5.1 TB/s, a large copy 4.76); 4096 of 36864 in fp16
+// 83-88 us (5.1-5.5); 1001 of 4096 in bf16, one round of blocks, 11-13 us (2.9-3.4).  Few
+// rows are bound by the latency of one load, the reductions and one store (one of 2048: 2.6 us).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -153,6 +153,19 @@ __device__ __forceinline__ double max_abs(double top, double y) {
     return top;
 }
 
+// Whether one of VEC gains or biases is a NaN or an infinity: all bits of its exponent set.
+template <typename T, int VEC>
+__device__ __forceinline__ bool not_finite(const Pack<T, VEC>& x) {
+    constexpr uint16_t BITS = std::is_same_v<T, __bf16> ? 0x7f80 : 0x7c00;
+    if constexpr (VEC == 1) return (__builtin_bit_cast(uint16_t, x.v[0]) & BITS) == BITS;
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 w[VEC / 2 + VEC % 2], top = {0, 0};
+    __builtin_memcpy(w, &x, sizeof(x));
+#pragma unroll
+    for (int k = 0; k < VEC / 2; ++k) top = __builtin_elementwise_max(top, w[k] & u16x2{0x7fff, 0x7fff});
+    return top[0] >= BITS || top[1] >= BITS;
+}
+
 // A value that all lanes hold, in scalar registers: it leaves vector registers for more waves
 // or loads (10000 rows of 3000 in fp32 82 -> 77 us, 1831 of 16384 in fp16 66 -> 65).
 template <bool SCALAR>
@@ -265,9 +278,33 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) __attribute__((amdgpu_waves_per
             if constexpr (BIAS) b[i] = load_pack<VEC>(element((const T*)p.b, place(i).at));
         }
     };
+    bool bad = false;  // a gain or bias that is no finite number: no y of its column is
+    auto check_gains = [&] {
+        bad = false;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            bad |= not_finite(g[i]);
+            if constexpr (BIAS) bad |= not_finite(b[i]);
+        }
+    };
+    // total and the terms of piece i's own elements
+    auto add_piece = [&](int i, double total, auto term) {
+        double all = total;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) all = term(e, all);
+        if (i < NV - 1) return all;
+        const int over = place(i).over;
+        if (over) {  // (lanes of few waves)
+            all = total;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) all = e >= over ? term(e, all) : all;
+        }
+        return all;
+    };
     if (AHEAD) {
         load_row(min(first, p.rows - 1));
         load_gains();
+        check_gains();
     }
     for (int row = first; row < p.rows; row += step) {
         if (!AHEAD) {
@@ -286,42 +323,54 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) __attribute__((amdgpu_waves_per
                 for (int e = 0; e < VEC; ++e) s[i][e] = (float)(S)(s[i][e] + (float)t[i].v[e]);
         }
         if (AHEAD && row + step < p.rows) load_row(row + step);
+        // s - mean, then y, are kept in fp64 where a thread has one piece; of more they are formed
+        // again for each use (kept, they would cost a long row half of its waves)
+        constexpr bool KEPT = NV == 1;
+        double kept[VEC];
+        if (KEPT) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) kept[e] = (double)s[0][e];
+        }
         double mean = 0.0;
         if (p.layer) {
             double sum = 0.0;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int over = place(i).over;
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) sum += (double)(i < NV - 1 || e >= over ? s[i][e] : 0.f);
-            }
+            for (int i = 0; i < NV; ++i)
+                sum = add_piece(i, sum, [&](int e, double a) { return a + (KEPT ? kept[e] : (double)s[i][e]); });
             sum = row_fold<LANES>(sum, lds1, Plus());
             mean = sum * p.inv_d;  // and one step of division: rows of one value have it as their mean
             mean = of_row<SCALAR>(fma(fma(-width, mean, sum), p.inv_d, mean));
-        }
-        double square = 0.0, top = 0.0, check = 0.0;  // check: NaN where some y is no finite number
+            if (KEPT) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int over = place(i).over;
-            again(s[i]);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const double v = (double)s[i][e] - mean;
-                square = fma(i < NV - 1 || e >= over ? v : 0.0, v, square);
-                if (!BIAS) {
-                    const double u = v * (double)(float)g[i].v[e];
-                    top = max_abs(top, u);
-                    check = fma(u, 0.0, check);
-                }
+                for (int e = 0; e < VEC; ++e) kept[e] -= mean;
             }
         }
+        auto centred = [&](int i, int e) { return KEPT ? kept[e] : (double)s[i][e] - mean; };
+        double square = 0.0, top = 0.0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (!KEPT) again(s[i]);
+            square = add_piece(i, square, [&](int e, double a) {
+                const double v = centred(i, e);
+                return fma(v, v, a);
+            });
+            if (!BIAS) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) top = max_abs(top, centred(i, e) * (double)(float)g[i].v[e]);
+            }
+        }
+        if (!AHEAD && !BIAS) check_gains();
         if (BIAS) {
             square = row_fold<LANES>(square, &lds2[0][0], Plus());
         } else {
-            if (check != 0.0) top = INFINITY;
+            if (bad) top = INFINITY;
             row_fold2<LANES>(square, top, lds2, Plus(), Larger());
         }
-        const double rstd = of_row<SCALAR>(rsqrt64(fma(square, p.inv_d, (double)p.eps)));
+        // (fp64 products of fp32 numbers do not overflow: where the variance is a positive number
+        // and gains and biases are finite, so is every y)
+        const double var = fma(square, p.inv_d, (double)p.eps);
+        const double rstd = of_row<SCALAR>(rsqrt64(var));
+        const bool none = !(var > 0.0 && var < INFINITY);
         // every lane has read its row: the sum may take its place
         if (p.sum) {
 #pragma unroll
@@ -330,17 +379,15 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) __attribute__((amdgpu_waves_per
                 if (at.over < VEC) store_pack<S, float, VEC>(element((S*)p.sum + (int64_t)row * p.ld_sum, at.at), s[i]);
             }
         }
-        // y is kept for the second use where a thread has one piece; of more it is formed again
-        // (kept, it would cost a long row half of its waves)
-        constexpr bool KEPT = NV == 1;
         auto normed = [&](int i, double (&y)[VEC]) {
-            again(s[i]);
+            if (!KEPT) again(s[i]);
             again(g[i]);
             if (BIAS) again(b[i]);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                y[e] = ((double)s[i][e] - mean) * rstd * (double)(float)g[i].v[e];
-                if (BIAS) y[e] += (double)(float)b[i].v[e];
+                const double v = centred(i, e) * rstd, gain = (double)(float)g[i].v[e];
+                if constexpr (BIAS) y[e] = fma(v, gain, (double)(float)b[i].v[e]);
+                else y[e] = v * gain;
             }
         };
         double y[VEC];
@@ -352,11 +399,8 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) __attribute__((amdgpu_waves_per
                 if (!KEPT) normed(i, y);
                 if (BIAS) {
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        top = max_abs(top, y[e]);
-                        check = fma(y[e], 0.0, check);
-                    }
-                    asm volatile("" : "+v"(check));  // (y is used up here)
+                    for (int e = 0; e < VEC; ++e) top = max_abs(top, y[e]);
+                    asm volatile("" : "+v"(top));  // (y is used up here)
                 }
                 if (p.out) {
                     float f[VEC];
@@ -371,11 +415,13 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) __attribute__((amdgpu_waves_per
             continue;
         }
         if (BIAS) {
-            if (check != 0.0) top = INFINITY;
+            if (!AHEAD) check_gains();
+            if (bad) top = INFINITY;
             top = row_fold<LANES>(top, lds3, Larger());
         } else {
             top *= rstd;
         }
+        if (none) top = INFINITY;
         const float scale = row_scale(top);
         const double inv = reciprocal64(scale);
         if (lane == 0) p.scale[row] = scale;
