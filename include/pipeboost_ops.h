@@ -244,7 +244,8 @@ int pb_op_quant_q8(int32_t dtype, const void* x, int64_t ld_x, int32_t x_f32, in
  *   epi 2: R += Y
  *   epi 3: R = Y                                             (logits)
  * bias [N] dt or NULL; C dt or R fp32 [M, N] with row stride ldo.  X and W hold any
- * 8-bit integers; both 16-byte aligned, row strides multiples of 16 up to 2^23.
+ * 8-bit integers; both 16-byte aligned, row strides multiples of 16 up to 2^23 (of 128:
+ * up to a third faster).
  * K is a multiple of 16, at most 131056; any M and N up to 2^24 whose tiles of 64 x 64
  * stay below 2^23.  workspace (may be NULL): partial sums where K is split, up to
  * pb_op_gemm_q8_workspace bytes (0 for refused sizes); results do not depend on it.

@@ -243,7 +243,7 @@ __device__ __forceinline__ void add_rest(const GemmQ8Params& p, int k0, int mb, 
 // LDS rows are 128 bytes, 16-byte chunks XOR-permuted by row & 7: operand reads of 16
 // rows are free of bank conflicts.
 //
-// 4096 x 36864 x 9216: 1016 us, 2.74 POP/s (the vendor library's 8-bit product 1212 us).  All
+// 4096 x 36864 x 9216: 980-1016 us, 2.7-2.8 POP/s (the vendor library's 8-bit product 1212 us).  All
 // tile heights copy 42-46 GB/s a CU (11 TB/s in all) into LDS, and that is the bound: one
 // round of 240 blocks (M 1511, N 4992, K 5120) takes 46.8 us with cold weights, 45 with a
 // sixteenth of its products, 36.7 if every copy finds its lines in the L2, 32.4 without

@@ -12,7 +12,7 @@
 //
 // Both read a row once into registers (fp32) and write it once: 4096 rows of 9216, fp32
 // stream and fp16 delta, 82-89 us (4.7-5.1 TB/s, a large copy 4.76); 4096 of 36864 in fp16
-// 83-88 us (5.1-5.5); 1001 of 4096 in bf16, one round of blocks, 11-13 us (2.9-3.4).  Few
+// 83-88 us (5.1-5.5); 1001 of 4091 in bf16, one round of blocks, 11-13 us (2.9-3.4).  Few
 // rows are bound by the latency of one load, the reductions and one store (one of 2048: 2.6 us).
 #include <algorithm>
 #include <cmath>
