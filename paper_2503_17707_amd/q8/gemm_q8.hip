@@ -41,22 +41,20 @@ __device__ __forceinline__ void store4(T* p, int left, const float (&y)[4]) {
 }
 
 template <typename T>
-__device__ __forceinline__ void load4(const T* p, int left, float (&f)[4]) {
-    T t[4] = {};
+__device__ __forceinline__ void load4(const T* p, int left, T (&t)[4]) {
     if (left >= 4) {
         __builtin_memcpy(t, p, sizeof(t));
     } else {
 #pragma unroll
-        for (int r = 0; r < 3; ++r)
-            if (r < left) t[r] = p[r];
+        for (int r = 0; r < 4; ++r) t[r] = r < 3 && r < left ? p[r] : T();
     }
-#pragma unroll
-    for (int r = 0; r < 4; ++r) f[r] = (float)t[r];
 }
 
-// What the epilogue knows of features n .. n+3.
+// What the epilogue knows of features n .. n+3: loaded first, made ready when the loads of
+// a wave's features, scales and old values are all on their way.
 struct Features {
-    float sw[4], b[4];
+    float sw[4], b[4], q[4];
+    uint16_t bias[4];
     int left;  // of them inside N: 4 or more, or fewer
 };
 
@@ -65,37 +63,53 @@ __device__ __forceinline__ Features load_features(const GemmQ8Params& p, int n) 
     f.left = p.N - n;
     load4(p.sw + n, f.left, f.sw);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) f.b[r] = 0.f;
-    if (p.bias) {
-        if (p.bf16) load4((const __bf16*)p.bias + n, f.left, f.b);
-        else load4((const _Float16*)p.bias + n, f.left, f.b);
-    }
+    for (int r = 0; r < 4; ++r) f.bias[r] = 0;  // (zero in both types)
+    if (p.bias) load4((const uint16_t*)p.bias + n, f.left, f.bias);
     return f;
 }
 
-// Features n .. n+3 of token m: (sum rounded to fp32, times sx) times sw plus bias,
-// the second product and the sum rounded once; then the epilogue.  Rows of the output
-// may start at any element (N odd): vectors go there as they come.
-__device__ __forceinline__ void epilogue8(const GemmQ8Params& p, int m, int n, float sx, const Features& f, i32x4 acc) {
-    float y[4];
+__device__ __forceinline__ void ready(const GemmQ8Params& p, int n, Features& f) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float wide = __uint_as_float((uint32_t)f.bias[r] << 16);
+        f.b[r] = p.bf16 ? wide : (float)__builtin_bit_cast(_Float16, f.bias[r]);
+        f.q[r] = n + r < p.qcols ? p.qscale : 1.f;
+    }
+}
+
+// What the residual stream holds there (asked for before the sums are at hand; a load after
+// another feature's store would wait for it).
+__device__ __forceinline__ void load_old(const GemmQ8Params& p, int m, int n, int left, float (&old)[4]) {
+    if (p.epi == Q8_RESID) load4((const float*)p.out + (int64_t)m * p.ldo + n, left, old);
+}
+
+// (the sum rounded to fp32, times sx) times sw plus bias, the second product and the sum
+// rounded once; then ReLU or the scale of the first qcols features (1 past them, and in other
+// epilogues).
+__device__ __forceinline__ void values(const GemmQ8Params& p, float sx, const Features& f, i32x4 acc, float (&y)[4]) {
+    const float least = p.epi == Q8_RELU ? 0.f : -INFINITY;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         y[r] = fmaf((float)acc[r] * sx, f.sw[r], f.b[r]);
-        if (p.epi == Q8_RELU) y[r] = y[r] < 0.f ? 0.f : y[r];  // (NaN stays)
-        if (p.epi == Q8_QKV && n + r < p.qcols) y[r] *= p.qscale;
+        y[r] = (y[r] < least ? least : y[r]) * f.q[r];  // (NaN stays)
         // the 16-bit rounding apart from the product before it, in every kernel
         asm volatile("" : "+v"(y[r]));
     }
+}
+
+// Features n .. n+3 of token m.  Rows of the output may start at any element (N odd): vectors
+// go there as they come.
+__device__ __forceinline__ void epilogue8(const GemmQ8Params& p, int m, int n, float sx, const Features& f, i32x4 acc,
+                                          const float (&old)[4]) {
+    float y[4];
+    values(p, sx, f, acc, y);
     const int64_t at = (int64_t)m * p.ldo + n;
     if (p.epi >= Q8_RESID) {
-        float* out = (float*)p.out + at;
         if (p.epi == Q8_RESID) {
-            float old[4];
-            load4(out, f.left, old);
 #pragma unroll
             for (int r = 0; r < 4; ++r) y[r] += old[r];
         }
-        store4(out, f.left, y);
+        store4((float*)p.out + at, f.left, y);
     } else if (p.bf16) {
         store4((__bf16*)p.out + at, f.left, y);
     } else {
@@ -169,6 +183,56 @@ __device__ __forceinline__ Job tile_job(const GemmQ8Params& p, const Split& sp) 
     return j;
 }
 
+// A wave's sums as they are stored where all of its features are inside N, ADD: onto what is
+// there.  No branch but for the row's end, the next row's old values asked for before this
+// one's stores (with branches on kind, type and edge about every four features and loads
+// between the stores: 1633 x 16384 x 4096 onto the stream 169 us, now 144, in fp16 136, now
+// 110; 4096 x 16384 x 4096 in fp16 277 and 235).
+template <typename T, bool ADD, int MF, int NF>
+__device__ __forceinline__ void store_inside(const GemmQ8Params& p, int mb, int nb, int lr, int lg, const float (&sx)[MF],
+                                             Features (&f)[NF], const i32x4 (&acc)[NF][MF]) {
+    T* out = (T*)p.out + (int64_t)(mb + lr) * p.ldo + (nb + 4 * lg);
+    float old[2][NF][4];
+    auto load_row = [&](int j) {
+        if (mb + 16 * j + lr < p.M) {
+#pragma unroll
+            for (int i = 0; i < NF; ++i) __builtin_memcpy(old[j & 1][i], out + 16 * j * p.ldo + 16 * i, sizeof(old[0][0]));
+        }
+    };
+    if (ADD) load_row(0);
+#pragma unroll
+    for (int i = 0; i < NF; ++i) ready(p, nb + 16 * i + 4 * lg, f[i]);
+#pragma unroll
+    for (int j = 0; j < MF; ++j) {
+        if (ADD && j + 1 < MF) load_row(j + 1);
+        if (mb + 16 * j + lr >= p.M) continue;
+        T t[NF][4];
+#pragma unroll
+        for (int i = 0; i < NF; ++i) {
+            float y[4];
+            values(p, sx[j], f[i], acc[i][j], y);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) t[i][r] = (T)(ADD ? y[r] + old[j & 1][i][r] : y[r]);
+        }
+        if constexpr (sizeof(T) == 2 && NF % 2 == 0) {
+            // two fragments' features 4 lg .. + 3 become one's 8 (lg / 2) .. + 7, a whole 16 bytes
+#pragma unroll
+            for (int i = 0; i < NF; i += 2) {
+                uint32_t a[2], b[2];
+                __builtin_memcpy(a, t[i], sizeof(a));
+                __builtin_memcpy(b, t[i + 1], sizeof(b));
+                const auto lo = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
+                const auto hi = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+                const uint32_t w[4] = {lo[0], hi[0], lo[1], hi[1]};
+                __builtin_memcpy(out + 16 * j * p.ldo + 16 * i + 12 * (lg & 1), w, sizeof(w));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NF; ++i) __builtin_memcpy(out + 16 * j * p.ldo + 16 * i, t[i], sizeof(t[i]));
+        }
+    }
+}
+
 // A wave's sums: acc[i][j] holds features nb + 16 i + 4 lg + r of token mb + 16 j + lr.
 template <int BN, int MF, int NF>
 __device__ __forceinline__ void store_tile(const GemmQ8Params& p, const Job& jb, int mb, int nb, int lr, int lg,
@@ -190,13 +254,25 @@ __device__ __forceinline__ void store_tile(const GemmQ8Params& p, const Job& jb,
     float sx[MF];
 #pragma unroll
     for (int j = 0; j < MF; ++j) sx[j] = p.sx[min(mb + 16 * j + lr, p.M - 1)];
+    const bool inside = nb + 16 * NF <= p.N;
+    if (inside && p.epi == Q8_RESID) store_inside<float, true>(p, mb, nb, lr, lg, sx, f, acc);
+    else if (inside && p.epi == Q8_LOGITS) store_inside<float, false>(p, mb, nb, lr, lg, sx, f, acc);
+    else if (inside && p.bf16) store_inside<__bf16, false>(p, mb, nb, lr, lg, sx, f, acc);
+    else if (inside) store_inside<_Float16, false>(p, mb, nb, lr, lg, sx, f, acc);
+    if (inside) return;
+#pragma unroll
+    for (int i = 0; i < NF; ++i) ready(p, nb + 16 * i + 4 * lg, f[i]);
 #pragma unroll
     for (int j = 0; j < MF; ++j) {
         const int m = mb + 16 * j + lr;
         if (m >= p.M) continue;
 #pragma unroll
-        for (int i = 0; i < NF; ++i)
-            if (f[i].left > 0) epilogue8(p, m, nb + 16 * i + 4 * lg, sx[j], f[i], acc[i][j]);
+        for (int i = 0; i < NF; ++i) {
+            const int n = nb + 16 * i + 4 * lg;
+            float old[4] = {};
+            if (f[i].left > 0) load_old(p, m, n, f[i].left, old);
+            if (f[i].left > 0) epilogue8(p, m, n, sx[j], f[i], acc[i][j], old);
+        }
     }
 }
 
@@ -535,10 +611,16 @@ __global__ __launch_bounds__(64 * KW) void q8_few_kernel(GemmQ8Params p) {
     part[wave][lane] = acc;
     __syncthreads();
     if (wave > 0) return;
+    const int n = n0 + 4 * lg;
+    float old[4] = {};
+    if (here && n < p.N) load_old(p, lr, n, p.N - n, old);
 #pragma unroll
     for (int k = 1; k < KW; ++k) acc += part[k][lane];
-    const int n = n0 + 4 * lg;
-    if (here && n < p.N) epilogue8(p, lr, n, p.sx[lr], load_features(p, n), acc);
+    if (here && n < p.N) {
+        Features f = load_features(p, n);
+        ready(p, n, f);
+        epilogue8(p, lr, n, p.sx[lr], f, acc, old);
+    }
 }
 
 // ---- the sums of split tiles -------------------------------------------------------------
@@ -555,8 +637,10 @@ __global__ __launch_bounds__(256) void q8_join_kernel(GemmQ8Params p, Split sp) 
     if (m >= p.M || n >= p.N) return;
     const int64_t stride = (int64_t)sp.tail * (BM * BN);
     const int32_t* src = p.ws + (int64_t)i * (BM * BN) + at;
-    const Features f = load_features(p, n);
+    Features f = load_features(p, n);
     const float sx = p.sx[m];
+    float old[4] = {};
+    load_old(p, m, n, f.left, old);
     i32x4 v = {0, 0, 0, 0};
     for (int s = 0; s < sp.splits; s += 8) {  // eight ranges' loads in flight together
         i32x4 o[8];
@@ -568,7 +652,8 @@ __global__ __launch_bounds__(256) void q8_join_kernel(GemmQ8Params p, Split sp) 
 #pragma unroll
         for (int q = 0; q < 8; ++q) v += o[q];
     }
-    epilogue8(p, m, n, sx, f, v);
+    ready(p, n, f);
+    epilogue8(p, m, n, sx, f, v, old);
 }
 
 // ---- launches ----------------------------------------------------------------------------
