@@ -678,17 +678,17 @@ struct Shape {
 // gained less than 0.2% beside these are not kept (16 waves or 32 features for few tokens,
 // 512-byte rows).
 constexpr Shape SHAPES[] = {
-    {FEW, 16, 16, 256, 256, 2048, 2.58f, 0.122f, 0.186f, 5.08f, 0.92f, 0.66f, 0.1f, 0, 0, 0},
-    {FEW, 16, 16, 256, 512, 256, 2.47f, 0.178f, 0.028f, 4.96f, 0.22f, 0.01f, 0, 0, 0, 0},
-    {RING, 32, 32, 256, 128, 512, 3.26f, 0.279f, 0, 7.78f, 0.78f, 0.15f, 2.0f, 2.3f, 5.1f, 0.01f},
-    {RING, 32, 64, 256, 256, 256, 3.47f, 0.301f, 0, 8.74f, 0.79f, 0.47f, 2.2f, 2.4f, 11.6f, 0.02f},
-    {RING, 64, 64, 256, 256, 256, 4.09f, 0.477f, 0, 7.50f, 0.34f, 0.22f, 3.0f, 2.1f, 14.6f, 0.04f},
-    {RING, 64, 128, 128, 512, 256, 4.10f, 0.337f, 0, 9.29f, 0.69f, 0.50f, 2.7f, 1.5f, 10.2f, 0.31f},
-    {RING, 128, 64, 256, 256, 256, 5.82f, 0.716f, 0, 5.34f, 0.23f, 0.12f, 4.2f, 1.3f, 29.f, 0.00f},
-    {RING, 128, 128, 128, 512, 256, 5.64f, 0.495f, 0, 6.90f, 0.37f, 0.34f, 4.4f, 1.6f, 10.6f, 0.23f},
-    {WIDE, 128, 256, 128, 512, 256, 8.84f, 0.714f, 0, 7.84f, 0.62f, 0.62f, 5.5f, 0.2f, 8.9f, 0.17f},
-    {WIDE, 192, 256, 128, 512, 256, 10.2f, 0.905f, 0, 6.87f, 0.35f, 0.37f, 6.3f, 0.0f, 8.0f, 0.09f},
-    {WIDE, 256, 256, 128, 512, 256, 11.9f, 1.080f, 0, 6.05f, 0.12f, 0.47f, 7.9f, 0.0f, 8.5f, 0.34f},
+    {FEW, 16, 16, 256, 256, 2048, 2.62f, 0.106f, 0.211f, 4.99f, 0.91f, 0.67f, 0.0f, 0, 0, 0},
+    {FEW, 16, 16, 256, 512, 256, 2.54f, 0.175f, 0.027f, 6.88f, 0.37f, 0.03f, 0, 0, 0, 0},
+    {RING, 32, 32, 256, 128, 512, 3.16f, 0.273f, 0, 7.72f, 0.79f, 0.17f, 1.9f, 2.4f, 4.5f, 0.01f},
+    {RING, 32, 64, 256, 256, 256, 3.32f, 0.304f, 0, 8.67f, 0.78f, 0.47f, 2.1f, 2.6f, 8.7f, 0.02f},
+    {RING, 64, 64, 256, 256, 256, 3.85f, 0.473f, 0, 7.70f, 0.37f, 0.23f, 2.7f, 2.4f, 10.6f, 0.03f},
+    {RING, 64, 128, 128, 512, 256, 3.53f, 0.335f, 0, 9.57f, 0.72f, 0.52f, 2.4f, 2.2f, 9.0f, 0.32f},
+    {RING, 128, 64, 256, 256, 256, 4.42f, 0.718f, 0, 5.45f, 0.19f, 0.12f, 2.7f, 2.3f, 8.9f, 0.10f},
+    {RING, 128, 128, 128, 512, 256, 4.30f, 0.492f, 0, 7.09f, 0.34f, 0.37f, 3.0f, 2.8f, 8.3f, 0.28f},
+    {WIDE, 128, 256, 128, 512, 256, 5.84f, 0.706f, 0, 8.68f, 0.70f, 0.61f, 3.6f, 3.0f, 8.0f, 0.32f},
+    {WIDE, 192, 256, 128, 512, 256, 7.24f, 0.874f, 0, 6.91f, 0.41f, 0.41f, 5.4f, 2.9f, 8.2f, 0.31f},
+    {WIDE, 256, 256, 128, 512, 256, 8.99f, 1.040f, 0, 6.90f, 0.29f, 0.47f, 6.9f, 2.4f, 8.5f, 0.83f},
 };
 constexpr int N_SHAPES = sizeof(SHAPES) / sizeof(SHAPES[0]);
 

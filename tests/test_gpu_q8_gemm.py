@@ -99,6 +99,8 @@ KERNELS = [
     (400, 26092, 144),  # 256 x 256
     (1, 13185, 2048), (1, 12146, 2176), (386, 4785, 6656), (88, 16863, 5328), (143, 6423, 9312), (566, 31211, 5504),
     (556, 22808, 2224), (403, 8506, 6784), (198, 22556, 3872),
+    (1, 754, 12032), (1, 918, 8320), (97, 19052, 12288), (639, 35, 1920), (1337, 86, 30288), (177, 16833, 3088), (1278, 1036, 12864),
+    (392, 5836, 10880), (452, 5855, 7744), (1169, 13350, 2816), (500, 5888, 7744), (1169, 13312, 2816),
     # weight rows a multiple of 4 KB apart: columns of tiles that start at other places of K
     (20, 1000, 4096), (40, 600, 8192), (64, 2100, 12288), (100, 5000, 4096), (128, 20000, 4096), (90, 520, 16384),
 ]
@@ -127,6 +129,14 @@ def test_every_kernel(M, N, K):
     pb.op_gemm_q8(1, 1, X, sx, W, sw, bias, C=C, workspace=_ws(M, N, K))
     want, tol = gemm64(X, sx, W, sw, bias, 1, 1.0, 0, old, torch.float16)
     assert bool(((C.double() - want).abs() <= tol).all())
+    bias = bias.bfloat16()
+    C = torch.zeros(M, N, dtype=torch.bfloat16, device="cuda")
+    pb.op_gemm_q8(0, 0, X, sx, W, sw, bias, C=C, qscale=0.3, qcols=N // 2 + 1, workspace=_ws(M, N, K))
+    want, tol = gemm64(X, sx, W, sw, bias, 0, 0.3, N // 2 + 1, old, torch.bfloat16)
+    assert bool(((C.double() - want).abs() <= tol).all())
+    pb.op_gemm_q8(0, 3, X, sx, W, sw, None, R=R, workspace=_ws(M, N, K))
+    want, tol = gemm64(X, sx, W, sw, None, 3, 1.0, 0, old, torch.bfloat16)
+    assert bool(((R.double() - want).abs() <= tol).all())
 
 
 @pytest.mark.parametrize("M,N,K", [(1, 300, 2048), (7, 130, 1040), (40, 515, 2064), (150, 260, 528), (600, 600, 320),
