@@ -53,7 +53,7 @@ __device__ __forceinline__ void load4(const T* p, int left, T (&t)[4]) {
 // What the epilogue knows of features n .. n+3: loaded first, made ready when the loads of
 // a wave's features, scales and old values are all on their way.
 struct Features {
-    float sw[4], b[4], q[4];
+    float sw[4], b[4];
     uint16_t bias[4];
     int left;  // of them inside N: 4 or more, or fewer
 };
@@ -68,12 +68,11 @@ __device__ __forceinline__ Features load_features(const GemmQ8Params& p, int n) 
     return f;
 }
 
-__device__ __forceinline__ void ready(const GemmQ8Params& p, int n, Features& f) {
+__device__ __forceinline__ void ready(const GemmQ8Params& p, Features& f) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         const float wide = __uint_as_float((uint32_t)f.bias[r] << 16);
         f.b[r] = p.bf16 ? wide : (float)__builtin_bit_cast(_Float16, f.bias[r]);
-        f.q[r] = n + r < p.qcols ? p.qscale : 1.f;
     }
 }
 
@@ -84,14 +83,14 @@ __device__ __forceinline__ void load_old(const GemmQ8Params& p, int m, int n, in
 }
 
 // (the sum rounded to fp32, times sx) times sw plus bias, the second product and the sum
-// rounded once; then ReLU or the scale of the first qcols features (1 past them, and in other
-// epilogues).
-__device__ __forceinline__ void values(const GemmQ8Params& p, float sx, const Features& f, i32x4 acc, float (&y)[4]) {
-    const float least = p.epi == Q8_RELU ? 0.f : -INFINITY;
+// rounded once; then ReLU or the scale of the first qcols features.
+__device__ __forceinline__ void values(const GemmQ8Params& p, int epi, int n, float sx, const Features& f, i32x4 acc,
+                                       float (&y)[4]) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         y[r] = fmaf((float)acc[r] * sx, f.sw[r], f.b[r]);
-        y[r] = (y[r] < least ? least : y[r]) * f.q[r];  // (NaN stays)
+        if (epi == Q8_RELU) y[r] = y[r] < 0.f ? 0.f : y[r];  // (NaN stays)
+        if (epi == Q8_QKV) y[r] *= n + r < p.qcols ? p.qscale : 1.f;
         // the 16-bit rounding apart from the product before it, in every kernel
         asm volatile("" : "+v"(y[r]));
     }
@@ -102,7 +101,7 @@ __device__ __forceinline__ void values(const GemmQ8Params& p, float sx, const Fe
 __device__ __forceinline__ void epilogue8(const GemmQ8Params& p, int m, int n, float sx, const Features& f, i32x4 acc,
                                           const float (&old)[4]) {
     float y[4];
-    values(p, sx, f, acc, y);
+    values(p, p.epi, n, sx, f, acc, y);
     const int64_t at = (int64_t)m * p.ldo + n;
     if (p.epi >= Q8_RESID) {
         if (p.epi == Q8_RESID) {
@@ -183,34 +182,38 @@ __device__ __forceinline__ Job tile_job(const GemmQ8Params& p, const Split& sp) 
     return j;
 }
 
-// A wave's sums as they are stored where all of its features are inside N, ADD: onto what is
-// there.  No branch but for the row's end, the next row's old values asked for before this
-// one's stores (with branches on kind, type and edge about every four features and loads
-// between the stores: 1633 x 16384 x 4096 onto the stream 169 us, now 144, in fp16 136, now
-// 110; 4096 x 16384 x 4096 in fp16 277 and 235).
-template <typename T, bool ADD, int MF, int NF>
+// A wave's sums as they are stored where all of its features are inside N.  No branch but for
+// the last token, the next row's old values asked for before this one's stores (with branches on
+// kind, type and edge about every four features and loads between the stores: 1633 x 16384 x
+// 4096 onto the stream 169 us, now 144, in fp16 136, now 110; 4096 x 16384 x 4096 in fp16 277
+// and 235).
+template <typename T, int EPI, int MF, int NF>
 __device__ __forceinline__ void store_inside(const GemmQ8Params& p, int mb, int nb, int lr, int lg, const float (&sx)[MF],
                                              Features (&f)[NF], const i32x4 (&acc)[NF][MF]) {
+    constexpr bool ADD = EPI == Q8_RESID;
     T* out = (T*)p.out + (int64_t)(mb + lr) * p.ldo + (nb + 4 * lg);
+    const T* next = out;
     float old[2][NF][4];
     auto load_row = [&](int j) {
         if (mb + 16 * j + lr < p.M) {
 #pragma unroll
-            for (int i = 0; i < NF; ++i) __builtin_memcpy(old[j & 1][i], out + 16 * j * p.ldo + 16 * i, sizeof(old[0][0]));
+            for (int i = 0; i < NF; ++i) __builtin_memcpy(old[j & 1][i], next + 16 * i, sizeof(old[0][0]));
         }
+        next += 16 * p.ldo;
     };
     if (ADD) load_row(0);
 #pragma unroll
-    for (int i = 0; i < NF; ++i) ready(p, nb + 16 * i + 4 * lg, f[i]);
+    for (int i = 0; i < NF; ++i) ready(p, f[i]);
 #pragma unroll
-    for (int j = 0; j < MF; ++j) {
+    for (int j = 0; j < MF; ++j, out += 16 * p.ldo) {
+        asm volatile("" : "+v"(out));  // (one row's address at a time)
         if (ADD && j + 1 < MF) load_row(j + 1);
         if (mb + 16 * j + lr >= p.M) continue;
         T t[NF][4];
 #pragma unroll
         for (int i = 0; i < NF; ++i) {
             float y[4];
-            values(p, sx[j], f[i], acc[i][j], y);
+            values(p, EPI, nb + 16 * i + 4 * lg, sx[j], f[i], acc[i][j], y);
 #pragma unroll
             for (int r = 0; r < 4; ++r) t[i][r] = (T)(ADD ? y[r] + old[j & 1][i][r] : y[r]);
         }
@@ -224,11 +227,11 @@ __device__ __forceinline__ void store_inside(const GemmQ8Params& p, int mb, int 
                 const auto lo = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
                 const auto hi = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
                 const uint32_t w[4] = {lo[0], hi[0], lo[1], hi[1]};
-                __builtin_memcpy(out + 16 * j * p.ldo + 16 * i + 12 * (lg & 1), w, sizeof(w));
+                __builtin_memcpy(out + 16 * i + 12 * (lg & 1), w, sizeof(w));
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < NF; ++i) __builtin_memcpy(out + 16 * j * p.ldo + 16 * i, t[i], sizeof(t[i]));
+            for (int i = 0; i < NF; ++i) __builtin_memcpy(out + 16 * i, t[i], sizeof(t[i]));
         }
     }
 }
@@ -255,13 +258,20 @@ __device__ __forceinline__ void store_tile(const GemmQ8Params& p, const Job& jb,
 #pragma unroll
     for (int j = 0; j < MF; ++j) sx[j] = p.sx[min(mb + 16 * j + lr, p.M - 1)];
     const bool inside = nb + 16 * NF <= p.N;
-    if (inside && p.epi == Q8_RESID) store_inside<float, true>(p, mb, nb, lr, lg, sx, f, acc);
-    else if (inside && p.epi == Q8_LOGITS) store_inside<float, false>(p, mb, nb, lr, lg, sx, f, acc);
-    else if (inside && p.bf16) store_inside<__bf16, false>(p, mb, nb, lr, lg, sx, f, acc);
-    else if (inside) store_inside<_Float16, false>(p, mb, nb, lr, lg, sx, f, acc);
-    if (inside) return;
+    if (inside) {
+        auto store = [&](auto kind, auto type) {
+            store_inside<decltype(type), decltype(kind)::value>(p, mb, nb, lr, lg, sx, f, acc);
+        };
+        if (p.epi == Q8_RESID) store(std::integral_constant<int, Q8_RESID>(), 0.f);
+        else if (p.epi == Q8_LOGITS) store(std::integral_constant<int, Q8_LOGITS>(), 0.f);
+        else if (p.epi == Q8_RELU && p.bf16) store(std::integral_constant<int, Q8_RELU>(), (__bf16)0);
+        else if (p.epi == Q8_RELU) store(std::integral_constant<int, Q8_RELU>(), (_Float16)0);
+        else if (p.bf16) store(std::integral_constant<int, Q8_QKV>(), (__bf16)0);
+        else store(std::integral_constant<int, Q8_QKV>(), (_Float16)0);
+        return;
+    }
 #pragma unroll
-    for (int i = 0; i < NF; ++i) ready(p, nb + 16 * i + 4 * lg, f[i]);
+    for (int i = 0; i < NF; ++i) ready(p, f[i]);
 #pragma unroll
     for (int j = 0; j < MF; ++j) {
         const int m = mb + 16 * j + lr;
@@ -301,6 +311,12 @@ __device__ __forceinline__ void add_rest(const GemmQ8Params& p, int k0, int mb, 
     }
 }
 
+// 16-byte chunks of a row past the start of a line of 128 bytes (rows are a multiple of 16 bytes
+// apart, so rows 8 apart have the same).
+__device__ __forceinline__ uint32_t turn_of(const int8_t* base, int64_t ld, uint32_t row) {
+    return ((uint32_t)((uintptr_t)base >> 4) + row * (uint32_t)(ld >> 4)) & 7;
+}
+
 // ---- 256-feature tiles: two wave groups in ping-pong ----------------------------------
 // 64 XF tokens x 256 features, eight waves (2 x 4) of 32 XF x 64, K tiles of 128 bytes in
 // two LDS stages, filled by LDS-DMA.  A K tile is four phases, one per quadrant of the
@@ -327,7 +343,11 @@ __device__ __forceinline__ void add_rest(const GemmQ8Params& p, int k0, int mb, 
 // each.  So a block takes as many tokens as fill tiles.  Two phases a tile, three stages, stages
 // of uneven depth for tokens and weights and K ranges that start apart took as long, weights
 // from memory into registers 1.7 times as long.
-template <int XF>
+//
+// SKEW: rows off 128 bytes in three stages, pieces as in the ring below (1511 x 4999 x 5104 67 ->
+// 54 us; three stages of taller tiles do not fit).  Piece t + 3 goes where piece t was, in the
+// same order and slots: it is asked for three tiles ahead and first read two tiles ahead.
+template <int XF, bool SKEW>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void q8_wide_kernel(GemmQ8Params p, Split sp) {
     constexpr int BM = 64 * XF, BN = 256, RB = 128;
     constexpr int XH = 16 * XF;                // tokens of a wave's X half
@@ -335,7 +355,8 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void q
     constexpr int XQ = (XC + 7) / 8;           // ... per wave (XF = 3: four waves repeat the last one)
     constexpr int LAG = (4 + 2 * XQ) * 3 / 2;  // copies younger than the one a slot needs
     constexpr int STAGE = (BM + BN) * RB;
-    __shared__ __attribute__((aligned(16))) uint8_t smem[2 * STAGE];
+    constexpr int S = SKEW ? 3 : 2;
+    __shared__ __attribute__((aligned(16))) uint8_t smem[S * STAGE];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave & 1, wn = wave >> 1;
@@ -347,51 +368,70 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void q
     // is number wave + 8 q of its region.  Lane i writes row i / 8, physical chunk i % 8.
     // Rows past the edge re-read the last one.
     const int lrow = lane >> 3, chk = ((lane & 7) ^ lrow) * 16;
+    const int lr = lane & 15, lg = lane >> 4;
     const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
     const int8_t* Xb = p.X + (int64_t)m0 * p.ldx + (int64_t)jb.t0 * RB;
     const int8_t* Wb = p.W + (int64_t)n0 * p.ldw + (int64_t)jb.t0 * RB;
+    // SKEW: rows 8 apart have the same turn, so a lane's chunks are late in all copies of X or W
+    // or in none (rows past the edge too: only where they start, not what is in range, goes by it)
+    const uint32_t begin_x = SKEW && chk / 16 + turn_of(Xb, p.ldx, lrow) < 8 ? RB : 0;
+    const uint32_t begin_w = SKEW && chk / 16 + turn_of(Wb, p.ldw, lrow) < 8 ? RB : 0;
     int xrow[2 * XQ], wrow[4];  // first row of copy q of region h: [XQ h + q], [2 h + q]
     uint32_t xoff[2 * XQ], woff[4];
 #pragma unroll
     for (int i = 0; i < 2 * XQ; ++i) {
         const int h = i / XQ, c = min(wave + 8 * (i % XQ), XC - 1);
         xrow[i] = (2 * (c / (XC / 2)) + h) * XH + (c % (XC / 2)) * 8;
-        xoff[i] = (uint32_t)min(xrow[i] + lrow, p.M - 1 - m0) * (uint32_t)p.ldx + chk;
+        xoff[i] = (uint32_t)min(xrow[i] + lrow, p.M - 1 - m0) * (uint32_t)p.ldx + chk + begin_x;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int h = i >> 1, c = wave + 8 * (i & 1);
         wrow[i] = (c >> 2) * 64 + h * 32 + (c & 3) * 8;
-        woff[i] = (uint32_t)min(wrow[i] + lrow, p.N - 1 - n0) * (uint32_t)p.ldw + chk;
+        woff[i] = (uint32_t)min(wrow[i] + lrow, p.N - 1 - n0) * (uint32_t)p.ldw + chk + begin_w;
     }
-    auto copy_x = [&](int t, int stage, int h) {
-        const int8_t* b = Xb + (int64_t)t * RB;
-#pragma unroll
-        for (int i = XQ * h; i < XQ * h + XQ; ++i) dma16s(b, xoff[i], lds0 + stage * STAGE + xrow[i] * RB);
+    // piece t; SKEW: counted from a tile before, of the first and last what is inside the range
+    const int last = SKEW ? nk : nk - 1;  // (a launch has a K tile for every block)
+    auto place = [&](uint32_t off, int t, uint32_t begin) -> uint32_t {
+        if constexpr (!SKEW) return off;
+        if (t == 0 && begin == 0) return off - chk + RB;
+        return t == last ? off - begin : off;
     };
-    auto copy_w = [&](int t, int stage, int h) {
-        const int8_t* b = Wb + (int64_t)t * RB;
+    auto copy_x = [&](int t, uint32_t stage, int h) {
+        const int8_t* b = Xb + (int64_t)(SKEW ? t - 1 : t) * RB;
 #pragma unroll
-        for (int i = 2 * h; i < 2 * h + 2; ++i) dma16s(b, woff[i], lds0 + stage * STAGE + (BM + wrow[i]) * RB);
+        for (int i = XQ * h; i < XQ * h + XQ; ++i) dma16s(b, place(xoff[i], t, begin_x), lds0 + stage + xrow[i] * RB);
+    };
+    auto copy_w = [&](int t, uint32_t stage, int h) {
+        const int8_t* b = Wb + (int64_t)(SKEW ? t - 1 : t) * RB;
+#pragma unroll
+        for (int i = 2 * h; i < 2 * h + 2; ++i) dma16s(b, place(woff[i], t, begin_w), lds0 + stage + (BM + wrow[i]) * RB);
     };
 
     i32x4 acc[4][2 * XF] = {};
-    const int lr = lane & 15, lg = lane >> 4;
     i32x4 w0[2][2], w1[2][2], x[XF][2];  // [fragment][k half]
     const uint32_t lk[2] = {(uint32_t)(lr * RB + ((lg ^ (lr & 7)) << 4)), (uint32_t)(lr * RB + (((4 + lg) ^ (lr & 7)) << 4))};
-    auto read_w = [&](i32x4(&w)[2][2], int stage, int h) {
-        const uint8_t* s = smem + stage * STAGE + (BM + wn * 64 + h * 32) * RB;
+    bool late_x[2], late_w[2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+    for (int kk = 0; kk < 2; ++kk) {
+        late_x[kk] = SKEW && kk * 4 + lg + turn_of(Xb, p.ldx, lr) >= 8;
+        late_w[kk] = SKEW && kk * 4 + lg + turn_of(Wb, p.ldw, lr) >= 8;
+    }
+    auto read_w = [&](i32x4(&w)[2][2], uint32_t stage, uint32_t next, int h) {
 #pragma unroll
-            for (int kk = 0; kk < 2; ++kk) w[i][kk] = *(const i32x4*)(s + i * 16 * RB + lk[kk]);
+        for (int kk = 0; kk < 2; ++kk) {
+            const uint8_t* s = smem + (late_w[kk] ? next : stage) + (BM + wn * 64 + h * 32) * RB;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) w[i][kk] = *(const i32x4*)(s + i * 16 * RB + lk[kk]);
+        }
     };
-    auto read_x = [&](int stage, int h) {
-        const uint8_t* s = smem + stage * STAGE + (2 * wm + h) * XH * RB;
+    auto read_x = [&](uint32_t stage, uint32_t next, int h) {
 #pragma unroll
-        for (int j = 0; j < XF; ++j)
+        for (int kk = 0; kk < 2; ++kk) {
+            const uint8_t* s = smem + (late_x[kk] ? next : stage) + (2 * wm + h) * XH * RB;
 #pragma unroll
-            for (int kk = 0; kk < 2; ++kk) x[j][kk] = *(const i32x4*)(s + j * 16 * RB + lk[kk]);
+            for (int j = 0; j < XF; ++j) x[j][kk] = *(const i32x4*)(s + j * 16 * RB + lk[kk]);
+        }
     };
     // nothing moves across the end of a slot
     auto barrier = [] { asm volatile("s_barrier" ::: "memory"); };
@@ -414,45 +454,52 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void q
         __builtin_amdgcn_sched_barrier(0);
     };
 
-    const int last = nk - 1;  // (a launch has a K tile for every block)
-    auto fill = [&](int t, int stage) {  // a whole stage, in order of need
-        copy_w(t, stage, stage);
-        copy_x(t, stage, 0);
-        copy_w(t, stage, 1 - stage);
-        copy_x(t, stage, 1);
+    auto fill = [&](int t, int stage, int first) {  // a whole stage, in order of need
+        copy_w(t, stage * STAGE, first);
+        copy_x(t, stage * STAGE, 0);
+        copy_w(t, stage * STAGE, 1 - first);
+        copy_x(t, stage * STAGE, 1);
     };
-    fill(0, 0);
-    fill(min(1, last), 1);
+    fill(0, 0, 0);
+    fill(min(1, last), 1, SKEW ? 0 : 1);
+    if (SKEW) fill(min(2, last), 2, 1);
     wait_vmcnt<LAG>();
     barrier();
-    read_w(w0, 0, 0);
+    read_w(w0, 0, STAGE, 0);
     end_memory();              // both groups hold Wa of tile 0: its region may be refilled
     if (wave >= 4) barrier();  // one slot behind from here on
+    uint32_t s0 = 0, s1 = STAGE, s2 = 2 * STAGE;  // the stages of pieces t, t + 1, t + 2
     auto tile = [&](int t, auto parity) {
-        constexpr int P = decltype(parity)::value;  // t % 2: the stage, and the feature half of Wa
+        constexpr int P = decltype(parity)::value;  // t % 2: the feature half of Wa, without SKEW the stage
         auto& wa = P ? w1 : w0;
         auto& wb = P ? w0 : w1;
-        const int tn = min(t + 2, last);
-        read_x(P, 0);
-        copy_w(tn, P, P);
+        const uint32_t here = SKEW ? s0 : P * STAGE, next = SKEW ? s1 : (1 - P) * STAGE;
+        const int tn = min(t + S, last);
+        read_x(here, next, 0);
+        copy_w(tn, here, P);
         wait_vmcnt<LAG>();  // Wb landed
         end_memory();
         products(wa, 2 * P, 0);
-        read_w(wb, P, 1 - P);
-        copy_x(tn, P, 0);
+        read_w(wb, here, next, 1 - P);
+        copy_x(tn, here, 0);
         wait_vmcnt<LAG>();  // X1 landed
         end_memory();
         products(wb, 2 - 2 * P, 0);
-        read_x(P, 1);
-        copy_w(tn, P, 1 - P);
+        read_x(here, next, 1);
+        copy_w(tn, here, 1 - P);
         wait_vmcnt<LAG>();  // Wa of t + 1 landed
         end_memory();
         products(wb, 2 - 2 * P, XF);
-        read_w(wb, 1 - P, 1 - P);  // Wa of t + 1
-        copy_x(tn, P, 1);
+        read_w(wb, next, s2, 1 - P);  // Wa of t + 1
+        copy_x(tn, here, 1);
         wait_vmcnt<LAG>();  // X0 of t + 1 landed
         end_memory();
         products(wa, 2 * P, XF);
+        if (SKEW) {
+            s0 = s1;
+            s1 = s2;
+            s2 = here;
+        }
     };
     const std::integral_constant<int, 0> even;
     const std::integral_constant<int, 1> odd;
@@ -475,7 +522,15 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void q
 // in flight while one is multiplied.  Bound by the weights' stream: 24 x 16384 x 4096 16.2 us
 // from memory (4.2 TB/s; 12.9 from the last-level cache), 64 x 36864 x 9216 70 us (4.9 TB/s).
 // 16-byte chunks are XOR-permuted by the low row bits.
-template <int BM, int BN, int WGM, int WGN, int BK, int S>
+//
+// SKEW: for rows that do not start on 128 bytes.  BK bytes of such a row from a K tile's first
+// on would touch a line more.  So a row's pieces start where its lines do, `turn` chunks
+// before its K tiles: piece t holds, in the places of a tile's chunks, those of tile t whose
+// place + turn is below CPR and the others (`late`) of tile t - 1.  A tile is read from two
+// stages; a ring of one more has as many copies in flight.  A step of 128 bytes took 1.5 and
+// 1.4 times as long (64 x 128 and 128 x 128), now 1.13 and 1.12; of 256 bytes 1.47 (32 x 64), now
+// 1.33, and 1.2, now as long (32 x 32, 64 x 64: not kept).  300 x 4096 x 4112 22.7 -> 18.8 us.
+template <int BM, int BN, int WGM, int WGN, int BK, int S, bool SKEW>
 __global__ __launch_bounds__(64 * WGM * WGN) void q8_ring_kernel(GemmQ8Params p, Split sp) {
     constexpr int NW = WGM * WGN;
     constexpr int WM = BM / WGM, WN = BN / WGN;
@@ -497,51 +552,78 @@ __global__ __launch_bounds__(64 * WGM * WGN) void q8_ring_kernel(GemmQ8Params p,
 
     const int8_t* Xb = p.X + (int64_t)m0 * p.ldx + (int64_t)jb.t0 * BK;
     const int8_t* Wb = p.W + (int64_t)n0 * p.ldw + (int64_t)jb.t0 * BK;
-    uint32_t off[NL];
+    auto chunk = [&](int j) { return (uint32_t)((lane % CPR) ^ (((wave + NW * j) * RPI + lane / CPR) & MASK)); };
+    uint32_t off[NL], late = 0;  // SKEW: off from a tile before, where the late ones are
 #pragma unroll
     for (int j = 0; j < NL; ++j) {
         const int row = (wave + NW * j) * RPI + lane / CPR;
-        const int ch = (lane % CPR) ^ (row & MASK);
-        off[j] = ((wave + NW * j) * RPI < BM ? (uint32_t)min(row, p.M - 1 - m0) * (uint32_t)p.ldx
-                                             : (uint32_t)min(row - BM, p.N - 1 - n0) * (uint32_t)p.ldw) + ch * 16;
+        const bool is_x = (wave + NW * j) * RPI < BM;
+        const uint32_t r = is_x ? min(row, p.M - 1 - m0) : min(row - BM, p.N - 1 - n0);
+        off[j] = r * (uint32_t)(is_x ? p.ldx : p.ldw) + chunk(j) * 16;
+        if constexpr (SKEW) {
+            if (chunk(j) + (is_x ? turn_of(Xb, p.ldx, r) : turn_of(Wb, p.ldw, r)) >= CPR) late |= 1u << j;
+            else off[j] += BK;
+        }
     }
     const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
+    const int pieces = SKEW && nk > 0 ? nk + 1 : nk;
     auto issue = [&](int t, int stage) {
-        t += jb.phase;
-        const int64_t at = (int64_t)(t >= nk ? t - nk : t) * BK;
+        if constexpr (!SKEW) {
+            t += jb.phase;
+            t = t >= nk ? t - nk : t;
+        }
+        const int64_t at = (int64_t)(SKEW ? t - 1 : t) * BK;
         const int8_t *xk = Xb + at, *wk = Wb + at;
 #pragma unroll
-        for (int j = 0; j < NL; ++j)
-            dma16s((wave + NW * j) * RPI < BM ? xk : wk, off[j], lds0 + stage * STAGE + (wave + NW * j) * 1024);
+        for (int j = 0; j < NL; ++j) {
+            uint32_t o = off[j];
+            if constexpr (SKEW) {  // nothing is read before a row's tiles, nor past them: what is there again
+                const bool l = late >> j & 1;
+                if (t == 0 && l) o += BK - chunk(j) * 16;
+                if (t == nk && !l) o -= BK;
+            }
+            dma16s((wave + NW * j) * RPI < BM ? xk : wk, o, lds0 + stage * STAGE + (wave + NW * j) * 1024);
+        }
     };
+    bool late_x[BK / 64], late_w[BK / 64];  // of this lane's chunks of a tile
+#pragma unroll
+    for (int kk = 0; kk < BK / 64; ++kk) {
+        late_x[kk] = SKEW && kk * 4 + lg + turn_of(Xb, p.ldx, lr) >= CPR;
+        late_w[kk] = SKEW && kk * 4 + lg + turn_of(Wb, p.ldw, lr) >= CPR;
+    }
     i32x4 acc[NF][MF] = {};
     auto compute = [&](int stage) {
         const uint8_t* s = smem + stage * STAGE;
+        const int next = SKEW ? (stage == S - 1 ? -(S - 1) * STAGE : STAGE) : 0;
 #pragma unroll
         for (int kk = 0; kk < BK / 64; ++kk) {
             const int ch = kk * 4 + lg;
+            const uint8_t *sx = s + (late_x[kk] ? next : 0), *sw = s + (late_w[kk] ? next : 0);
             i32x4 b[MF];
 #pragma unroll
             for (int j = 0; j < MF; ++j) {
                 const int row = wm * WM + j * 16 + lr;
-                b[j] = *(const i32x4*)(s + row * BK + ((ch ^ (row & MASK)) << 4));
+                b[j] = *(const i32x4*)(sx + row * BK + ((ch ^ (row & MASK)) << 4));
             }
 #pragma unroll
             for (int i = 0; i < NF; ++i) {
                 const int row = BM + wn * WN + i * 16 + lr;
-                const i32x4 a = *(const i32x4*)(s + row * BK + ((ch ^ (row & MASK)) << 4));
+                const i32x4 a = *(const i32x4*)(sw + row * BK + ((ch ^ (row & MASK)) << 4));
 #pragma unroll
                 for (int j = 0; j < MF; ++j) acc[i][j] = mma8(a, b[j], acc[i][j]);
             }
         }
     };
+    // tile t is whole once pieces up to t (SKEW: t + 1) have landed
+    constexpr int BEHIND = SKEW ? S - 3 : S - 2;
+    static_assert(BEHIND >= 1, "copies in flight");
 #pragma unroll
     for (int q = 0; q < S - 1; ++q)
-        if (q < nk) issue(q, q);
+        if (q < pieces) issue(q, q);
     int t = 0, st = 0;
-    for (; t + S - 1 < nk; ++t) {
-        wait_vmcnt<(S - 2) * NL>();
-        __syncthreads();  // stage st visible to all waves; the stage before it free
+    for (; t + S - 1 < pieces; ++t) {
+        wait_vmcnt<BEHIND * NL>();
+        __syncthreads();  // tile t visible to all waves; the stage before it free
         issue(t + S - 1, st == 0 ? S - 1 : st - 1);
         compute(st);
         st = st == S - 1 ? 0 : st + 1;
@@ -618,7 +700,7 @@ __global__ __launch_bounds__(64 * KW) void q8_few_kernel(GemmQ8Params p) {
     for (int k = 1; k < KW; ++k) acc += part[k][lane];
     if (here && n < p.N) {
         Features f = load_features(p, n);
-        ready(p, n, f);
+        ready(p, f);
         epilogue8(p, lr, n, p.sx[lr], f, acc, old);
     }
 }
@@ -652,7 +734,7 @@ __global__ __launch_bounds__(256) void q8_join_kernel(GemmQ8Params p, Split sp) 
 #pragma unroll
         for (int q = 0; q < 8; ++q) v += o[q];
     }
-    ready(p, n, f);
+    ready(p, f);
     epilogue8(p, m, n, sx, f, v, old);
 }
 
@@ -681,14 +763,14 @@ constexpr Shape SHAPES[] = {
     {FEW, 16, 16, 256, 256, 2048, 2.62f, 0.106f, 0.211f, 4.99f, 0.91f, 0.67f, 0.0f, 0, 0, 0},
     {FEW, 16, 16, 256, 512, 256, 2.54f, 0.175f, 0.027f, 6.88f, 0.37f, 0.03f, 0, 0, 0, 0},
     {RING, 32, 32, 256, 128, 512, 3.16f, 0.273f, 0, 7.72f, 0.79f, 0.17f, 1.9f, 2.4f, 4.5f, 0.01f},
-    {RING, 32, 64, 256, 256, 256, 3.32f, 0.304f, 0, 8.67f, 0.78f, 0.47f, 2.1f, 2.6f, 8.7f, 0.02f},
+    {RING, 32, 64, 256, 256, 256, 3.32f, 0.304f, 0, 8.67f, 0.78f, 0.33f, 2.1f, 2.6f, 8.7f, 0.02f},
     {RING, 64, 64, 256, 256, 256, 3.85f, 0.473f, 0, 7.70f, 0.37f, 0.23f, 2.7f, 2.4f, 10.6f, 0.03f},
-    {RING, 64, 128, 128, 512, 256, 3.53f, 0.335f, 0, 9.57f, 0.72f, 0.52f, 2.4f, 2.2f, 9.0f, 0.32f},
+    {RING, 64, 128, 128, 512, 256, 3.53f, 0.335f, 0, 9.57f, 0.72f, 0.13f, 2.4f, 2.2f, 9.0f, 0.32f},
     {RING, 128, 64, 256, 256, 256, 4.42f, 0.718f, 0, 5.45f, 0.19f, 0.12f, 2.7f, 2.3f, 8.9f, 0.10f},
-    {RING, 128, 128, 128, 512, 256, 4.30f, 0.492f, 0, 7.09f, 0.34f, 0.37f, 3.0f, 2.8f, 8.3f, 0.28f},
-    {WIDE, 128, 256, 128, 512, 256, 5.84f, 0.706f, 0, 8.68f, 0.70f, 0.61f, 3.6f, 3.0f, 8.0f, 0.32f},
+    {RING, 128, 128, 128, 512, 256, 4.30f, 0.492f, 0, 7.09f, 0.34f, 0.12f, 3.0f, 2.8f, 8.3f, 0.28f},
+    {WIDE, 128, 256, 128, 512, 256, 5.84f, 0.706f, 0, 8.68f, 0.70f, 0.28f, 3.6f, 3.0f, 8.0f, 0.32f},
     {WIDE, 192, 256, 128, 512, 256, 7.24f, 0.874f, 0, 6.91f, 0.41f, 0.41f, 5.4f, 2.9f, 8.2f, 0.31f},
-    {WIDE, 256, 256, 128, 512, 256, 8.99f, 1.040f, 0, 6.90f, 0.29f, 0.47f, 6.9f, 2.4f, 8.5f, 0.83f},
+    {WIDE, 256, 256, 128, 512, 256, 8.99f, 1.040f, 0, 6.90f, 0.29f, 0.46f, 6.9f, 2.4f, 8.5f, 0.83f},
 };
 constexpr int N_SHAPES = sizeof(SHAPES) / sizeof(SHAPES[0]);
 
@@ -703,17 +785,17 @@ size_t bytes_of(const Plan& c) {
     return c.splits > 1 ? (size_t)c.tail * c.splits * SHAPES[c.shape].bm * SHAPES[c.shape].bn * 4 : 0;
 }
 
+// Whether some row starts inside 128 bytes (asked without operands: packed rows).
+bool skewed(const GemmQ8Params& p) {
+    return ((p.W ? (uintptr_t)p.W | (uintptr_t)p.X | (uintptr_t)p.ldw | (uintptr_t)p.ldx : (uintptr_t)p.K) & 127) != 0;
+}
+
 // Weight rows a multiple of 4 KB apart have the same K on the same memory channels, so blocks
 // in step ask few of them at a time: where copies fetch 256 bytes of a row, columns of tiles
 // start at 16 places of K (cold weights: 7 x 36864 x 8192 65 -> 58 us, 24 x 16384 x 4096 18.1 ->
 // 16.2, 48 x 16384 x 8192 34.5 -> 29.3).  Copies of 128 bytes lose by it (69 -> 90 us in tiles of
 // 64 x 128), as do more tokens, whose rows would come from beyond the L2 several times.
-int phases_of(const GemmQ8Params& p, const Shape& c) { return c.kind == RING && c.bk == 256 && p.M <= 128 && p.ldw % 4096 == 0 ? 16 : 1; }
-
-// Whether some row starts inside 128 bytes (asked without operands: packed rows).
-bool skewed(const GemmQ8Params& p) {
-    return ((p.W ? (uintptr_t)p.W | (uintptr_t)p.X | (uintptr_t)p.ldw | (uintptr_t)p.ldx : (uintptr_t)p.K) & 127) != 0;
-}
+int phases_of(const GemmQ8Params& p, const Shape& c) { return c.kind == RING && c.bk == 256 && p.M <= 128 && p.ldw % 4096 == 0 && !skewed(p) ? 16 : 1; }
 
 // Predicted time of a launch: whole rounds of tiles, then what is left of them, then the
 // ranges of split tiles, each round as long as its K steps; beside it the weights, of the
@@ -795,9 +877,12 @@ void launch_tiles(F kernel, const GemmQ8Params& p, const Plan& c, hipStream_t s)
     if (sp.tail) PB_LAUNCH((q8_join_kernel<BM, BN>), sp.tail * (BM * BN / 4 / 256), 256, 0, s, p, sp);
 }
 
-template <int BM, int BN, int WGM, int WGN, int BK, int S>
+template <int BM, int BN, int WGM, int WGN, int BK, int S, int S_SKEW>
 void launch_ring(const GemmQ8Params& p, const Plan& c, hipStream_t s) {
-    launch_tiles<BM, BN>(q8_ring_kernel<BM, BN, WGM, WGN, BK, S>, p, c, s);
+    if constexpr (S_SKEW > 0) {
+        if (skewed(p)) return launch_tiles<BM, BN>(q8_ring_kernel<BM, BN, WGM, WGN, BK, S_SKEW, true>, p, c, s);
+    }
+    launch_tiles<BM, BN>(q8_ring_kernel<BM, BN, WGM, WGN, BK, S, false>, p, c, s);
 }
 
 template <int KW>
@@ -809,15 +894,18 @@ void launch_plan(const GemmQ8Params& p, const Plan& c, hipStream_t s) {
     switch (c.shape) {
         case 0: launch_few<4>(p, s); break;
         case 1: launch_few<8>(p, s); break;
-        case 2: launch_ring<32, 32, 1, 2, 256, 4>(p, c, s); break;
-        case 3: launch_ring<32, 64, 1, 4, 256, 4>(p, c, s); break;
-        case 4: launch_ring<64, 64, 1, 4, 256, 4>(p, c, s); break;
-        case 5: launch_ring<64, 128, 2, 4, 128, 4>(p, c, s); break;
-        case 6: launch_ring<128, 64, 2, 2, 256, 3>(p, c, s); break;
-        case 7: launch_ring<128, 128, 2, 4, 128, 4>(p, c, s); break;
-        case 8: launch_tiles<128, 256>(q8_wide_kernel<2>, p, c, s); break;
-        case 9: launch_tiles<192, 256>(q8_wide_kernel<3>, p, c, s); break;
-        case 10: launch_tiles<256, 256>(q8_wide_kernel<4>, p, c, s); break;
+        case 2: launch_ring<32, 32, 1, 2, 256, 4, 0>(p, c, s); break;
+        case 3: launch_ring<32, 64, 1, 4, 256, 4, 5>(p, c, s); break;
+        case 4: launch_ring<64, 64, 1, 4, 256, 4, 0>(p, c, s); break;
+        case 5: launch_ring<64, 128, 2, 4, 128, 4, 6>(p, c, s); break;
+        case 6: launch_ring<128, 64, 2, 2, 256, 3, 0>(p, c, s); break;
+        case 7: launch_ring<128, 128, 2, 4, 128, 4, 5>(p, c, s); break;
+        case 8:
+            if (skewed(p)) launch_tiles<128, 256>(q8_wide_kernel<2, true>, p, c, s);
+            else launch_tiles<128, 256>(q8_wide_kernel<2, false>, p, c, s);
+            break;
+        case 9: launch_tiles<192, 256>(q8_wide_kernel<3, false>, p, c, s); break;
+        case 10: launch_tiles<256, 256>(q8_wide_kernel<4, false>, p, c, s); break;
     }
 }
 

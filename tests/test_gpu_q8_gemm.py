@@ -101,9 +101,44 @@ KERNELS = [
     (556, 22808, 2224), (403, 8506, 6784), (198, 22556, 3872),
     (1, 754, 12032), (1, 918, 8320), (97, 19052, 12288), (639, 35, 1920), (1337, 86, 30288), (177, 16833, 3088), (1278, 1036, 12864),
     (392, 5836, 10880), (452, 5855, 7744), (1169, 13350, 2816), (500, 5888, 7744), (1169, 13312, 2816),
+    (88, 47, 8336), (1, 18285, 24624), (248, 8249, 6800), (111, 19495, 10272), (377, 11177, 2480), (2662, 6290, 2128),
+    (152, 5752, 10304), (528, 27648, 2768), (231, 10660, 12048),
     # weight rows a multiple of 4 KB apart: columns of tiles that start at other places of K
     (20, 1000, 4096), (40, 600, 8192), (64, 2100, 12288), (100, 5000, 4096), (128, 20000, 4096), (90, 520, 16384),
 ]
+
+
+# bytes / 16 before X's and W's first row and between their rows; lines are 8 of them
+OFF = [(0, 1, 0, 1), (1, 0, 0, 0), (0, 0, 7, 0), (3, 2, 5, 4), (7, 7, 1, 3), (4, 5, 2, 6), (2, 4, 6, 2), (5, 6, 3, 7)]
+
+
+@pytest.mark.parametrize("M,N,K", [(40, 700, 512), (50, 6144, 1280), (200, 640, 128), (200, 1000, 144), (150, 2000, 1664), (333, 1280, 5120),
+                                   (260, 8192, 4096), (500, 520, 256), (900, 2048, 1920), (1511, 4999, 400), (1100, 5000, 128),
+                                   (1500, 5000, 272), (1000, 1300, 9216)])
+@pytest.mark.parametrize("off", OFF, ids=str)
+def test_rows_off_lines(M, N, K, off):
+    """Rows that start anywhere in a line of 128 bytes: sums are exact, so every bit is that of packed rows."""
+    import torch
+
+    from paper_2503_17707_amd import binding as pb
+
+    log("gemm off lines", M, N, K, off)
+    g = torch.Generator("cuda").manual_seed(M + N + K)
+
+    def rows(n, before, between):
+        ld = (K + 127) // 128 * 128 + 16 * between
+        buf = torch.randint(-128, 128, (16 * before + n * ld,), generator=g, device="cuda").to(torch.int8)
+        return buf[16 * before:].view(n, ld)[:, :K]
+
+    X, W = rows(M, off[0], off[1]), rows(N, off[2], off[3])
+    sx = torch.rand(M, generator=g, device="cuda") + 0.5
+    sw = torch.rand(N, generator=g, device="cuda") + 0.5
+    n64 = (X.double() @ W.double().t()).float()  # exact sums, rounded once, as the kernels round them
+    want = n64 * sx[:, None] * sw[None]
+    for ws in (_ws(M, N, K), None):
+        R = torch.zeros(M, N, device="cuda")
+        pb.op_gemm_q8(1, 3, X, sx, W, sw, None, R=R, workspace=ws)
+        assert torch.equal(R, want)
 
 
 @pytest.mark.parametrize("M,N,K", KERNELS)
