@@ -14,6 +14,7 @@
 // copies that feed them; between, the copies alone (see the wide tiles).
 #include <cmath>
 #include <type_traits>
+#include <utility>
 
 #include "../csrc/common.h"
 #include "q8.h"
@@ -799,66 +800,79 @@ int phases_of(const GemmQ8Params& p, const Shape& c) { return c.kind == RING && 
 
 // Predicted time of a launch: whole rounds of tiles, then what is left of them, then the
 // ranges of split tiles, each round as long as its K steps; beside it the weights, of the
-// shorter one the share `both`.
-float time_of(const GemmQ8Params& p, const Plan& plan, int tiles, int whole) {
-    const Shape& c = SHAPES[plan.shape];
-    int kt = whole, splits = 1, tail = 0;
-    if (plan.splits > 1) {
-        kt = (whole + plan.splits - 1) / plan.splits;
+// shorter one the share `both`.  (Shapes as constants: a choice takes 0.04 to 0.23 us of a call,
+// 0.1 to 0.5 as data.)
+template <int I>
+float time_of(const GemmQ8Params& p, bool skew, int split, int tail, int tiles, int whole) {
+    constexpr Shape c = SHAPES[I];
+    int kt = whole, splits = 1;
+    if (split > 1) {
+        kt = (whole + split - 1) / split;
         splits = (whole + kt - 1) / kt;
-        tail = splits > 1 ? plan.tail : 0;
+        if (splits == 1) tail = 0;
     }
     const int rounds = (tiles - tail + c.slots - 1) / c.slots, cut = (tail * splits + c.slots - 1) / c.slots;
-    float work = (float)(rounds * whole + cut * kt) * c.step, weights = (float)p.N * (float)p.K * 1e-6f / c.tbs;
-    if (skewed(p)) work *= 1.f + c.skew;
+    float work = (float)(rounds * whole + cut * kt) * c.step, weights = (float)p.N * (float)p.K * (1e-6f / c.tbs);
+    if (skew) work *= 1.f + c.skew;
     work *= 1.f + c.token * (float)p.M;
     if (tail && kt * c.bk % 4096 == 0) weights *= 1.f + c.channels;
     float t = c.start + fmaxf(work, weights) + c.both * fminf(work, weights) + (float)(rounds + cut - 1) * c.round;
     if (p.K % c.bk) t += 0.6f;
     // (0.5: the join's launch where no graph replays it)
-    if (tail) t += c.join + 0.5f + (float)tail * (float)splits * (float)(c.bm * c.bn) * 8e-6f / c.join_tbs;
+    if constexpr (c.kind != FEW)
+        if (tail) t += c.join + 0.5f + (float)(tail * splits) * ((float)(c.bm * c.bn) * 8e-6f / c.join_tbs);
     return t;
 }
 
-Plan plan_of(const GemmQ8Params& p, size_t room) {
-    Plan best{-1, 1, 0};
-    float best_t = 0.f;
-    auto consider = [&](const Plan& c, int tiles, int whole) {
-        if (bytes_of(c) > room) return;
-        const float t = time_of(p, c, tiles, whole);
-        if (best.shape >= 0 && t >= best_t) return;
-        best = c;
-        best_t = t;
-    };
-    for (int i = 0; i < N_SHAPES; ++i) {
-        const Shape& c = SHAPES[i];
-        if (c.kind == FEW) {
-            // measured side by side: 4 waves from 12288 features on, where blocks are many
-            if (p.M <= 16 && (c.threads == 256) == (p.N >= 12288)) consider({i, 1, 0}, tiles_of(p, c), p.K / c.bk);
-            continue;
-        }
-        if (c.kind == WIDE ? p.M <= 64 || p.K < 128 : c.bm == 32 ? p.M > 64 : c.bm == 64 ? p.M > 512 : p.M <= 32) continue;
-        const int tiles = tiles_of(p, c), whole = p.K / c.bk;
-        consider({i, 1, 0}, tiles, whole);
-        // the splits that come next to filling the chip: of all tiles, or of a last round's
-        int tried = 0;
-        if (tiles < c.slots) {
-            for (const int s : {16, 12, 8, 6, 5, 4, 3, 2})
-                if (tried < 3 && s * tiles <= c.slots && whole >= 2 * s) {
-                    consider({i, s, tiles}, tiles, whole);
-                    ++tried;
-                }
-            if (!tried && whole >= 4) consider({i, 2, tiles}, tiles, whole);
-        } else if (const int tail = tiles % 256) {
-            for (const int s : {8, 6, 5, 4, 3, 2})
-                if (tried < 2 && s * tail <= 256 && whole >= 2 * s) {
-                    consider({i, s, tail}, tiles, whole);
-                    ++tried;
-                }
-        }
+struct Choice {
+    Plan plan;
+    float t;
+};
+
+template <int I>
+void consider(const GemmQ8Params& p, bool skew, size_t room, Choice& best) {
+    constexpr Shape c = SHAPES[I];
+    // 4 waves for few tokens from 12288 features on, where blocks are many (measured side by side)
+    if constexpr (c.kind == FEW) {
+        if (p.M > 16 || (c.threads == 256) != (p.N >= 12288)) return;
+    } else {
+        if (c.kind == WIDE ? p.M <= 64 || p.K < 128 : c.bm == 32 ? p.M > 64 : c.bm == 64 ? p.M > 512 : p.M <= 32) return;
     }
-    return best;
+    const int tiles = tiles_of(p, c), whole = p.K / c.bk;
+    auto take = [&](int split, int tail) {
+        if (split > 1 && bytes_of({I, split, tail}) > room) return;
+        const float t = time_of<I>(p, skew, split, tail, tiles, whole);
+        if (best.plan.shape < 0 || t < best.t) best = {{I, split, tail}, t};
+    };
+    take(1, 0);
+    if (c.kind == FEW) return;
+    // the splits that come next to filling the chip: of all tiles, or of a last round's
+    int tried = 0;
+    if (tiles < c.slots) {
+        for (const int s : {16, 12, 8, 6, 5, 4, 3, 2})
+            if (tried < 3 && s * tiles <= c.slots && whole >= 2 * s) {
+                take(s, tiles);
+                ++tried;
+            }
+        if (!tried && whole >= 4) take(2, tiles);
+    } else if (const int tail = tiles % 256) {
+        for (const int s : {8, 6, 5, 4, 3, 2})
+            if (tried < 2 && s * tail <= 256 && whole >= 2 * s) {
+                take(s, tail);
+                ++tried;
+            }
+    }
 }
+
+template <int... I>
+Plan best_of(const GemmQ8Params& p, size_t room, std::integer_sequence<int, I...>) {
+    Choice best{{-1, 1, 0}, 0.f};
+    const bool skew = skewed(p);
+    (consider<I>(p, skew, room, best), ...);
+    return best.plan;
+}
+
+Plan plan_of(const GemmQ8Params& p, size_t room) { return best_of(p, room, std::make_integer_sequence<int, N_SHAPES>()); }
 
 template <int BM, int BN, typename F>
 void launch_tiles(F kernel, const GemmQ8Params& p, const Plan& c, hipStream_t s) {
