@@ -919,27 +919,37 @@ def op_page_fork(dtype: int, pools, parents, tables, lens, refs, grow, out_table
 # ---- linear layers in 8 bits ------------------------------------------------------
 # 8-bit rows are int8 [rows, cols] with contiguous rows; their scales float32 [rows].
 #
-# A call of one token waits for its host work: each wrapper below asks one condition over
-# plain attributes, and only a call that fails it goes through the checks that find and
-# name what is wrong (a product of one token called in a row: 6.7 us, 9.8 with those checks
-# before every call).
+# A call of one token waits for its host work.  The conditions on its tensors are asked by a
+# small extension module (q8/py_q8.cpp), which hands them to the C entry point; a call that does
+# not meet them goes through the checks below, which find and name what is wrong.
 
+ARGS_PATH = os.path.join(HERE, "lib", "pipeboost_q8_args.so")
 _q8 = None
 
 
 def _q8_ready():
-    """(types of dtype 0 and 1, int8, float32, current device, its current stream)"""
+    """The extension module, with the loaded library's entry points."""
     global _q8, _torch
+    L = lib()
+    import importlib.machinery
+    import importlib.util
+
     import torch
 
+    if not os.path.exists(ARGS_PATH):
+        raise RuntimeError("pipeboost_q8_args.so is not built (%s); run __graft_entry__.build()" % ARGS_PATH)
+    loader = importlib.machinery.ExtensionFileLoader("pipeboost_q8_args", ARGS_PATH)
+    m = importlib.util.module_from_spec(importlib.util.spec_from_loader("pipeboost_q8_args", loader))
+    loader.exec_module(m)
+    m.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.pb_op_norm_q8, L.pb_op_quant_q8, L.pb_op_gemm_q8)))
     _torch = torch
     torch.cuda.is_available() and torch.cuda.current_stream()  # initialises the runtime
-    dev = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    if raw is None:
-        raw = lambda d: torch.cuda.current_stream(d).cuda_stream  # noqa: E731
-    _q8 = ((torch.bfloat16, torch.float16), torch.int8, torch.float32, dev, raw)
-    return _q8
+    _q8 = m
+    return m
+
+
+def _kinds(dtype):
+    return (_torch.bfloat16, _torch.float16)[dtype]
 
 
 def _refuse(op, why, *args):
@@ -947,12 +957,13 @@ def _refuse(op, why, *args):
 
 
 def _rows_wrong(op, name, t, dtypes, shape):
-    if t.dtype not in dtypes or tuple(t.shape) != tuple(shape) or (t.stride(1) != 1 and shape[1] > 1):
+    if (t.layout is not _torch.strided or t.dtype not in dtypes or tuple(t.shape) != tuple(shape)
+            or (t.stride(1) != 1 and shape[1] > 1)):
         _refuse(op, "%s must be %s %s with contiguous rows", name, " or ".join(str(d) for d in dtypes), list(shape))
 
 
 def _vector_wrong(op, name, t, dtype, n):
-    if t.dtype is not dtype or tuple(t.shape) != (n,) or not t.is_contiguous():
+    if t.layout is not _torch.strided or t.dtype is not dtype or tuple(t.shape) != (n,) or not t.is_contiguous():
         _refuse(op, "%s must be contiguous %s [%d]", name, dtype, n)
 
 
@@ -965,18 +976,20 @@ def _device_wrong(op, tensors, stream):
         _refuse(op, "tensors on %s, which is not the current device", first.device)
     if stream is not None and stream.device_index != first.get_device():
         _refuse(op, "the stream is another device's")
-    raise AssertionError("%s: arguments that no check names" % op)
+    _refuse(op, "a size past 32 bits, or a tensor that is no plain memory")
 
 
-def _norm_q8_wrong(dtype, x, g, q, scale, delta, sum, b, out, stream):
+def _norm_q8_failed(rc, dtype, x, g, q, scale, delta, sum, b, out, stream):
+    if rc != _q8.LOOK:
+        check(rc)
     op = "op_norm_q8"
-    kinds, i8, f32, _, _ = _q8
+    i8, f32 = _torch.int8, _torch.float32
     if dtype not in (0, 1):
         _refuse(op, "bad dtype %s", dtype)
     if x.dim() != 2:
         _refuse(op, "x must be [rows, d]")
     rows, d = of = x.shape
-    kind = kinds[dtype]
+    kind = _kinds(dtype)
     _rows_wrong(op, "x", x, (f32, kind), of)
     if (q is None) != (scale is None):
         _refuse(op, "q and scale go together")
@@ -996,57 +1009,22 @@ def op_norm_q8(dtype: int, x, g, q=None, scale=None, delta=None, sum=None, b=Non
     """pb_op_norm_q8: x [rows, d] float32 or dtype's type; delta (dtype's type) is added and the sum stored in `sum`
     (x's type; may be x); its RMS norm (layer: layer norm) with gain g and bias b [d] goes to q int8 [rows, d] with
     scale float32 [rows], and to out (dtype's type) where given.  Rows may be strided."""
-    kinds, i8, f32, device, raw = _q8 or _q8_ready()
-    of = x.shape
-    dev = x.get_device()
-    ok = dtype in (0, 1) and len(of) == 2 and dev >= 0 and dev == device() and (q is None) == (scale is None)
-    if ok:
-        rows, d = of
-        kind, xt = kinds[dtype], x.dtype
-        # (a row of one element may have any stride inside)
-        one = d == 1
-        ld_x, e = x.stride()
-        ok = ((xt is f32 or xt is kind) and (e == 1 or one) and g.dtype is kind and g.shape == (d,) and g.is_contiguous()
-              and g.get_device() == dev and (stream is None or stream.device_index == dev))
-        ld_delta = ld_sum = ld_out = ld_q = 0
-        p_delta = p_sum = p_out = p_q = p_scale = p_b = None
-        if delta is not None and ok:
-            ld_delta, e = delta.stride() if delta.shape == of else (0, None)
-            ok = delta.dtype is kind and (e == 1 or one and e is not None) and delta.get_device() == dev
-            p_delta = delta.data_ptr()
-        if sum is not None and ok:
-            ld_sum, e = sum.stride() if sum.shape == of else (0, None)
-            ok = sum.dtype is xt and (e == 1 or one and e is not None) and sum.get_device() == dev
-            p_sum = sum.data_ptr()
-        if q is not None and ok:
-            ld_q, e = q.stride() if q.shape == of else (0, None)
-            ok = (q.dtype is i8 and (e == 1 or one and e is not None) and q.get_device() == dev and scale.dtype is f32
-                  and scale.shape == (rows,) and scale.is_contiguous() and scale.get_device() == dev)
-            p_q, p_scale = q.data_ptr(), scale.data_ptr()
-        if out is not None and ok:
-            ld_out, e = out.stride() if out.shape == of else (0, None)
-            ok = out.dtype is kind and (e == 1 or one and e is not None) and out.get_device() == dev
-            p_out = out.data_ptr()
-        if b is not None and ok:
-            ok = b.dtype is kind and b.shape == (d,) and b.is_contiguous() and b.get_device() == dev
-            p_b = b.data_ptr()
-    if not ok:
-        _norm_q8_wrong(dtype, x, g, q, scale, delta, sum, b, out, stream)
-    rc = lib().pb_op_norm_q8(dtype, layer, x.data_ptr(), ld_x, xt is f32, p_delta, ld_delta, p_sum, ld_sum, g.data_ptr(),
-                             p_b, eps, p_out, ld_out, p_q, ld_q, p_scale, rows, d,
-                             raw(dev) if stream is None else stream.cuda_stream)
+    rc = (_q8 or _q8_ready()).norm(dtype, layer, x, g, q, scale, delta, sum, b, out, eps, -1 if stream is None else stream.device_index,
+                                   0 if stream is None else stream.cuda_stream)
     if rc:
+        _norm_q8_failed(rc, dtype, x, g, q, scale, delta, sum, b, out, stream)
+
+
+def _quant_q8_failed(rc, dtype, x, q, scale, stream):
+    if rc != _q8.LOOK:
         check(rc)
-
-
-def _quant_q8_wrong(dtype, x, q, scale, stream):
     op = "op_quant_q8"
-    kinds, i8, f32, _, _ = _q8
+    i8, f32 = _torch.int8, _torch.float32
     if dtype not in (0, 1):
         _refuse(op, "bad dtype %s", dtype)
     if x.dim() != 2:
         _refuse(op, "x must be [rows, cols]")
-    _rows_wrong(op, "x", x, (f32, kinds[dtype]), x.shape)
+    _rows_wrong(op, "x", x, (f32, _kinds(dtype)), x.shape)
     _rows_wrong(op, "q", q, (i8,), x.shape)
     _vector_wrong(op, "scale", scale, f32, x.shape[0])
     _device_wrong(op, [x, q, scale], stream)
@@ -1054,23 +1032,10 @@ def _quant_q8_wrong(dtype, x, q, scale, stream):
 
 def op_quant_q8(dtype: int, x, q, scale, stream=None):
     """pb_op_quant_q8: x [rows, cols] (float32 or dtype's type) to q int8 [rows, cols] and scale float32 [rows]."""
-    kinds, i8, f32, device, raw = _q8 or _q8_ready()
-    of = x.shape
-    dev = x.get_device()
-    ok = dtype in (0, 1) and len(of) == 2 and q.shape == of and dev >= 0 and dev == device()
-    if ok:
-        rows, cols = of
-        xt = x.dtype
-        (ld_x, ex), (ld_q, eq) = x.stride(), q.stride()
-        ok = ((xt is f32 or xt is kinds[dtype]) and (ex == eq == 1 or cols == 1) and q.dtype is i8 and scale.dtype is f32
-              and scale.shape == (rows,) and scale.is_contiguous() and q.get_device() == dev
-              and scale.get_device() == dev and (stream is None or stream.device_index == dev))
-    if not ok:
-        _quant_q8_wrong(dtype, x, q, scale, stream)
-    rc = lib().pb_op_quant_q8(dtype, x.data_ptr(), ld_x, xt is f32, q.data_ptr(), ld_q, scale.data_ptr(), rows, cols,
-                              raw(dev) if stream is None else stream.cuda_stream)
+    rc = (_q8 or _q8_ready()).quant(dtype, x, q, scale, -1 if stream is None else stream.device_index,
+                                    0 if stream is None else stream.cuda_stream)
     if rc:
-        check(rc)
+        _quant_q8_failed(rc, dtype, x, q, scale, stream)
 
 
 def gemm_q8_workspace(M: int, N: int, K: int) -> int:
@@ -1078,9 +1043,11 @@ def gemm_q8_workspace(M: int, N: int, K: int) -> int:
     return lib().pb_op_gemm_q8_workspace(M, N, K)
 
 
-def _gemm_q8_wrong(dtype, epi, X, sx, W, sw, bias, out, workspace, stream):
+def _gemm_q8_failed(rc, dtype, epi, X, sx, W, sw, bias, out, workspace, stream):
+    if rc != _q8.LOOK:
+        check(rc)
     op = "op_gemm_q8"
-    kinds, i8, f32, _, _ = _q8
+    i8, f32 = _torch.int8, _torch.float32
     if dtype not in (0, 1) or epi not in (0, 1, 2, 3):
         _refuse(op, "bad dtype %s or epilogue %s", dtype, epi)
     if X.dim() != 2 or W.dim() != 2:
@@ -1091,10 +1058,10 @@ def _gemm_q8_wrong(dtype, epi, X, sx, W, sw, bias, out, workspace, stream):
     _vector_wrong(op, "sx", sx, f32, M)
     _vector_wrong(op, "sw", sw, f32, N)
     if bias is not None:
-        _vector_wrong(op, "bias", bias, kinds[dtype], N)
+        _vector_wrong(op, "bias", bias, _kinds(dtype), N)
     if out is None:
         _refuse(op, "epilogues 0 and 1 write C, 2 and 3 R")
-    _rows_wrong(op, "R" if epi >= 2 else "C", out, (f32 if epi >= 2 else kinds[dtype],), (M, N))
+    _rows_wrong(op, "R" if epi >= 2 else "C", out, (f32 if epi >= 2 else _kinds(dtype),), (M, N))
     if workspace is not None and not workspace.is_contiguous():
         _refuse(op, "a workspace must be contiguous")
     _device_wrong(op, [X, sx, W, sw, bias, out, workspace], stream)
@@ -1104,35 +1071,7 @@ def op_gemm_q8(dtype: int, epi: int, X, sx, W, sw, bias=None, C=None, R=None, qs
                workspace=None, stream=None):
     """pb_op_gemm_q8: X int8 [M, K] with sx [M], W int8 [N, K] with sw [N], bias [N] of dtype's type or None; epilogues 0
     and 1 write C [M, N] (dtype's type), 2 adds to R [M, N] (float32), 3 writes it.  Rows may be strided."""
-    kinds, i8, f32, device, raw = _q8 or _q8_ready()
-    wide = epi >= 2
-    out = R if wide else C
-    xs, ws = X.shape, W.shape
-    dev = X.get_device()
-    ok = dtype in (0, 1) and 0 <= epi <= 3 and len(xs) == len(ws) == 2 and out is not None and dev >= 0 and dev == device()
-    if ok:
-        (M, K), (N, K_w) = xs, ws
-        (ldx, ex), (ldw, ew) = X.stride(), W.stride()
-        ldo, eo = out.stride() if out.shape == (M, N) else (0, None)
-        ok = (K_w == K and X.dtype is i8 and W.dtype is i8 and (ex == ew == 1 or K == 1) and (eo == 1 or N == 1 and eo is not None)
-              and out.dtype is (f32 if wide else kinds[dtype])
-              and sx.dtype is f32 and sx.shape == (M,) and sx.is_contiguous()
-              and sw.dtype is f32 and sw.shape == (N,) and sw.is_contiguous()
-              and W.get_device() == dev and sx.get_device() == dev and sw.get_device() == dev
-              and out.get_device() == dev and (stream is None or stream.device_index == dev))
-        p_bias = p_ws = None
-        n_ws = 0
-        if bias is not None and ok:
-            ok = bias.dtype is kinds[dtype] and bias.shape == (N,) and bias.is_contiguous() and bias.get_device() == dev
-            p_bias = bias.data_ptr()
-        if workspace is not None and ok:
-            ok = workspace.is_contiguous() and workspace.get_device() == dev
-            p_ws, n_ws = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    if not ok:
-        _gemm_q8_wrong(dtype, epi, X, sx, W, sw, bias, out, workspace, stream)
-    p_out = out.data_ptr()
-    rc = lib().pb_op_gemm_q8(dtype, epi, X.data_ptr(), ldx, sx.data_ptr(), W.data_ptr(), ldw, sw.data_ptr(), p_bias, p_out,
-                             p_out, ldo, M, N, K, qscale, qcols, p_ws, n_ws,
-                             raw(dev) if stream is None else stream.cuda_stream)
+    rc = (_q8 or _q8_ready()).gemm(dtype, epi, X, sx, W, sw, bias, C, R, qscale, qcols, workspace,
+                                   -1 if stream is None else stream.device_index, 0 if stream is None else stream.cuda_stream)
     if rc:
-        check(rc)
+        _gemm_q8_failed(rc, dtype, epi, X, sx, W, sw, bias, R if epi >= 2 else C, workspace, stream)

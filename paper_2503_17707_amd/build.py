@@ -22,6 +22,7 @@ LIB = os.path.join(OUT_DIR, "libpipeboost.so")
 SOURCES = ["gemm.hip", "attention.hip", "misc.hip", "lmhead.hip", "model.cpp", "sched.cpp"]
 PAGED_SOURCES = ["paged_attention.hip", "paged_cache.hip", "beam.hip", "paged_ops.cpp"]
 Q8_SOURCES = ["gemm_q8.hip", "rows_q8.hip", "q8_ops.cpp"]
+ARGS = os.path.join(OUT_DIR, "pipeboost_q8_args.so")
 ARCH = os.environ.get("PB_OFFLOAD_ARCH", "gfx950")
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=" + ARCH, "-Wall", "-Wno-unused-result",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -43,6 +44,26 @@ def _compile(src: str, obj_dir: str, defines=()) -> str:
     return obj
 
 
+def build_args() -> str:
+    """The extension module that looks over the 8-bit operators' tensors (host code, torch's headers)."""
+    import sysconfig
+
+    import torch
+    from torch.utils.cpp_extension import ROCM_HOME, include_paths, library_paths
+
+    os.makedirs(OUT_DIR, exist_ok=True)
+    tmp = ARGS + ".tmp%d" % os.getpid()
+    cmd = (["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall", "-D__HIP_PLATFORM_AMD__=1",
+            "-DUSE_ROCM=1", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI, os.path.join(Q8, "py_q8.cpp"), "-o", tmp]
+           + ["-isystem" + d for d in include_paths() + [sysconfig.get_paths()["include"], os.path.join(ROCM_HOME or "/opt/rocm", "include")]]
+           + ["-L" + d for d in library_paths()] + ["-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"])
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("compile of py_q8.cpp failed:\n%s\n%s" % (" ".join(cmd), r.stderr))
+    os.replace(tmp, ARGS)
+    return ARGS
+
+
 def build(verbose: bool = False, out: str = LIB, defines=()) -> str:
     """Compile and link; `out` and `defines` (NAME=VALUE) select a variant build."""
     tag = hashlib.md5(repr((out, tuple(defines))).encode()).hexdigest()[:10]
@@ -51,7 +72,10 @@ def build(verbose: bool = False, out: str = LIB, defines=()) -> str:
     os.makedirs(os.path.dirname(out), exist_ok=True)
     sources = SOURCES + PAGED_SOURCES + Q8_SOURCES
     with cf.ThreadPoolExecutor(max_workers=min(8, len(sources))) as ex:
+        args = ex.submit(build_args) if out == LIB else None
         objs = list(ex.map(lambda s: _compile(s, obj_dir, defines), sources))
+        if args:
+            args.result()
     tmp = out + ".tmp%d" % os.getpid()
     cmd = ["hipcc", "-shared", "-fPIC", "--offload-arch=" + ARCH, "-o", tmp] + objs
     r = subprocess.run(cmd, capture_output=True, text=True)

@@ -128,6 +128,16 @@ def test_wrappers_refuse_what_the_library_cannot_see():
     refused(pb.op_norm_q8, 1, x, g, q, s, delta=h, sum=h)
     refused(pb.op_quant_q8, 1, h, q, s)
     refused(pb.op_quant_q8, 0, h, q, s)
+    refused(pb.op_quant_q8, 2, h, q, s)
+    refused(pb.op_quant_q8, 1, h.to_sparse(), q, s)
+    refused(pb.op_quant_q8, 1, h, q, s.to_sparse())
+    for bad in (("f16", h, q, s), (None, h, q, s), (1.5, h, q, s)):
+        with pytest.raises(TypeError):
+            pb.op_quant_q8(*bad)
+    with pytest.raises(TypeError):
+        pb.op_norm_q8(1, h, g, q, s, eps="small")
+    with pytest.raises(TypeError):
+        pb.op_gemm_q8(1, 2, q, s, q, s, R=torch.zeros(3, 3), qcols=None)
     refused(pb.op_quant_q8, 1, h, q[:, :32], s)
     refused(pb.op_quant_q8, 1, h, q, s[:2])
     refused(pb.op_gemm_q8, 1, 0, q, s, q, s, C=torch.zeros(3, 3, dtype=torch.float16))
