@@ -891,6 +891,7 @@ void launch_tiles(F kernel, const GemmQ8Params& p, const Plan& c, hipStream_t s)
     if (sp.tail) PB_LAUNCH((q8_join_kernel<BM, BN>), sp.tail * (BM * BN / 4 / 256), 256, 0, s, p, sp);
 }
 
+// S_SKEW: stages for rows off 128 bytes (0: the same kernel, which lost little by them).
 template <int BM, int BN, int WGM, int WGN, int BK, int S, int S_SKEW>
 void launch_ring(const GemmQ8Params& p, const Plan& c, hipStream_t s) {
     if constexpr (S_SKEW > 0) {
