@@ -247,10 +247,12 @@ int pb_op_quant_q8(int32_t dtype, const void* x, int64_t ld_x, int32_t x_f32, in
  * 8-bit integers; both 16-byte aligned, row strides multiples of 16 up to 2^23 (of 128:
  * up to a third faster).
  * K is a multiple of 16, at most 131056; any M and N up to 2^24 whose tiles of 64 x 64
- * stay below 2^23.  workspace (may be NULL): partial sums where K is split, up to
- * pb_op_gemm_q8_workspace bytes (0 for refused sizes); results do not depend on it.
- * It carries nothing from one call to the next; calls that may run at the same time
- * (on two streams, in two graphs) need one each. */
+ * stay below 2^23.  workspace (may be NULL): partial sums where K is split.
+ * pb_op_gemm_q8_workspace bytes hold those of every call of up to M tokens on rows of any
+ * stride (at most 64 MiB; 0 for refused sizes and where K is never split); with fewer the
+ * call splits less and may take longer.  Results do not depend on it.  It carries nothing
+ * from one call to the next; calls that may run at the same time (on two streams, in two
+ * graphs) need one each. */
 int pb_op_gemm_q8(int32_t dtype, int32_t epi, const int8_t* X, int64_t ldx, const float* sx, const int8_t* W,
                   int64_t ldw, const float* sw, const void* bias, void* C, float* R, int64_t ldo, int32_t M,
                   int32_t N, int32_t K, float qscale, int32_t qcols, void* workspace, size_t workspace_bytes,

@@ -1039,7 +1039,7 @@ def op_quant_q8(dtype: int, x, q, scale, stream=None):
 
 
 def gemm_q8_workspace(M: int, N: int, K: int) -> int:
-    """Bytes of workspace with which op_gemm_q8 splits K as it likes."""
+    """Bytes of workspace with which op_gemm_q8 splits K as it likes, for up to M tokens and rows of any stride."""
     return lib().pb_op_gemm_q8_workspace(M, N, K)
 
 

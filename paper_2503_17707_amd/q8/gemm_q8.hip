@@ -781,8 +781,8 @@ bool gemm_q8_fits(int M, int N) {
 
 size_t gemm_q8_workspace(int M, int N, int K) {
     GemmQ8Params p{};
-    p.M = M; p.N = N; p.K = K; p.ldx = p.ldw = K;
-    return bytes_of(plan_of(p, (size_t)1 << 60));
+    p.M = M; p.N = N; p.K = K;
+    return workspace_of(p);
 }
 
 hipError_t launch_gemm_q8(const GemmQ8Params& p, hipStream_t s) {

@@ -62,10 +62,18 @@ inline size_t bytes_of(const Plan& c) {
     return c.splits > 1 ? (size_t)c.tail * c.splits * SHAPES[c.shape].bm * SHAPES[c.shape].bn * 4 : 0;
 }
 
-// Whether some row starts inside 128 bytes (asked without operands: packed rows).
+// Whether some row starts inside 128 bytes.
 inline bool skewed(const GemmQ8Params& p) {
-    return ((p.W ? (uintptr_t)p.W | (uintptr_t)p.X | (uintptr_t)p.ldw | (uintptr_t)p.ldx : (uintptr_t)p.K) & 127) != 0;
+    return (((uintptr_t)p.W | (uintptr_t)p.X | (uintptr_t)p.ldw | (uintptr_t)p.ldx) & 127) != 0;
 }
+
+// The numbers of tokens that a kernel is considered for (tall tiles of few tokens would be idle).
+constexpr int fewest_tokens(const Shape& c) { return c.kind == WIDE ? 65 : c.kind == RING && c.bm == 128 ? 33 : 1; }
+constexpr int most_tokens(const Shape& c) { return c.kind == FEW ? 16 : c.bm == 32 ? 64 : c.bm == 64 ? 512 : 1 << 24; }
+
+// Ranges of K that tiles are cut into, if a range has two steps and the ranges fit the chip at once:
+// of all tiles (fewer than slots), or of a last round's (256 blocks).
+constexpr int ALL_SPLITS[] = {16, 12, 8, 6, 5, 4, 3, 2}, TAIL_SPLITS[] = {8, 6, 5, 4, 3, 2};
 
 // Weight rows a multiple of 4 KB apart have the same K on the same memory channels, so blocks
 // in step ask few of them at a time: where copies fetch 256 bytes of a row, columns of tiles
@@ -109,11 +117,8 @@ template <int I>
 void consider(const GemmQ8Params& p, bool skew, size_t room, Choice& best) {
     constexpr Shape c = SHAPES[I];
     // 4 waves for few tokens from 12288 features on, where blocks are many (measured side by side)
-    if constexpr (c.kind == FEW) {
-        if (p.M > 16 || (c.threads == 256) != (p.N >= 12288)) return;
-    } else {
-        if (c.kind == WIDE ? p.M <= 64 || p.K < 128 : c.bm == 32 ? p.M > 64 : c.bm == 64 ? p.M > 512 : p.M <= 32) return;
-    }
+    if (p.M < fewest_tokens(c) || p.M > most_tokens(c) || (c.kind == WIDE && p.K < 128)) return;
+    if (c.kind == FEW && (c.threads == 256) != (p.N >= 12288)) return;
     const int tiles = tiles_of(p, c), whole = p.K / c.bk;
     auto take = [&](int split, int tail) {
         if (split > 1 && bytes_of({I, split, tail}) > room) return;
@@ -125,14 +130,13 @@ void consider(const GemmQ8Params& p, bool skew, size_t room, Choice& best) {
     // the splits that come next to filling the chip: of all tiles, or of a last round's
     int tried = 0;
     if (tiles < c.slots) {
-        for (const int s : {16, 12, 8, 6, 5, 4, 3, 2})
+        for (const int s : ALL_SPLITS)
             if (tried < 3 && s * tiles <= c.slots && whole >= 2 * s) {
                 take(s, tiles);
                 ++tried;
             }
-        if (!tried && whole >= 4) take(2, tiles);
     } else if (const int tail = tiles % 256) {
-        for (const int s : {8, 6, 5, 4, 3, 2})
+        for (const int s : TAIL_SPLITS)
             if (tried < 2 && s * tail <= 256 && whole >= 2 * s) {
                 take(s, tail);
                 ++tried;
@@ -164,6 +168,25 @@ inline Split split_of(const GemmQ8Params& p, const Plan& c) {
         }
     }
     return sp;
+}
+
+// Bytes that hold the sums of every plan for up to p.M tokens, whatever the rows' strides: a
+// kernel's ranges are at most the largest split's of all its tiles, and at most its slots.
+inline size_t workspace_of(const GemmQ8Params& p) {
+    size_t most = 0;
+    for (const Shape& c : SHAPES) {
+        if (c.kind == FEW || p.M < fewest_tokens(c) || (c.kind == WIDE && p.K < 128)) continue;
+        GemmQ8Params q = p;
+        q.M = p.M < most_tokens(c) ? p.M : most_tokens(c);
+        for (const int s : ALL_SPLITS) {
+            if (p.K / c.bk < 2 * s) continue;
+            const int64_t ranges = (int64_t)tiles_of(q, c) * s;
+            const size_t bytes = (size_t)(ranges < c.slots ? ranges : c.slots) * c.bm * c.bn * 4;
+            most = bytes > most ? bytes : most;
+            break;
+        }
+    }
+    return most;
 }
 
 }  // namespace pb::q8

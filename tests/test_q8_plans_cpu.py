@@ -57,3 +57,25 @@ def test_ranges_hold_every_step_of_a_launch_once(exe):
     few = np.array([k[0].startswith("few") for k in P.KERNELS])[shape]
     assert (M <= 16)[few].all() and not cut[few].any()
     assert (K >= 128)[shape >= 8].all()  # two stages of their ring are filled without asking
+
+
+def test_a_workspace_for_the_most_tokens_serves_fewer(exe):
+    """pb_op_gemm_q8_workspace(M, N, K) holds the sums of every call of up to M tokens, on rows of any stride."""
+    import numpy as np
+    import q8_plans as P
+
+    from paper_2503_17707_amd import binding as pb
+
+    rows = P.sample(9, 60_000)
+    rows = np.concatenate([rows, [(m, n, k, k, k, 1 << 30, (1 << 30) + 16, 0) for n, k in ((5120, 5120), (2048, 8192), (4096, 16384))
+                                  for m in range(1, 2049)]])  # weights off lines
+    rng = np.random.default_rng(1)
+    most = np.where(rng.integers(0, 2, len(rows)) == 0, rows[:, 0], rows[:, 0] + rng.integers(0, 4096, len(rows)))
+    asked = np.array([pb.gemm_q8_workspace(int(m), int(r[1]), int(r[2])) for m, r in zip(most, rows)])
+    assert (asked >= 0).all() and (asked <= P.ASKED).all() and not (asked % 16).any()
+    rows[:, 7] = 1 << 40
+    free = P.plans(exe, rows)
+    over = (free[:, 7] > asked).nonzero()[0]
+    assert not len(over), (len(over), rows[over[:3]].tolist(), most[over[:3]], asked[over[:3]], free[over[:3]].tolist())
+    rows[:, 7] = asked
+    assert (P.plans(exe, rows) == free).all()
