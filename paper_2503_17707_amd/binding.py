@@ -941,6 +941,8 @@ def _q8_ready():
     loader = importlib.machinery.ExtensionFileLoader("pipeboost_q8_args", ARGS_PATH)
     m = importlib.util.module_from_spec(importlib.util.spec_from_loader("pipeboost_q8_args", loader))
     loader.exec_module(m)
+    if getattr(m, "TORCH", None) != str(torch.__version__):  # tensors are read by that version's headers
+        raise RuntimeError("pipeboost_q8_args.so is for torch %s, not %s; run __graft_entry__.build()" % (getattr(m, "TORCH", "?"), torch.__version__))
     m.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.pb_op_norm_q8, L.pb_op_quant_q8, L.pb_op_gemm_q8)))
     _torch = torch
     torch.cuda.is_available() and torch.cuda.current_stream()  # initialises the runtime

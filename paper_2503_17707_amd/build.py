@@ -54,7 +54,8 @@ def build_args() -> str:
     os.makedirs(OUT_DIR, exist_ok=True)
     tmp = ARGS + ".tmp%d" % os.getpid()
     cmd = (["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall", "-D__HIP_PLATFORM_AMD__=1",
-            "-DUSE_ROCM=1", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI, os.path.join(Q8, "py_q8.cpp"), "-o", tmp]
+            "-DUSE_ROCM=1", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+            '-DPB_TORCH="%s"' % torch.__version__, os.path.join(Q8, "py_q8.cpp"), "-o", tmp]
            + ["-isystem" + d for d in include_paths() + [sysconfig.get_paths()["include"], os.path.join(ROCM_HOME or "/opt/rocm", "include")]]
            + ["-L" + d for d in library_paths()] + ["-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"])
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -62,6 +63,16 @@ def build_args() -> str:
         raise RuntimeError("compile of py_q8.cpp failed:\n%s\n%s" % (" ".join(cmd), r.stderr))
     os.replace(tmp, ARGS)
     return ARGS
+
+
+def _try_args():
+    """build_args where it can be built: the library does without it, and programs of the C ABI without torch."""
+    try:
+        build_args()
+    except Exception as e:
+        if os.path.exists(ARGS):
+            os.remove(ARGS)  # an older one would be called with newer arguments
+        sys.stderr.write("%s was not built (the 8-bit operators' Python wrappers need it): %s\n" % (os.path.basename(ARGS), e))
 
 
 def build(verbose: bool = False, out: str = LIB, defines=()) -> str:
@@ -72,10 +83,9 @@ def build(verbose: bool = False, out: str = LIB, defines=()) -> str:
     os.makedirs(os.path.dirname(out), exist_ok=True)
     sources = SOURCES + PAGED_SOURCES + Q8_SOURCES
     with cf.ThreadPoolExecutor(max_workers=min(8, len(sources))) as ex:
-        args = ex.submit(build_args) if out == LIB else None
+        if out == LIB:
+            ex.submit(_try_args)
         objs = list(ex.map(lambda s: _compile(s, obj_dir, defines), sources))
-        if args:
-            args.result()
     tmp = out + ".tmp%d" % os.getpid()
     cmd = ["hipcc", "-shared", "-fPIC", "--offload-arch=" + ARCH, "-o", tmp] + objs
     r = subprocess.run(cmd, capture_output=True, text=True)

@@ -202,6 +202,9 @@ PyModuleDef MODULE = {PyModuleDef_HEAD_INIT, "pipeboost_q8_args", nullptr, -1, M
 
 PyMODINIT_FUNC PyInit_pipeboost_q8_args() {
     PyObject* m = PyModule_Create(&MODULE);
-    if (m) PyModule_AddIntConstant(m, "LOOK", LOOK);
+    if (m && (PyModule_AddIntConstant(m, "LOOK", LOOK) < 0 || PyModule_AddStringConstant(m, "TORCH", PB_TORCH) < 0)) {
+        Py_DECREF(m);
+        return nullptr;
+    }
     return m;
 }
