@@ -211,7 +211,8 @@ size_t pb_op_page_fork_workspace(int32_t out_rows, int32_t n_pages);
  * attention, quant_q8, gemm_q8 (o, onto the stream), norm_q8, gemm_q8 (fc1),
  * quant_q8, gemm_q8 (fc2).  Calls only enqueue kernels, allocate nothing and can be
  * captured into a HIP graph; every buffer and the stream belong to the current
- * device; outputs must not overlap inputs or each other, but where said.
+ * device; outputs must not overlap inputs or each other, but where said (an operand
+ * is taken to reach from its first element to its last: columns of one matrix overlap).
  *
  * A row y in 8 bits: scale = max |y| / 127 as fp32, q = y / scale to the nearest
  * integer, ties to even.  (Formed in fp64 from the operands as they are stored:
@@ -238,7 +239,9 @@ int pb_op_quant_q8(int32_t dtype, const void* x, int64_t ld_x, int32_t x_f32, in
                    float* scale, int32_t rows, int32_t cols, void* stream);
 
 /* Y[m, n] = sx[m] sw[n] sum_k X[m, k] W[n, k] + bias[n], the sum exact in 32 bits,
- * with the epilogues of pb_op_gemm and one that stores fp32:
+ * formed as (sx sum) sw + bias in fp32 (the first product rounded, so it has to be a
+ * float itself: |sx sum| below 2^128), with the epilogues of pb_op_gemm and one that
+ * stores fp32:
  *   epi 0: C = dt(Y * (n < qcols ? qscale : 1))
  *   epi 1: C = dt(max(Y, 0))
  *   epi 2: R += Y

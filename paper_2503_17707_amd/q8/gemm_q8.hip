@@ -7,7 +7,7 @@
 // one token.  Lane l gives 16 bytes of row l % 16, the 16 at K offset 16 (l / 16) of
 // the step's 64; which of the 64 a lane holds does not matter as long as both operands
 // agree, and sums of integers do not depend on their order: every kernel and split gives
-// the same bits, so a rule of predicted times chooses freely among them (below).
+// the same bits, so a rule of predicted times chooses freely among them (gemm_q8_plan.h).
 //
 // What bounds them: one to some sixty tokens, reading the weights once; thousands, the
 // matrix units (2 M N K operations, twice those of 16 bits a cycle) about as much as the

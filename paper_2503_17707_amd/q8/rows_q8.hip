@@ -7,8 +7,11 @@
 // about 2^-45 of the border of two integers, and neither the order of a sum nor the
 // split of a row over lanes shows in them.  (In fp32 one number in some 50 000 would
 // be off by one step.)  CDNA4 does fp64 outside the matrix units at half the rate of
-// fp32; the fifteen or so such operations an element keep the vector units busy for up to
-// 0.7 of the time that memory takes.
+// fp32.  A layer norm with a bias takes some fourteen such operations an element and, of rows
+// of several pieces a thread, eight or nine conversions (an element is widened again for each
+// use).  With a delta to read and a sum to write that keeps the vector units busy for two thirds
+// of the time; without, it is the bound: 4096 rows of 9216 in fp32 62 us, 3.1 TB/s, the vector
+// units 0.78 busy (RMS without a bias, nine operations: 44 us, 4.3 TB/s).
 //
 // Both read a row once into registers (fp32) and write it once: 4096 rows of 9216, fp32
 // stream and fp16 delta, 82-89 us (4.7-5.1 TB/s, a large copy 4.76); 4096 of 36864 in fp16
@@ -522,7 +525,7 @@ int row_blocks(int rows, int per_block) {
 template <typename T, typename S, int VEC, int NV, int LANES>
 void norm_nv(const NormQ8Params& p, int threads, hipStream_t s) {
     int blocks = row_blocks(p.rows, LANES ? 256 / LANES : 1);
-    if (loads_ahead(VEC, NV, LANES)) blocks = std::min(blocks, 256 * (1024 / threads));  // 16 waves a CU
+    if (loads_ahead(VEC, NV, LANES)) blocks = std::min(blocks, 256 * (1024 / threads));  // whole blocks of 16 waves a CU
     if (p.b) PB_LAUNCH((norm_q8_kernel<T, S, VEC, NV, LANES, true>), blocks, threads, 0, s, p);
     else PB_LAUNCH((norm_q8_kernel<T, S, VEC, NV, LANES, false>), blocks, threads, 0, s, p);
 }
@@ -534,10 +537,13 @@ void quant_nv(const QuantQ8Params& p, hipStream_t s) {
 
 // Rows of up to 128 pieces share waves.  Longer ones have a block each, of a piece (16 bits) or
 // two (fp32) a thread, as many waves as may be; from there on rows are walked over with the
-// next one's loads in flight, 12 fp32 or 16 16-bit elements a thread, which leaves 16 waves a CU
+// next one's loads in flight, 12 fp32 or 16 16-bit elements a thread
 // (30 M elements in fp32, two pieces a thread without loads ahead -> three with: rows of 4104
 // 90 -> 78 us, 6144 72 -> 69, 8192 95 -> 76, but 3600 71 -> 83; in fp16, one piece -> two: 8192
 // 58 -> 53, 6656 64 -> 60, 6144 59 -> 62).  16 fp32 elements leave no registers to load ahead.
+// A CU gets the whole blocks that 16 waves hold: 9 waves to 16, fewest just past 512 threads (layer norm
+// of 30 M elements with a delta, fp32: 6144 67 us, 6148 81, 7168 76, 8192 73; fp16: 8192 50, 8200 66, 9216
+// 61, 10240 58).
 template <typename T, typename S>
 void norm_type(const NormQ8Params& p, hipStream_t s) {
     constexpr int VEC = 16 / sizeof(S), MOST = 1024;
