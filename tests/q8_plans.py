@@ -163,7 +163,7 @@ CASES = [
 ]
 
 
-def checker(folder):
+def host_program(folder):
     """The host program that answers for the rule; None without a compiler."""
     hipcc = shutil.which("hipcc")
     if not hipcc:

@@ -6,7 +6,7 @@ import pytest
 def exe(tmp_path_factory):
     import q8_plans
 
-    path = q8_plans.checker(tmp_path_factory.mktemp("q8_plans"))
+    path = q8_plans.host_program(tmp_path_factory.mktemp("q8_plans"))
     if path is None:
         pytest.skip("hipcc not available")
     return path
